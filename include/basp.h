@@ -349,6 +349,73 @@ int basp_qkv_proj_rope(const basp_plan *plan, int hidden, const void *const *x_s
 int basp_out_proj(const basp_plan *plan, int hidden, const void *const *o_seq, const void *w_o,
                   void *const *y_seq, void *stream);
 
+/* ---- root-mean-square norms of every query and key head with the rotary position embedding in the same pass (the paper
+ * does not treat either; models with per-head norms, Qwen3 among them, put the norm between the projection and the
+ * rotation, so the rotation cannot sit in the projection's epilogue).  For every head vector x of D features:
+ *   z = x w / sqrt(mean(x^2) + eps),   y = R(pos) z     (rotation, tables and positions as in basp_qkv_proj_rope)
+ * q_seq, k_seq / q_out, k_out: sequence-sharded Q ([Bl][T][Hq][D]) and K; w_q, w_k: bf16 [D], shared by all heads.  fp32
+ * arithmetic, one rounding to bf16.  q_out[r] may be q_seq[r] itself (in place), k_out[r] k_seq[r]; no other overlap.
+ * Requires D a multiple of 16 up to 128 and eps > 0 (BASP_ERR_INVALID).  The tables need 4-byte alignment.
+ *
+ * The backward pass takes the norm's inputs again (so the forward must not have run in place), dq_out / dk_out = the
+ * gradients of q_out / k_out, and writes dq_seq, dk_seq (bf16; dq_seq[r] may be dq_out[r] itself) and dw_q, dw_k (fp32 [D],
+ * summed over all ranks, tokens and heads; written, not added to).  The same inputs give the same bits. */
+int basp_qk_norm_rope(const basp_plan *plan, const void *const *q_seq, const void *const *k_seq, const void *w_q,
+                      const void *w_k, const float *rope_cos, const float *rope_sin, float eps, void *const *q_out,
+                      void *const *k_out, void *stream);
+int basp_qk_norm_rope_bwd(const basp_plan *plan, const void *const *q_seq, const void *const *k_seq, const void *w_q,
+                          const void *w_k, const float *rope_cos, const float *rope_sin, float eps,
+                          const void *const *dq_out, const void *const *dk_out, void *const *dq_seq, void *const *dk_seq,
+                          float *dw_q, float *dw_k, void *workspace, size_t workspace_bytes, void *stream);
+size_t basp_qk_norm_rope_bwd_workspace_bytes(const basp_plan *plan);
+
+/* ---- what the layer's backward pass needs (Q, K, V, O, sequence-sharded) kept in 8 bits between the passes: about half
+ * the memory of the bf16 shards.  Per head vector x[D]:
+ *   scale = max|x| / 127,   code = round_half_even(x (127 / max|x|)),   brought back as bf16(code scale)
+ * (fp32 arithmetic), so an element is off by at most scale / 2 plus the rounding to bf16.  A vector that holds an infinity or
+ * a NaN comes back as NaN in all its elements; one whose max|x| is below 2^-100 as zeros.
+ *   basp_ckpt_pack         writes rank r's checkpoint: ckpt_shards[r], basp_ckpt_bytes(plan, r) bytes (0 for a NULL plan or a
+ *                          rank out of range)
+ *   basp_ckpt_reshard_s2h  the all-to-all of the four tensors from their checkpoints: head-sharded bf16 Q, K, V, O in one launch
+ *   basp_layer_bwd_ckpt    basp_layer_bwd_seq with the checkpoints in the place of q_seq, k_seq, v_seq and o_seq (same
+ *                          workspace).  The gradients are those of the attention at the values brought back, with the
+ *                          forward pass's lse.
+ * A checkpoint of rank r holds: int8 codes of Q [Bl][T][Hq][D], K, V [Bl][T][Hkv][D], O, then the fp32 scales of Q [Bl][T][Hq],
+ * K, V, O; every section is padded to a multiple of 16 bytes (T: the rank's own tokens per sequence).
+ * Requires D a multiple of 16 up to 128. */
+size_t basp_ckpt_bytes(const basp_plan *plan, int rank);
+int basp_ckpt_pack(const basp_plan *plan, const void *const *q_seq, const void *const *k_seq, const void *const *v_seq,
+                   const void *const *o_seq, void *const *ckpt_shards, void *stream);
+int basp_ckpt_reshard_s2h(const basp_plan *plan, const void *const *ckpt_shards, void *const *q_head, void *const *k_head,
+                          void *const *v_head, void *const *o_head, void *stream);
+int basp_layer_bwd_ckpt(const basp_plan *plan, const void *const *ckpt_shards, const float *const *lse_shards,
+                        const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq,
+                        void *workspace, size_t workspace_bytes, float softmax_scale, void *stream);
+
+/* ---- the training loss behind the last layer: softmax cross entropy of the language-model head on the ranks' sequence
+ * shards, without keeping the logits.  For a token with hidden state x (a row of x_seq[r], bf16 [Bl*T][hidden]) and label y:
+ *   z = x W^T  (w: bf16 [vocab][hidden], shared by all ranks),   lse = ln sum_v exp(z_v),   loss = lse - z_y
+ * labels[r]: int64 [Bl*T]; a label outside [0, vocab) (such as -100) marks a token without a loss: its loss is 0 and it has
+ * no part in the gradients.  loss_seq[r], lse_seq[r]: fp32 [Bl*T] (lse_seq may be NULL).  bf16 products with fp32 sums; the logits are not rounded.
+ *
+ * basp_lm_loss_grad also writes the gradients of sum_tokens g loss with g = token_weights[r][token] (fp32 [Bl*T]; NULL table:
+ * 1 each):  dz = g (softmax(z) - onehot(y)),  dx_seq[r] = dz W (bf16),  dw = sum dz^T x (bf16 [vocab][hidden]; summed in fp32, rounded
+ * once).  dz is rounded to bf16 as an operand.  A NULL dx_seq or dw (not both) leaves that gradient and its product out.  A token of weight 0 has no part in the gradients whatever its values.  Both
+ * gradients are written, not added to; the same inputs and piece_rows give the same bits.
+ * The rows are worked on in pieces of piece_rows (rounded up to 128; 0: 8192; at most 32768), 2 bytes per logit of one piece
+ * in the workspace, plus 4 vocab hidden bytes for the running sum of dw where there are several pieces.
+ * Requires hidden a multiple of 8 up to 65536 and vocab up to 2^24 (BASP_ERR_UNSUPPORTED; neither positive:
+ * BASP_ERR_INVALID); labels 8-byte aligned, the fp32 arrays 4-byte.  The size queries return 0 for what the call refuses. */
+int basp_lm_loss_fwd(const basp_plan *plan, int hidden, int vocab, const void *const *x_seq, const void *w,
+                     const long long *const *labels, float *const *loss_seq, float *const *lse_seq, void *workspace,
+                     size_t workspace_bytes, void *stream);
+size_t basp_lm_loss_fwd_workspace_bytes(const basp_plan *plan, int vocab);
+int basp_lm_loss_grad(const basp_plan *plan, int hidden, int vocab, const void *const *x_seq, const void *w,
+                      const long long *const *labels, const float *const *token_weights, float *const *loss_seq,
+                      float *const *lse_seq, void *const *dx_seq, void *dw, int piece_rows, void *workspace,
+                      size_t workspace_bytes, void *stream);
+size_t basp_lm_loss_grad_workspace_bytes(const basp_plan *plan, int hidden, int vocab, int piece_rows);
+
 /* ---- device status.  Every wait inside the kernels (on a shared-memory barrier) is bounded;
  * when one expires the kernel records where, lets its copies drain, frees its tensor memory
  * and returns.  basp_get_status synchronises `stream`, copies the four status words of the

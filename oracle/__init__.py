@@ -497,6 +497,81 @@ def qkv_proj_rope(X: np.ndarray, W: np.ndarray, Hq: int, Hkv: int, D: int, cos, 
     return rope(q, cos, sin, positions), rope(k, cos, sin, positions), v
 
 
+# --------------------------------------------------- head norms, 8-bit checkpoints, language-model loss
+def qk_norm_rope(x: np.ndarray, w: np.ndarray, cos, sin, positions, eps: float) -> np.ndarray:
+    """Root-mean-square norm of every head vector, x [tokens, H, D] and w [D] in fp64, then `rope`."""
+    x = np.asarray(x, dtype=np.float64)
+    return rope(x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * np.asarray(w, dtype=np.float64), cos, sin, positions)
+
+
+def qk_norm_rope_bwd(x: np.ndarray, w: np.ndarray, cos, sin, positions, eps: float, dy: np.ndarray) -> tuple:
+    """Gradients (dx, dw) of `qk_norm_rope` in fp64 by the chain rule, step by step: the rotation's transpose turns by the
+    opposite angle; z = n w; n = x / sqrt(s) with s = mean x^2 + eps and ds/dx = 2 x / D."""
+    x, w = np.asarray(x, dtype=np.float64), np.asarray(w, dtype=np.float64)
+    D = x.shape[-1]
+    s = (x * x).mean(-1, keepdims=True) + eps
+    n = x / np.sqrt(s)
+    dz = rope(dy, cos, -np.asarray(sin, dtype=np.float64), positions)
+    dn = dz * w
+    ds = (dn * x).sum(-1, keepdims=True) * (-0.5) * s ** -1.5
+    return dn / np.sqrt(s) + ds * 2.0 * x / D, (dz * n).sum((0, 1))
+
+
+def ckpt_codes(x: np.ndarray) -> tuple:
+    """8-bit codes [..., D] and fp32 scales [...] of head vectors x [..., D] (exact fp32 values of bf16 numbers): the fp32
+    arithmetic of the definition, one operation at a time.  A vector with a non-finite element has the scale NaN."""
+    x = np.asarray(x, dtype=np.float32)
+    with np.errstate(all="ignore"):
+        top = np.abs(x).max(-1)
+        zero, bad = top < np.float32(2.0 ** -100), ~np.isfinite(x).all(-1)
+        inv = np.where(zero | bad, np.float32(0), np.float32(127) / np.where(zero | bad, np.float32(1), top))
+        scale = np.where(bad, np.float32(np.nan), np.where(zero, np.float32(0), top / np.float32(127)))
+        codes = np.rint(np.where(bad[..., None], np.float32(0), x) * inv[..., None])
+    return codes.astype(np.int8), scale.astype(np.float32)
+
+
+def ckpt_values(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
+    """What the codes stand for, before the rounding to bf16 (fp32)."""
+    return codes.astype(np.float32) * np.asarray(scales, dtype=np.float32)[..., None]
+
+
+def attn_bwd_given(Q, K, V, O, lse, dO, scale: float | None = None, causal: bool = True) -> dict:
+    """Gradients of the attention at given values with the statistics of another evaluation: fp64 Q, O, dO [S, H, D],
+    K, V [S, Hkv, D], lse [H, S].  P = exp(scale q.k - lse), Delta = dO.O, dS = P (dO.v - Delta)."""
+    S, H, D = Q.shape
+    g = H // K.shape[1]
+    scale = _scale(scale, D)
+    dQ, dK, dV = np.zeros(Q.shape), np.zeros(K.shape), np.zeros(V.shape)
+    mask = np.tril(np.ones((S, S), dtype=bool)) if causal else np.ones((S, S), dtype=bool)
+    for h in range(H):
+        k, v = K[:, h // g], V[:, h // g]
+        P = np.where(mask, np.exp(scale * Q[:, h] @ k.T - lse[h][:, None]), 0.0)
+        dS = P * (dO[:, h] @ v.T - (dO[:, h] * O[:, h]).sum(-1, keepdims=True))
+        dQ[:, h] = scale * dS @ k
+        dK[:, h // g] += scale * dS.T @ Q[:, h]
+        dV[:, h // g] += P.T @ dO[:, h]
+    return dict(dQ=dQ, dK=dK, dV=dV)
+
+
+def lm_loss(x: np.ndarray, w: np.ndarray, labels: np.ndarray, weights: np.ndarray | None = None) -> dict:
+    """Softmax cross entropy of z = x w^T in fp64: x [tokens, hidden], w [vocab, hidden], labels [tokens] (outside
+    [0, vocab): no loss).  With weights [tokens] also the gradients of sum(weights * loss)."""
+    x, w = np.asarray(x, dtype=np.float64), np.asarray(w, dtype=np.float64)
+    valid = (labels >= 0) & (labels < w.shape[0])
+    rows = np.arange(x.shape[0])
+    at = np.where(valid, labels, 0)
+    z = x @ w.T
+    top = z.max(-1, keepdims=True)
+    lse = top[:, 0] + np.log(np.exp(z - top).sum(-1))
+    out = dict(loss=np.where(valid, lse - z[rows, at], 0.0), lse=lse)
+    if weights is not None:
+        dz = np.exp(z - lse[:, None])
+        dz[rows, at] -= 1.0
+        dz *= np.where(valid, weights, 0.0)[:, None]
+        out.update(dz=dz, dx=dz @ w, dw=dz.T @ x)
+    return out
+
+
 # ----------------------------------------------------------------- bf16 helpers
 def bf16_bits_to_f64(bits: np.ndarray) -> np.ndarray:
     """Exact widening of bf16 bit patterns to fp64."""

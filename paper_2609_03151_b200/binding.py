@@ -32,6 +32,9 @@ EXPORTS = [
     "basp_strerror", "basp_last_cuda_error", "basp_launch_count", "basp_selftest_wait_timeout", "basp_qkv_proj", "basp_out_proj",
     "basp_reshard_qkv_s2h_ranks", "basp_reshard_h2s_ranks", "basp_attn_fwd_ranks", "basp_layer_fwd_fused_ranks",
     "basp_qkv_proj_rope", "basp_layer_bwd_seq", "basp_layer_bwd_seq_workspace_bytes", "basp_plan_create_parts", "basp_attn_bwd_deterministic",
+    "basp_qk_norm_rope", "basp_qk_norm_rope_bwd", "basp_qk_norm_rope_bwd_workspace_bytes",
+    "basp_ckpt_bytes", "basp_ckpt_pack", "basp_ckpt_reshard_s2h", "basp_layer_bwd_ckpt",
+    "basp_lm_loss_fwd", "basp_lm_loss_fwd_workspace_bytes", "basp_lm_loss_grad", "basp_lm_loss_grad_workspace_bytes",
 ]
 
 
@@ -88,6 +91,18 @@ lib.basp_selftest_wait_timeout.argtypes = [ctypes.c_uint, c_void_p]
 lib.basp_qkv_proj.argtypes = [c_void_p, c_int, _PP, c_void_p, _PP, _PP, _PP, c_void_p]
 lib.basp_out_proj.argtypes = [c_void_p, c_int, _PP, c_void_p, _PP, c_void_p]
 lib.basp_qkv_proj_rope.argtypes = [c_void_p, c_int, _PP, c_void_p, c_void_p, c_void_p, _PP, _PP, _PP, c_void_p]
+lib.basp_qk_norm_rope.argtypes = [c_void_p, _PP, _PP] + [c_void_p] * 4 + [c_float, _PP, _PP, c_void_p]
+lib.basp_qk_norm_rope_bwd.argtypes = [c_void_p, _PP, _PP] + [c_void_p] * 4 + [c_float] + [_PP] * 4 + \
+    [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+lib.basp_ckpt_pack.argtypes = [c_void_p] + [_PP] * 5 + [c_void_p]
+lib.basp_ckpt_reshard_s2h.argtypes = [c_void_p] + [_PP] * 5 + [c_void_p]
+lib.basp_layer_bwd_ckpt.argtypes = [c_void_p] + [_PP] * 6 + [c_void_p, c_size_t, c_float, c_void_p]
+lib.basp_lm_loss_fwd.argtypes = [c_void_p, c_int, c_int, _PP, c_void_p, _PP, _PP, _PP, c_void_p, c_size_t, c_void_p]
+lib.basp_lm_loss_grad.argtypes = [c_void_p, c_int, c_int, _PP, c_void_p] + [_PP] * 5 + [c_void_p, c_int, c_void_p, c_size_t, c_void_p]
+for _n, _a in (("basp_qk_norm_rope_bwd_workspace_bytes", []), ("basp_ckpt_bytes", [c_int]),
+               ("basp_lm_loss_fwd_workspace_bytes", [c_int]), ("basp_lm_loss_grad_workspace_bytes", [c_int] * 3)):
+    getattr(lib, _n).argtypes = [c_void_p] + _a
+    getattr(lib, _n).restype = c_size_t
 lib.basp_strerror.argtypes = [c_int]
 lib.basp_strerror.restype = c_char_p
 lib.basp_last_cuda_error.restype = c_char_p
@@ -404,6 +419,138 @@ def basp_out_proj(plan, hidden, o_seq, w_o, y_seq, stream=None):
     n = plan.N
     _check(lib.basp_out_proj(plan.handle, int(hidden), _ptrs(o_seq, n), c_void_p(w_o.data_ptr()), _ptrs(y_seq, n),
                              _stream(stream)), "basp_out_proj")
+
+
+def _typed(tensors, dtype, numel, what):
+    """Refuses tensors that the library would misread (it sees addresses only): wrong type or size, gaps between the
+    elements, not in the current device's memory.  Raw addresses pass as they are."""
+    for i, t in enumerate(tensors or ()):
+        if not isinstance(t, torch.Tensor):
+            continue
+        if t.dtype != dtype or t.numel() != numel(i) or not t.is_contiguous():
+            raise ValueError(f"{what}[{i}]: expected {numel(i)} contiguous elements of {dtype}, got {tuple(t.shape)} of "
+                             f"{t.dtype}" + ("" if t.is_contiguous() else ", not contiguous"))
+        if not t.is_cuda:
+            raise ValueError(f"{what}[{i}] is on {t.device}: the library works on device memory")
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{what}[{i}] is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return tensors
+
+
+def _addr(t, dtype, numel, what):
+    if t is None:
+        return None
+    _typed([t], dtype, lambda i: numel, what)
+    return c_void_p(t.data_ptr() if hasattr(t, "data_ptr") else int(t))
+
+
+def _space(workspace):
+    """Address and size of a workspace tensor."""
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected contiguous device memory, got a tensor on {workspace.device}")
+    if workspace.device.index != torch.cuda.current_device():
+        raise ValueError(f"workspace is on {workspace.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size()
+
+
+def _shards(plan, tensors, per_token, what, dtype=torch.bfloat16):
+    """Pointer table of sequence shards with `per_token` elements per token."""
+    return _ptrs(_typed(tensors, dtype, lambda r: plan.Bl * plan.rank_tokens(r) * per_token, what), plan.N)
+
+
+def basp_qk_norm_rope(plan, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, q_out, k_out, eps=1e-6, stream=None):
+    """Head norms of Q and K with the rotary embedding: z = x w / sqrt(mean(x^2) + eps), then the rotation of
+    basp_qkv_proj_rope (same feature-major tables).  q_out[r] may be q_seq[r], k_out[r] may be k_seq[r]."""
+    q, k, table = plan.Hq * plan.D, plan.Hkv * plan.D, plan.D // 2 * plan.S
+    _check(lib.basp_qk_norm_rope(plan.handle, _shards(plan, q_seq, q, "q_seq"), _shards(plan, k_seq, k, "k_seq"),
+                                 _addr(w_q, torch.bfloat16, plan.D, "w_q"), _addr(w_k, torch.bfloat16, plan.D, "w_k"),
+                                 _addr(rope_cos, torch.float32, table, "rope_cos"),
+                                 _addr(rope_sin, torch.float32, table, "rope_sin"), eps, _shards(plan, q_out, q, "q_out"),
+                                 _shards(plan, k_out, k, "k_out"), _stream(stream)), "basp_qk_norm_rope")
+
+
+def basp_qk_norm_rope_bwd_workspace_bytes(plan) -> int:
+    return int(lib.basp_qk_norm_rope_bwd_workspace_bytes(plan.handle))
+
+
+def basp_qk_norm_rope_bwd(plan, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, dq_out, dk_out, dq_seq, dk_seq, dw_q, dw_k,
+                          workspace, eps=1e-6, stream=None):
+    """Gradients of basp_qk_norm_rope: dq_seq, dk_seq (bf16; may be dq_out, dk_out themselves) and dw_q, dw_k (fp32 [D])."""
+    q, k, table = plan.Hq * plan.D, plan.Hkv * plan.D, plan.D // 2 * plan.S
+    _check(lib.basp_qk_norm_rope_bwd(plan.handle, _shards(plan, q_seq, q, "q_seq"), _shards(plan, k_seq, k, "k_seq"),
+                                     _addr(w_q, torch.bfloat16, plan.D, "w_q"), _addr(w_k, torch.bfloat16, plan.D, "w_k"),
+                                     _addr(rope_cos, torch.float32, table, "rope_cos"),
+                                     _addr(rope_sin, torch.float32, table, "rope_sin"), eps,
+                                     _shards(plan, dq_out, q, "dq_out"), _shards(plan, dk_out, k, "dk_out"),
+                                     _shards(plan, dq_seq, q, "dq_seq"), _shards(plan, dk_seq, k, "dk_seq"),
+                                     _addr(dw_q, torch.float32, plan.D, "dw_q"), _addr(dw_k, torch.float32, plan.D, "dw_k"),
+                                     *_space(workspace), _stream(stream)), "basp_qk_norm_rope_bwd")
+
+
+def basp_ckpt_bytes(plan, rank) -> int:
+    """Bytes of rank's 8-bit checkpoint of Q, K, V and O."""
+    return int(lib.basp_ckpt_bytes(plan.handle, int(rank)))
+
+
+def _ckpt(plan, ckpt):
+    return _ptrs(_typed(ckpt, torch.uint8, lambda r: basp_ckpt_bytes(plan, r), "ckpt"), plan.N)
+
+
+def basp_ckpt_pack(plan, q_seq, k_seq, v_seq, o_seq, ckpt, stream=None):
+    """Q, K, V and O to 8 bits with one scale per head vector; ckpt[r]: uint8 tensor of basp_ckpt_bytes(plan, r)."""
+    q, k = plan.Hq * plan.D, plan.Hkv * plan.D
+    _check(lib.basp_ckpt_pack(plan.handle, _shards(plan, q_seq, q, "q_seq"), _shards(plan, k_seq, k, "k_seq"),
+                              _shards(plan, v_seq, k, "v_seq"), _shards(plan, o_seq, q, "o_seq"), _ckpt(plan, ckpt),
+                              _stream(stream)), "basp_ckpt_pack")
+
+
+def basp_ckpt_reshard_s2h(plan, ckpt, q_head, k_head, v_head, o_head, stream=None):
+    """Checkpoints to head-sharded bf16 Q, K, V and O: the reading back and the all-to-all in one launch."""
+    heads = [_ptrs(_typed(t, torch.bfloat16, lambda r, h=h: plan.Bl * plan.S * h * plan.D, n), plan.N)
+             for n, t, h in (("q_head", q_head, plan.Hq_l), ("k_head", k_head, plan.Hkv_l), ("v_head", v_head, plan.Hkv_l),
+                             ("o_head", o_head, plan.Hq_l))]
+    _check(lib.basp_ckpt_reshard_s2h(plan.handle, _ckpt(plan, ckpt), *heads, _stream(stream)), "basp_ckpt_reshard_s2h")
+
+
+def basp_layer_bwd_ckpt(plan, ckpt, lse_shards, do_seq, dq_seq, dk_seq, dv_seq, workspace, softmax_scale=0.0, stream=None):
+    """basp_layer_bwd_seq from the 8-bit checkpoints (workspace: basp_layer_bwd_seq_workspace_bytes)."""
+    q, k = plan.Hq * plan.D, plan.Hkv * plan.D
+    lse = _typed(lse_shards, torch.float32, lambda r: plan.Bl * plan.Hq_l * plan.S, "lse_shards")
+    _check(lib.basp_layer_bwd_ckpt(plan.handle, _ckpt(plan, ckpt), _ptrs(lse, plan.N), _shards(plan, do_seq, q, "do_seq"),
+                                   _shards(plan, dq_seq, q, "dq_seq"), _shards(plan, dk_seq, k, "dk_seq"),
+                                   _shards(plan, dv_seq, k, "dv_seq"), *_space(workspace), softmax_scale, _stream(stream)),
+           "basp_layer_bwd_ckpt")
+
+
+def basp_lm_loss_fwd_workspace_bytes(plan, vocab) -> int:
+    return int(lib.basp_lm_loss_fwd_workspace_bytes(plan.handle, int(vocab)))
+
+
+def basp_lm_loss_grad_workspace_bytes(plan, hidden, vocab, piece_rows=0) -> int:
+    return int(lib.basp_lm_loss_grad_workspace_bytes(plan.handle, int(hidden), int(vocab), int(piece_rows)))
+
+
+def basp_lm_loss_fwd(plan, hidden, vocab, x_seq, w, labels, loss_seq, lse_seq, workspace, stream=None):
+    """Per-token cross entropy of softmax(x W^T) against `labels` (int64; outside [0, vocab): no loss) and the log-sum-exp
+    (lse_seq may be None), fp32."""
+    _check(lib.basp_lm_loss_fwd(plan.handle, int(hidden), int(vocab), _shards(plan, x_seq, hidden, "x_seq"),
+                                _addr(w, torch.bfloat16, vocab * hidden, "w"), _shards(plan, labels, 1, "labels", torch.int64),
+                                _shards(plan, loss_seq, 1, "loss_seq", torch.float32),
+                                _shards(plan, lse_seq, 1, "lse_seq", torch.float32), *_space(workspace), _stream(stream)),
+           "basp_lm_loss_fwd")
+
+
+def basp_lm_loss_grad(plan, hidden, vocab, x_seq, w, labels, token_weights, loss_seq, lse_seq, dx_seq, dw, workspace,
+                      piece_rows=0, stream=None):
+    """basp_lm_loss_fwd together with the gradients of sum(token_weights * loss): dx_seq and dw, bf16 (token_weights: fp32
+    shards, or None for 1 each; dx_seq or dw None: not wanted)."""
+    _check(lib.basp_lm_loss_grad(plan.handle, int(hidden), int(vocab), _shards(plan, x_seq, hidden, "x_seq"),
+                                 _addr(w, torch.bfloat16, vocab * hidden, "w"), _shards(plan, labels, 1, "labels", torch.int64),
+                                 _shards(plan, token_weights, 1, "token_weights", torch.float32),
+                                 _shards(plan, loss_seq, 1, "loss_seq", torch.float32),
+                                 _shards(plan, lse_seq, 1, "lse_seq", torch.float32), _shards(plan, dx_seq, hidden, "dx_seq"),
+                                 _addr(dw, torch.bfloat16, vocab * hidden, "dw"), int(piece_rows), *_space(workspace),
+                                 _stream(stream)), "basp_lm_loss_grad")
 
 
 def basp_selftest_wait_timeout(limit_us: int, stream=None):

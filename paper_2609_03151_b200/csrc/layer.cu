@@ -106,11 +106,13 @@ extern "C" size_t basp_layer_bwd_seq_workspace_bytes(const basp_plan *p) {
     return (size_t)p->N * (4 * q_head_bytes(p) + 4 * kv_head_bytes(p)) + basp_attn_bwd_workspace_bytes(p);
 }
 
-extern "C" int basp_layer_bwd_seq(const basp_plan *p, const void *const *q_seq, const void *const *k_seq,
-                                  const void *const *v_seq, const void *const *o_seq, const float *const *lse_shards,
-                                  const void *const *do_seq, void *const *dq_seq, void *const *dk_seq,
-                                  void *const *dv_seq, void *workspace, size_t workspace_bytes, float softmax_scale,
-                                  void *stream) {
+namespace {
+// The layer's backward pass where no head-sharded copies were kept: `restore` brings Q, K, V and O back head-sharded, the
+// rest (exchange of dO, attention backward, exchanges of the gradients) follows.
+template <typename Restore>
+int layer_bwd_restored(const basp_plan *p, Restore &&restore, const float *const *lse_shards, const void *const *do_seq,
+                       void *const *dq_seq, void *const *dk_seq, void *const *dv_seq, void *workspace, size_t workspace_bytes,
+                       float softmax_scale, void *stream) {
     if (!p || !workspace) return BASP_ERR_NULL;
     if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
     if (!aligned16(workspace)) return BASP_ERR_ALIGN;
@@ -131,9 +133,7 @@ extern "C" int basp_layer_bwd_seq(const basp_plan *p, const void *const *q_seq, 
         dvh[r] = w + n * (4 * qb + 3 * kb) + (size_t)r * kb;
     }
     char *bwd_ws = w + n * (4 * qb + 4 * kb);
-    int rc = basp_reshard_qkv_s2h(p, q_seq, k_seq, v_seq, qh, kh, vh, stream);
-    if (rc != BASP_OK) return rc;
-    rc = basp_reshard_s2h(p, p->Hq, o_seq, oh, stream);
+    int rc = restore(qh, kh, vh, oh);
     if (rc != BASP_OK) return rc;
     rc = basp_reshard_s2h(p, p->Hq, do_seq, doh, stream);
     if (rc != BASP_OK) return rc;
@@ -141,6 +141,30 @@ extern "C" int basp_layer_bwd_seq(const basp_plan *p, const void *const *q_seq, 
                        softmax_scale, stream);
     if (rc != BASP_OK) return rc;
     return basp_reshard_grads_h2s(p, dqh, dkh, dvh, dq_seq, dk_seq, dv_seq, stream);
+}
+}  // namespace
+
+extern "C" int basp_layer_bwd_seq(const basp_plan *p, const void *const *q_seq, const void *const *k_seq,
+                                  const void *const *v_seq, const void *const *o_seq, const float *const *lse_shards,
+                                  const void *const *do_seq, void *const *dq_seq, void *const *dk_seq,
+                                  void *const *dv_seq, void *workspace, size_t workspace_bytes, float softmax_scale,
+                                  void *stream) {
+    auto restore = [&](void *const *qh, void *const *kh, void *const *vh, void *const *oh) {
+        const int rc = basp_reshard_qkv_s2h(p, q_seq, k_seq, v_seq, qh, kh, vh, stream);
+        return rc != BASP_OK ? rc : basp_reshard_s2h(p, p->Hq, o_seq, oh, stream);
+    };
+    return layer_bwd_restored(p, restore, lse_shards, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes,
+                              softmax_scale, stream);
+}
+
+extern "C" int basp_layer_bwd_ckpt(const basp_plan *p, const void *const *ckpt_shards, const float *const *lse_shards,
+                                   const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq,
+                                   void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
+    auto restore = [&](void *const *qh, void *const *kh, void *const *vh, void *const *oh) {
+        return basp_ckpt_reshard_s2h(p, ckpt_shards, qh, kh, vh, oh, stream);
+    };
+    return layer_bwd_restored(p, restore, lse_shards, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes,
+                              softmax_scale, stream);
 }
 
 namespace {
