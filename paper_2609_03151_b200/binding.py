@@ -91,14 +91,14 @@ lib.basp_selftest_wait_timeout.argtypes = [ctypes.c_uint, c_void_p]
 lib.basp_qkv_proj.argtypes = [c_void_p, c_int, _PP, c_void_p, _PP, _PP, _PP, c_void_p]
 lib.basp_out_proj.argtypes = [c_void_p, c_int, _PP, c_void_p, _PP, c_void_p]
 lib.basp_qkv_proj_rope.argtypes = [c_void_p, c_int, _PP, c_void_p, c_void_p, c_void_p, _PP, _PP, _PP, c_void_p]
-lib.basp_qk_norm_rope.argtypes = [c_void_p, _PP, _PP] + [c_void_p] * 4 + [c_float, _PP, _PP, c_void_p]
-lib.basp_qk_norm_rope_bwd.argtypes = [c_void_p, _PP, _PP] + [c_void_p] * 4 + [c_float] + [_PP] * 4 + \
-    [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
-lib.basp_ckpt_pack.argtypes = [c_void_p] + [_PP] * 5 + [c_void_p]
-lib.basp_ckpt_reshard_s2h.argtypes = [c_void_p] + [_PP] * 5 + [c_void_p]
-lib.basp_layer_bwd_ckpt.argtypes = [c_void_p] + [_PP] * 6 + [c_void_p, c_size_t, c_float, c_void_p]
-lib.basp_lm_loss_fwd.argtypes = [c_void_p, c_int, c_int, _PP, c_void_p, _PP, _PP, _PP, c_void_p, c_size_t, c_void_p]
-lib.basp_lm_loss_grad.argtypes = [c_void_p, c_int, c_int, _PP, c_void_p] + [_PP] * 5 + [c_void_p, c_int, c_void_p, c_size_t, c_void_p]
+# the calls below take their tables as addresses (see _Marshal)
+lib.basp_qk_norm_rope.argtypes = [c_void_p] * 7 + [c_float] + [c_void_p] * 3
+lib.basp_qk_norm_rope_bwd.argtypes = [c_void_p] * 7 + [c_float] + [c_void_p] * 7 + [c_size_t, c_void_p]
+lib.basp_ckpt_pack.argtypes = [c_void_p] * 7
+lib.basp_ckpt_reshard_s2h.argtypes = [c_void_p] * 7
+lib.basp_layer_bwd_ckpt.argtypes = [c_void_p] * 8 + [c_size_t, c_float, c_void_p]
+lib.basp_lm_loss_fwd.argtypes = [c_void_p, c_int, c_int] + [c_void_p] * 6 + [c_size_t, c_void_p]
+lib.basp_lm_loss_grad.argtypes = [c_void_p, c_int, c_int] + [c_void_p] * 8 + [c_int, c_void_p, c_size_t, c_void_p]
 for _n, _a in (("basp_qk_norm_rope_bwd_workspace_bytes", []), ("basp_ckpt_bytes", [c_int]),
                ("basp_lm_loss_fwd_workspace_bytes", [c_int]), ("basp_lm_loss_grad_workspace_bytes", [c_int] * 3)):
     getattr(lib, _n).argtypes = [c_void_p] + _a
@@ -153,6 +153,7 @@ class Plan:
         self.S, self.Hq, self.Hkv, self.D = cfg.seq_len, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
         self.Hq_l, self.Hkv_l = info.q_heads_per_rank, info.kv_heads_per_rank
         self.T_last = info.tokens_last_rank
+        self.sizes = {}        # elements of the ranks' shards, by elements per token
 
     def rank_tokens(self, r: int) -> int:
         """Tokens per sequence in rank r's sequence-sharded shards (the last rank of a group is short when the group
@@ -421,52 +422,95 @@ def basp_out_proj(plan, hidden, o_seq, w_o, y_seq, stream=None):
                              _stream(stream)), "basp_out_proj")
 
 
-def _typed(tensors, dtype, numel, what):
-    """Refuses tensors that the library would misread (it sees addresses only): wrong type or size, gaps between the
-    elements, not in the current device's memory.  Raw addresses pass as they are."""
-    for i, t in enumerate(tensors or ()):
-        if not isinstance(t, torch.Tensor):
-            continue
-        if t.dtype != dtype or t.numel() != numel(i) or not t.is_contiguous():
-            raise ValueError(f"{what}[{i}]: expected {numel(i)} contiguous elements of {dtype}, got {tuple(t.shape)} of "
-                             f"{t.dtype}" + ("" if t.is_contiguous() else ", not contiguous"))
-        if not t.is_cuda:
-            raise ValueError(f"{what}[{i}] is on {t.device}: the library works on device memory")
-        if t.device.index != torch.cuda.current_device():
-            raise ValueError(f"{what}[{i}] is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return tensors
+_T = torch.Tensor
+_numel, _contiguous, _device, _data_ptr, _dtype = _T.numel, _T.is_contiguous, _T.get_device, _T.data_ptr, _T.dtype.__get__
 
 
-def _addr(t, dtype, numel, what):
-    if t is None:
-        return None
-    _typed([t], dtype, lambda i: numel, what)
-    return c_void_p(t.data_ptr() if hasattr(t, "data_ptr") else int(t))
+class _Marshal:
+    """Pointer tables and checks of one call.  The library sees addresses only, so tensors that it would misread are refused
+    here: wrong type or size, gaps between the elements, not in the current device's memory.  Raw addresses and objects with a
+    data_ptr (as_shards) pass as they are.  Short calls take less time on the GPU than here, so all shards of a type are checked
+    together, by functions that loop outside the interpreter."""
+
+    __slots__ = ("device", "kept")
+
+    def __init__(self):
+        self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+        self.kept = []                 # the tables, while the call reads them
+
+    def address(self, t, dtype, numel, what):
+        if isinstance(t, _T):
+            if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+                raise ValueError(f"{what}: expected {numel} contiguous elements of {dtype}, got {tuple(t.shape)} of {t.dtype}"
+                                 + ("" if t.is_contiguous() else ", not contiguous"))
+            if not t.is_cuda:
+                raise ValueError(f"{what} is on {t.device}: the library works on device memory")
+            if t.get_device() != self.device:
+                raise ValueError(f"{what} is on {t.device}, the current device is cuda:{self.device}")
+            return t.data_ptr()
+        return None if t is None else t.data_ptr() if hasattr(t, "data_ptr") else int(t)
+
+    def tables(self, dtype, *named):
+        """Addresses of pointer tables, one for each (name, shards or None, tuple of their sizes in elements)."""
+        flat, sizes = [], ()
+        for what, shards, want in named:
+            if shards is not None:
+                if len(shards) != len(want):
+                    raise ValueError(f"expected {len(want)} shards, got {len(shards)}: {what}")
+                flat += shards
+                sizes += want
+        try:
+            right = tuple(map(_numel, flat)) == sizes and set(map(_dtype, flat)) == {dtype} and \
+                set(map(_device, flat)) == {self.device} and all(map(_contiguous, flat))
+        except TypeError:              # not all of them tensors
+            right = False
+        if right:
+            table = (c_void_p * len(flat))(*map(_data_ptr, flat))
+        else:
+            names = [f"{what}[{i}]" for what, shards, want in named if shards is not None for i in range(len(want))]
+            table = (c_void_p * len(flat))(*[self.address(t, dtype, n, what) for t, n, what in zip(flat, sizes, names)])
+        self.kept.append(table)
+        at, out = ctypes.addressof(table), []
+        for _, shards, want in named:
+            out.append(None if shards is None else at)
+            if shards is not None:
+                at += 8 * len(want)
+        return out
+
+    def space(self, workspace):
+        """Address and size of a workspace tensor."""
+        if workspace.get_device() != self.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected contiguous memory of the current device, got a tensor on {workspace.device}")
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+    def stream(self, stream):
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.device if self.device >= 0 else torch.cuda.current_device())
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _space(workspace):
-    """Address and size of a workspace tensor."""
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError(f"workspace: expected contiguous device memory, got a tensor on {workspace.device}")
-    if workspace.device.index != torch.cuda.current_device():
-        raise ValueError(f"workspace is on {workspace.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size()
+def _per_rank(plan, per_token):
+    """Elements of every rank's sequence shard with `per_token` elements per token."""
+    sizes = plan.sizes.get(per_token)
+    if sizes is None:
+        sizes = plan.sizes[per_token] = tuple(plan.Bl * plan.rank_tokens(r) * per_token for r in range(plan.N))
+    return sizes
 
 
-def _shards(plan, tensors, per_token, what, dtype=torch.bfloat16):
-    """Pointer table of sequence shards with `per_token` elements per token."""
-    return _ptrs(_typed(tensors, dtype, lambda r: plan.Bl * plan.rank_tokens(r) * per_token, what), plan.N)
+def _qk(plan):
+    return _per_rank(plan, plan.Hq * plan.D), _per_rank(plan, plan.Hkv * plan.D)
 
 
 def basp_qk_norm_rope(plan, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, q_out, k_out, eps=1e-6, stream=None):
     """Head norms of Q and K with the rotary embedding: z = x w / sqrt(mean(x^2) + eps), then the rotation of
     basp_qkv_proj_rope (same feature-major tables).  q_out[r] may be q_seq[r], k_out[r] may be k_seq[r]."""
-    q, k, table = plan.Hq * plan.D, plan.Hkv * plan.D, plan.D // 2 * plan.S
-    _check(lib.basp_qk_norm_rope(plan.handle, _shards(plan, q_seq, q, "q_seq"), _shards(plan, k_seq, k, "k_seq"),
-                                 _addr(w_q, torch.bfloat16, plan.D, "w_q"), _addr(w_k, torch.bfloat16, plan.D, "w_k"),
-                                 _addr(rope_cos, torch.float32, table, "rope_cos"),
-                                 _addr(rope_sin, torch.float32, table, "rope_sin"), eps, _shards(plan, q_out, q, "q_out"),
-                                 _shards(plan, k_out, k, "k_out"), _stream(stream)), "basp_qk_norm_rope")
+    m, D, table = _Marshal(), plan.D, plan.D // 2 * plan.S
+    q, k = _qk(plan)
+    x, xk, y, yk = m.tables(torch.bfloat16, ("q_seq", q_seq, q), ("k_seq", k_seq, k), ("q_out", q_out, q), ("k_out", k_out, k))
+    _check(lib.basp_qk_norm_rope(plan.handle, x, xk, m.address(w_q, torch.bfloat16, D, "w_q"),
+                                 m.address(w_k, torch.bfloat16, D, "w_k"), m.address(rope_cos, torch.float32, table, "rope_cos"),
+                                 m.address(rope_sin, torch.float32, table, "rope_sin"), eps, y, yk, m.stream(stream)),
+           "basp_qk_norm_rope")
 
 
 def basp_qk_norm_rope_bwd_workspace_bytes(plan) -> int:
@@ -476,15 +520,16 @@ def basp_qk_norm_rope_bwd_workspace_bytes(plan) -> int:
 def basp_qk_norm_rope_bwd(plan, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, dq_out, dk_out, dq_seq, dk_seq, dw_q, dw_k,
                           workspace, eps=1e-6, stream=None):
     """Gradients of basp_qk_norm_rope: dq_seq, dk_seq (bf16; may be dq_out, dk_out themselves) and dw_q, dw_k (fp32 [D])."""
-    q, k, table = plan.Hq * plan.D, plan.Hkv * plan.D, plan.D // 2 * plan.S
-    _check(lib.basp_qk_norm_rope_bwd(plan.handle, _shards(plan, q_seq, q, "q_seq"), _shards(plan, k_seq, k, "k_seq"),
-                                     _addr(w_q, torch.bfloat16, plan.D, "w_q"), _addr(w_k, torch.bfloat16, plan.D, "w_k"),
-                                     _addr(rope_cos, torch.float32, table, "rope_cos"),
-                                     _addr(rope_sin, torch.float32, table, "rope_sin"), eps,
-                                     _shards(plan, dq_out, q, "dq_out"), _shards(plan, dk_out, k, "dk_out"),
-                                     _shards(plan, dq_seq, q, "dq_seq"), _shards(plan, dk_seq, k, "dk_seq"),
-                                     _addr(dw_q, torch.float32, plan.D, "dw_q"), _addr(dw_k, torch.float32, plan.D, "dw_k"),
-                                     *_space(workspace), _stream(stream)), "basp_qk_norm_rope_bwd")
+    m, D, table = _Marshal(), plan.D, plan.D // 2 * plan.S
+    q, k = _qk(plan)
+    x, xk, dy, dyk, dx, dxk = m.tables(torch.bfloat16, ("q_seq", q_seq, q), ("k_seq", k_seq, k), ("dq_out", dq_out, q),
+                                       ("dk_out", dk_out, k), ("dq_seq", dq_seq, q), ("dk_seq", dk_seq, k))
+    _check(lib.basp_qk_norm_rope_bwd(plan.handle, x, xk, m.address(w_q, torch.bfloat16, D, "w_q"),
+                                     m.address(w_k, torch.bfloat16, D, "w_k"),
+                                     m.address(rope_cos, torch.float32, table, "rope_cos"),
+                                     m.address(rope_sin, torch.float32, table, "rope_sin"), eps, dy, dyk, dx, dxk,
+                                     m.address(dw_q, torch.float32, D, "dw_q"), m.address(dw_k, torch.float32, D, "dw_k"),
+                                     *m.space(workspace), m.stream(stream)), "basp_qk_norm_rope_bwd")
 
 
 def basp_ckpt_bytes(plan, rank) -> int:
@@ -492,34 +537,37 @@ def basp_ckpt_bytes(plan, rank) -> int:
     return int(lib.basp_ckpt_bytes(plan.handle, int(rank)))
 
 
-def _ckpt(plan, ckpt):
-    return _ptrs(_typed(ckpt, torch.uint8, lambda r: basp_ckpt_bytes(plan, r), "ckpt"), plan.N)
+def _ckpt(plan, m, ckpt):
+    sizes = plan.sizes.get("ckpt")
+    if sizes is None:
+        sizes = plan.sizes["ckpt"] = tuple(basp_ckpt_bytes(plan, r) for r in range(plan.N))
+    return m.tables(torch.uint8, ("ckpt", ckpt, sizes))[0]
 
 
 def basp_ckpt_pack(plan, q_seq, k_seq, v_seq, o_seq, ckpt, stream=None):
     """Q, K, V and O to 8 bits with one scale per head vector; ckpt[r]: uint8 tensor of basp_ckpt_bytes(plan, r)."""
-    q, k = plan.Hq * plan.D, plan.Hkv * plan.D
-    _check(lib.basp_ckpt_pack(plan.handle, _shards(plan, q_seq, q, "q_seq"), _shards(plan, k_seq, k, "k_seq"),
-                              _shards(plan, v_seq, k, "v_seq"), _shards(plan, o_seq, q, "o_seq"), _ckpt(plan, ckpt),
-                              _stream(stream)), "basp_ckpt_pack")
+    m = _Marshal()
+    q, k = _qk(plan)
+    t = m.tables(torch.bfloat16, ("q_seq", q_seq, q), ("k_seq", k_seq, k), ("v_seq", v_seq, k), ("o_seq", o_seq, q))
+    _check(lib.basp_ckpt_pack(plan.handle, *t, _ckpt(plan, m, ckpt), m.stream(stream)), "basp_ckpt_pack")
 
 
 def basp_ckpt_reshard_s2h(plan, ckpt, q_head, k_head, v_head, o_head, stream=None):
     """Checkpoints to head-sharded bf16 Q, K, V and O: the reading back and the all-to-all in one launch."""
-    heads = [_ptrs(_typed(t, torch.bfloat16, lambda r, h=h: plan.Bl * plan.S * h * plan.D, n), plan.N)
-             for n, t, h in (("q_head", q_head, plan.Hq_l), ("k_head", k_head, plan.Hkv_l), ("v_head", v_head, plan.Hkv_l),
-                             ("o_head", o_head, plan.Hq_l))]
-    _check(lib.basp_ckpt_reshard_s2h(plan.handle, _ckpt(plan, ckpt), *heads, _stream(stream)), "basp_ckpt_reshard_s2h")
+    m, vec = _Marshal(), plan.Bl * plan.S * plan.D
+    q, k = (vec * plan.Hq_l,) * plan.N, (vec * plan.Hkv_l,) * plan.N
+    t = m.tables(torch.bfloat16, ("q_head", q_head, q), ("k_head", k_head, k), ("v_head", v_head, k), ("o_head", o_head, q))
+    _check(lib.basp_ckpt_reshard_s2h(plan.handle, _ckpt(plan, m, ckpt), *t, m.stream(stream)), "basp_ckpt_reshard_s2h")
 
 
 def basp_layer_bwd_ckpt(plan, ckpt, lse_shards, do_seq, dq_seq, dk_seq, dv_seq, workspace, softmax_scale=0.0, stream=None):
     """basp_layer_bwd_seq from the 8-bit checkpoints (workspace: basp_layer_bwd_seq_workspace_bytes)."""
-    q, k = plan.Hq * plan.D, plan.Hkv * plan.D
-    lse = _typed(lse_shards, torch.float32, lambda r: plan.Bl * plan.Hq_l * plan.S, "lse_shards")
-    _check(lib.basp_layer_bwd_ckpt(plan.handle, _ckpt(plan, ckpt), _ptrs(lse, plan.N), _shards(plan, do_seq, q, "do_seq"),
-                                   _shards(plan, dq_seq, q, "dq_seq"), _shards(plan, dk_seq, k, "dk_seq"),
-                                   _shards(plan, dv_seq, k, "dv_seq"), *_space(workspace), softmax_scale, _stream(stream)),
-           "basp_layer_bwd_ckpt")
+    m = _Marshal()
+    q, k = _qk(plan)
+    (lse,) = m.tables(torch.float32, ("lse_shards", lse_shards, (plan.Bl * plan.Hq_l * plan.S,) * plan.N))
+    t = m.tables(torch.bfloat16, ("do_seq", do_seq, q), ("dq_seq", dq_seq, q), ("dk_seq", dk_seq, k), ("dv_seq", dv_seq, k))
+    _check(lib.basp_layer_bwd_ckpt(plan.handle, _ckpt(plan, m, ckpt), lse, *t, *m.space(workspace), softmax_scale,
+                                   m.stream(stream)), "basp_layer_bwd_ckpt")
 
 
 def basp_lm_loss_fwd_workspace_bytes(plan, vocab) -> int:
@@ -533,24 +581,25 @@ def basp_lm_loss_grad_workspace_bytes(plan, hidden, vocab, piece_rows=0) -> int:
 def basp_lm_loss_fwd(plan, hidden, vocab, x_seq, w, labels, loss_seq, lse_seq, workspace, stream=None):
     """Per-token cross entropy of softmax(x W^T) against `labels` (int64; outside [0, vocab): no loss) and the log-sum-exp
     (lse_seq may be None), fp32."""
-    _check(lib.basp_lm_loss_fwd(plan.handle, int(hidden), int(vocab), _shards(plan, x_seq, hidden, "x_seq"),
-                                _addr(w, torch.bfloat16, vocab * hidden, "w"), _shards(plan, labels, 1, "labels", torch.int64),
-                                _shards(plan, loss_seq, 1, "loss_seq", torch.float32),
-                                _shards(plan, lse_seq, 1, "lse_seq", torch.float32), *_space(workspace), _stream(stream)),
-           "basp_lm_loss_fwd")
+    m, n = _Marshal(), _per_rank(plan, 1)
+    (x,) = m.tables(torch.bfloat16, ("x_seq", x_seq, _per_rank(plan, hidden)))
+    (y,) = m.tables(torch.int64, ("labels", labels, n))
+    loss, lse = m.tables(torch.float32, ("loss_seq", loss_seq, n), ("lse_seq", lse_seq, n))
+    _check(lib.basp_lm_loss_fwd(plan.handle, int(hidden), int(vocab), x, m.address(w, torch.bfloat16, vocab * hidden, "w"), y,
+                                loss, lse, *m.space(workspace), m.stream(stream)), "basp_lm_loss_fwd")
 
 
 def basp_lm_loss_grad(plan, hidden, vocab, x_seq, w, labels, token_weights, loss_seq, lse_seq, dx_seq, dw, workspace,
                       piece_rows=0, stream=None):
     """basp_lm_loss_fwd together with the gradients of sum(token_weights * loss): dx_seq and dw, bf16 (token_weights: fp32
     shards, or None for 1 each; dx_seq or dw None: not wanted)."""
-    _check(lib.basp_lm_loss_grad(plan.handle, int(hidden), int(vocab), _shards(plan, x_seq, hidden, "x_seq"),
-                                 _addr(w, torch.bfloat16, vocab * hidden, "w"), _shards(plan, labels, 1, "labels", torch.int64),
-                                 _shards(plan, token_weights, 1, "token_weights", torch.float32),
-                                 _shards(plan, loss_seq, 1, "loss_seq", torch.float32),
-                                 _shards(plan, lse_seq, 1, "lse_seq", torch.float32), _shards(plan, dx_seq, hidden, "dx_seq"),
-                                 _addr(dw, torch.bfloat16, vocab * hidden, "dw"), int(piece_rows), *_space(workspace),
-                                 _stream(stream)), "basp_lm_loss_grad")
+    m, n, wide = _Marshal(), _per_rank(plan, 1), _per_rank(plan, hidden)
+    x, dx = m.tables(torch.bfloat16, ("x_seq", x_seq, wide), ("dx_seq", dx_seq, wide))
+    (y,) = m.tables(torch.int64, ("labels", labels, n))
+    g, loss, lse = m.tables(torch.float32, ("token_weights", token_weights, n), ("loss_seq", loss_seq, n), ("lse_seq", lse_seq, n))
+    _check(lib.basp_lm_loss_grad(plan.handle, int(hidden), int(vocab), x, m.address(w, torch.bfloat16, vocab * hidden, "w"), y, g,
+                                 loss, lse, dx, m.address(dw, torch.bfloat16, vocab * hidden, "dw"), int(piece_rows),
+                                 *m.space(workspace), m.stream(stream)), "basp_lm_loss_grad")
 
 
 def basp_selftest_wait_timeout(limit_us: int, stream=None):

@@ -5,8 +5,8 @@
 //   dz = g (softmax(z) - onehot(y)),       dx = dz W,       dW = sum_tokens dz^T x
 //
 // Three products, each 2 rows*vocab*hidden operations on the tensor cores, and one element-wise pass:
-//   (1) z = x W^T          epilogue: per row and 256-column tile the maximum m and the sum of exp(z - m), the target's
-//                          logit apart from the others; for the gradient also every logit as its distance below the tile's
+//   (1) z = x W^T          epilogue: per row and 128 columns the maximum m and the sum of exp(z - m), the target's
+//                          logit apart from the others; for the gradient also every logit as its distance below that
 //                          maximum, 16 bits: rn((m - z) log2(e) 2^10), saturating at 2^-64 of the maximum's probability
 //   (merge)                rows' statistics -> loss and lse
 //   (dz)                   in place: 16-bit distance -> bf16 dz (and the piece's rows of x side by side for (3), those without a
@@ -46,11 +46,17 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 192;
-constexpr int kBM = 128, kBN = 256, kBK = 64, kStages = 4;
-constexpr int kABytes = kBM * kBK * 2, kBBytes = kBN * kBK * 2;
+constexpr int kBM = 128, kBN = 256, kBK = 64;      // rows of an accumulator, columns of a tile, K block
+constexpr int kABytes = kBM * kBK * 2;
+template <bool kPair>
+constexpr int kRowsPerCta = kPair ? 2 * kBM : kBM;
+template <bool kPair>
+constexpr int kTileM = kPair ? 4 * kBM : kBM;
+constexpr int kThreads = 320;                      // TMA warp, MMA warp, eight epilogue warps
+constexpr int kStages = 4, kStageBytes = 48 << 10; // A 128 and B 256 rows of 128 bytes, or A 256 and half of B
 constexpr int kMnBlock = kBK * 64 * 2;             // one 64-column block of an MN-major operand: 64 rows of 128 bytes
 constexpr int kSms = 148;                          // of the GPU this code is written for; plans the split, not the grid
+constexpr int kStatCols = 128;                     // columns that share a maximum: as many as a thread holds in registers
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kCodeStep = 1024.f;                // distances in 2^-10 of log2
 constexpr float kCodeMax = 65535.f;                // and above: probability zero
@@ -79,18 +85,20 @@ __device__ __forceinline__ Token token_of(const Rows &s, int i) {
 
 template <int R>
 struct LossParams {
-    CUtensorMap x[R];          // (1): boxes of a slot's rows
+    CUtensorMap x[R];          // (1): boxes of one slot
     CUtensorMap w, dz;
     CUtensorMap kept;          // (3): the piece's rows of x, zero where a row has no part in the gradients
     const long long *label[R];
     __nv_bfloat16 *dx[R];
     Rows rows;
-    int tiles_m, tiles_n, k_blocks, splits;
+    int tiles_m, tiles_n, k_blocks, splits, group;
     int vocab, hidden;
+    bool wide;                 // (2), (3): every row of the result starts on a multiple of 32 bytes
     size_t pitch;              // columns of a row of 16-bit logits
     int piece_rows;
-    float2 *stats;             // [tiles_n][piece_rows]: maximum, sum
-    float *target;             // [piece_rows]: the target's logit
+    float2 *stats;             // [groups of kStatCols columns][piece_rows]: maximum, sum
+    unsigned *scale;           // bits of the largest |weight| of the piece: dz is in its units, so that equal weights leave
+                               // p - 1 as it is (rounding -1 g would be one relative error common to all tokens)
     uint16_t *codes;           // [piece_rows][pitch]
     float *partial;            // (2) with splits > 1: [splits][piece_rows][hidden]
     const float *acc_in;       // (3) sum of the earlier pieces, or NULL
@@ -116,225 +124,318 @@ struct Bars {
         }                                                                       \
     } while (0)
 
-// Tile coordinates of a work item.  (1): row tiles fastest, so the piece's x stays in L2 and W streams once; (2), (3):
-// column tiles of `hidden` fastest.
+// Tile coordinates of a work item: row tiles in groups, within a group row tiles fastest.  The SMs work on neighbouring
+// items at the same time, so a group's first operand stays in L2 while the second streams by.
 struct Item {
-    int m, n, kb0, kb1, split;
+    int m, n, kb0, kb1;
+    int split;
 };
 template <int kKind, int R>
 __device__ __forceinline__ Item item_of(const LossParams<R> &p, int i) {
     Item t;
     t.split = 0; t.kb0 = 0; t.kb1 = p.k_blocks;
-    if constexpr (kKind == kStats || kKind == kLogits) {
-        t.n = i / p.tiles_m;
-        t.m = i - t.n * p.tiles_m;
-    } else {
-        const int q = i / p.tiles_n;
-        t.n = i - q * p.tiles_n;
-        t.split = kKind == kDx ? q / p.tiles_m : 0;
-        t.m = q - t.split * p.tiles_m;
-        if constexpr (kKind == kDx) {
-            t.kb0 = (int)((long long)p.k_blocks * t.split / p.splits);
-            t.kb1 = (int)((long long)p.k_blocks * (t.split + 1) / p.splits);
-        }
+    if constexpr (kKind == kDx) {
+        const int tiles = p.tiles_m * p.tiles_n;
+        t.split = i / tiles;
+        i -= t.split * tiles;
+        t.kb0 = (int)((long long)p.k_blocks * t.split / p.splits);
+        t.kb1 = (int)((long long)p.k_blocks * (t.split + 1) / p.splits);
     }
+    const int per_group = p.group * p.tiles_n, g = i / per_group, m0 = g * p.group;
+    const int wide = min(p.group, p.tiles_m - m0);
+    i -= g * per_group;
+    t.n = i / wide;
+    t.m = m0 + i - t.n * wide;
     return t;
 }
 
-__device__ __forceinline__ void store_bf16x32(__nv_bfloat16 *dst, const float (&v)[32], int cols) {
+// 32 columns of a row, or its last `cols` (a multiple of 8).  wide: rows start on multiples of 32 bytes, whole sectors at a time
+__device__ __forceinline__ void store_bf16x32(__nv_bfloat16 *dst, const float (&v)[32], int cols, bool wide) {
+    uint32_t w[16];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (8 * i >= cols) break;                  // cols is a multiple of 8
-        uint4 o;
-        o.x = pack_bf16x2(v[8 * i + 0], v[8 * i + 1]); o.y = pack_bf16x2(v[8 * i + 2], v[8 * i + 3]);
-        o.z = pack_bf16x2(v[8 * i + 4], v[8 * i + 5]); o.w = pack_bf16x2(v[8 * i + 6], v[8 * i + 7]);
-        *reinterpret_cast<uint4 *>(dst + 8 * i) = o;
+    for (int i = 0; i < 16; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (16 * i < cols)
+                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                             :: "l"(dst + 16 * i), "r"(w[8 * i]), "r"(w[8 * i + 1]), "r"(w[8 * i + 2]), "r"(w[8 * i + 3]),
+                                "r"(w[8 * i + 4]), "r"(w[8 * i + 5]), "r"(w[8 * i + 6]), "r"(w[8 * i + 7]) : "memory");
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (8 * i < cols) *reinterpret_cast<uint4 *>(dst + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
 }
 
-template <int kKind, int R>
+// kPair = false: a CTA works on 128 x 256 tiles; its two accumulators take turns, so that the epilogue of one tile runs under
+// the main loop of the next.
+// kPair = true: two neighbouring CTAs (a cluster) work on one 512 x 256 tile, each with 256 of its rows and half of B; the two
+// accumulators of a CTA are the upper and lower 128 of its rows.  The last blocks of K are issued for the upper rows first, the
+// first blocks of the next tile too: either epilogue then runs under the other half's products.
+template <int kKind, int R, bool kPair>
 __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_constant__ LossParams<R> p) {
+    constexpr int kS = kStages, kRows = kRowsPerCta<kPair>, kBCols = kPair ? kBN / 2 : kBN;
+    constexpr int kA = kRows * kBK * 2, kB = kBCols * kBK * 2;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *sA = smem;                                    // kStages x 16 KiB
-    uint8_t *sB = smem + kStages * kABytes;                // kStages x 32 KiB
+    uint8_t *sA = smem;
+    uint8_t *sB = smem + kS * kA;
     __shared__ Bars bars;
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int total = p.tiles_m * p.tiles_n * p.splits;
+    const int half = kPair ? (int)cluster_rank() : 0;      // this CTA's rows and columns of the tile
+    const int first = kPair ? blockIdx.x >> 1 : blockIdx.x, step = kPair ? gridDim.x >> 1 : gridDim.x;
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(&bars.full[s], 1); mbar_init(&bars.empty[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&bars.acc_full[a], 1); mbar_init(&bars.acc_empty[a], 4); }
+        for (int s = 0; s < kS; ++s) { mbar_init(&bars.full[s], 1); mbar_init(&bars.empty[s], 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&bars.acc_full[a], 1); mbar_init(&bars.acc_empty[a], 8); }
         bars.abort_flag = 0;
         fence_mbar_init();
+        if (kKind == kLogits && blockIdx.x == 0) *p.scale = 0;
     }
-    if (warp == 1) { tmem_alloc(&bars.tmem_base, 512); tmem_relinquish(); }
+    if (warp == 1) {
+        if constexpr (kPair) { tmem_alloc_pair(&bars.tmem_base, 512); tmem_relinquish_pair(); }
+        else { tmem_alloc(&bars.tmem_base, 512); tmem_relinquish(); }
+    }
     tc_fence_before();
     __syncthreads();
+    if constexpr (kPair) cluster_sync();                   // both CTAs' barriers and tensor memory are there
     tc_fence_after();
     const uint32_t tmem = bars.tmem_base;
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer (lane 0 issues)
         uint32_t it = 0;
-        for (int i = blockIdx.x; i < total; i += gridDim.x) {
+        for (int i = first; i < total; i += step) {
             const Item t = item_of<kKind>(p, i);
+            const int m0 = t.m * kTileM<kPair> + half * kRows, n0 = t.n * kBN + half * kBCols;
+            int mine = 0;                                  // (1): slots of this CTA's rows
+            uint32_t expect = (kA + kB) * (kPair ? 2 : 1); // bytes of the tile's K block
+            if constexpr (kKind == kStats || kKind == kLogits) {
+                const int per_cta = kRows >> p.rows.slot_log2, rest = p.rows.slots - t.m * (kTileM<kPair> >> p.rows.slot_log2);
+                mine = min(per_cta, max(0, rest - half * per_cta));
+                expect = kB * (kPair ? 2 : 1) + (uint32_t)(min(rest, kPair ? 2 * per_cta : per_cta) << p.rows.slot_log2) * kBK * 2;
+            }
             for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
-                const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+                const uint32_t s = it % kS, ph = (it / kS) & 1;
                 LOSS_WAIT(&bars.empty[s], ph ^ 1, 0, kb);
                 if (lane == 0) {
-                    uint8_t *a = sA + s * kABytes, *b = sB + s * kBBytes;
-                    mbar_arrive_expect_tx(&bars.full[s], kABytes + kBBytes);
+                    uint8_t *a = sA + s * kA, *b = sB + s * kB;
+                    // a pair's loads are all counted on the first CTA's barrier
+                    const uint32_t bar = kPair ? map_to_rank(&bars.full[s], 0) : 0;
+                    if (half == 0) mbar_arrive_expect_tx(&bars.full[s], expect);
+                    auto load = [&](uint8_t *dst, const CUtensorMap *map, int c, int r) {
+                        if constexpr (kPair) tma_load_3d_pair(dst, map, bar, c, 0, r);
+                        else tma_load_3d(dst, map, &bars.full[s], c, 0, r);
+                    };
                     if constexpr (kKind == kStats || kKind == kLogits) {
-                        // a slot past the piece's end is read past its rank's last row: zeros
-                        const int slot = 1 << p.rows.slot_log2;
-                        for (int j = 0; j < kBM; j += slot) {
-                            const int sl = (t.m * kBM + j) >> p.rows.slot_log2, at = p.rows.slot_begin + sl;
-                            const bool in = sl < p.rows.slots;
-                            const int r = in ? at / p.rows.per_rank : 0;
-                            tma_load_3d(a + j * kBK * 2, &p.x[r], &bars.full[s], kb * kBK, 0,
-                                        (in ? at - r * p.rows.per_rank : p.rows.per_rank) << p.rows.slot_log2);
+                        // slots past the piece's end are left as they are: a row of A reaches its own row of the product only
+                        for (int j = 0; j < mine; ++j) {
+                            const int at = p.rows.slot_begin + (m0 >> p.rows.slot_log2) + j, r = at / p.rows.per_rank;
+                            load(a + (j << p.rows.slot_log2) * kBK * 2, &p.x[r], kb * kBK, (at - r * p.rows.per_rank) << p.rows.slot_log2);
                         }
-                        tma_load_3d(b, &p.w, &bars.full[s], kb * kBK, 0, t.n * kBN);
+                        load(b, &p.w, kb * kBK, n0);
                     } else if constexpr (kKind == kDx) {
-                        tma_load_3d(a, &p.dz, &bars.full[s], kb * kBK, 0, t.m * kBM);
 #pragma unroll
-                        for (int c = 0; c < kBN / 64; ++c)
-                            tma_load_3d(b + c * kMnBlock, &p.w, &bars.full[s], t.n * kBN + c * 64, 0, kb * kBK);
+                        for (int j = 0; j < kRows; j += kBM) load(a + j * kBK * 2, &p.dz, kb * kBK, m0 + j);
+#pragma unroll
+                        for (int c = 0; c < kBCols / 64; ++c) load(b + c * kMnBlock, &p.w, n0 + c * 64, kb * kBK);
                     } else {
 #pragma unroll
-                        for (int c = 0; c < kBM / 64; ++c)
-                            tma_load_3d(a + c * kMnBlock, &p.dz, &bars.full[s], t.m * kBM + c * 64, 0, kb * kBK);
+                        for (int c = 0; c < kRows / 64; ++c) load(a + c * kMnBlock, &p.dz, m0 + c * 64, kb * kBK);
 #pragma unroll
-                        for (int c = 0; c < kBN / 64; ++c)
-                            tma_load_3d(b + c * kMnBlock, &p.kept, &bars.full[s], t.n * kBN + c * 64, 0, kb * kBK);
+                        for (int c = 0; c < kBCols / 64; ++c) load(b + c * kMnBlock, &p.kept, n0 + c * 64, kb * kBK);
                     }
                 }
             }
         }
     } else if (warp == 1) {
-        // ------------------------------------------------------------------ MMA issuer (lane 0 issues)
-        const uint32_t idesc = make_idesc_bf16(kBM, kBN, kKind == kDw, kKind == kDx || kKind == kDw);
+        // ------------------------------------------------------------------ MMA issuer (lane 0 of the first CTA issues)
+        const uint32_t idesc = make_idesc_bf16(kPair ? 2 * kBM : kBM, kBN, kKind == kDw, kKind == kDx || kKind == kDw);
         const uint64_t desc_k = make_smem_desc_sw128(0, 16, 1024), desc_mn = make_smem_desc_sw128(0, kMnBlock, 1024);
         const uint64_t da0 = (kKind == kDw ? desc_mn : desc_k) | (uint64_t)(smem_u32(sA) >> 4);
         const uint64_t db0 = (kKind == kDx || kKind == kDw ? desc_mn : desc_k) | (uint64_t)(smem_u32(sB) >> 4);
         // 16 elements of K: 32 bytes along a row, or 16 rows of 128 bytes
         constexpr int kStepA = kKind == kDw ? 128 : 2, kStepB = kKind == kDx || kKind == kDw ? 128 : 2;
-        uint32_t it = 0, cnt = 0;
-        for (int i = blockIdx.x; i < total; i += gridDim.x, ++cnt) {
-            const Item t = item_of<kKind>(p, i);
-            const uint32_t acc = cnt & 1;
-            LOSS_WAIT(&bars.acc_empty[acc], ((cnt >> 1) & 1) ^ 1, 1, i);
-            tc_fence_after();
-            for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
-                const uint32_t s = it % kStages, ph = (it / kStages) & 1;
-                LOSS_WAIT(&bars.full[s], ph, 2, kb);
-                tc_fence_after();
-                if (lane == 0) {
-                    const uint64_t da = da0 + s * (kABytes >> 4), db = db0 + s * (kBBytes >> 4);
+        // 128 rows (of each CTA) from `sub` on, stage s, into accumulator acc
+        auto products = [&](uint32_t s, int sub, uint32_t acc, bool fresh) {
+            if (lane != 0) return;
+            const uint64_t da = da0 + s * (kA >> 4) + sub * (kABytes >> 4), db = db0 + s * (kB >> 4);
 #pragma unroll
-                    for (int kk = 0; kk < kBK / 16; ++kk)
-                        mma_ss(tmem + acc * kBN, da + kk * kStepA, db + kk * kStepB, idesc, (kb > t.kb0) || (kk > 0));
-                    tc_commit(&bars.empty[s]);
-                }
+            for (int kk = 0; kk < kBK / 16; ++kk) {
+                if constexpr (kPair)
+                    mma_ss_pair(tmem + acc * kBN, da + kk * kStepA, db + kk * kStepB, idesc, !fresh || (kk > 0));
+                else
+                    mma_ss(tmem + acc * kBN, da + kk * kStepA, db + kk * kStepB, idesc, !fresh || (kk > 0));
             }
-            if (lane == 0) tc_commit(&bars.acc_full[acc]);
+        };
+        auto commit = [&](uint64_t *bar) {
+            if (lane != 0) return;
+            if constexpr (kPair) tc_commit_pair(bar);
+            else tc_commit(bar);
+        };
+        uint32_t it = 0, cnt = 0;
+        for (int i = half == 0 ? first : total; i < total; i += step, ++cnt) {
+            const Item t = item_of<kKind>(p, i);
+            const int n = t.kb1 - t.kb0;
+            if constexpr (!kPair) {
+                const uint32_t acc = cnt & 1;
+                LOSS_WAIT(&bars.acc_empty[acc], ((cnt >> 1) & 1) ^ 1, 1, i);
+                tc_fence_after();
+                for (int u = 0; u < n; ++u, ++it) {
+                    const uint32_t s = it % kS;
+                    LOSS_WAIT(&bars.full[s], (it / kS) & 1, 2, u);
+                    tc_fence_after();
+                    products(s, 0, acc, u == 0);
+                    commit(&bars.empty[s]);
+                }
+                commit(&bars.acc_full[acc]);
+            } else {
+                const int head = min(kS, n), tail = min(kS, n - head);
+                LOSS_WAIT(&bars.acc_empty[0], (cnt & 1) ^ 1, 1, i);
+                tc_fence_after();
+                for (int u = 0; u < head; ++u) {
+                    const uint32_t s = (it + u) % kS;
+                    LOSS_WAIT(&bars.full[s], ((it + u) / kS) & 1, 2, u);
+                    tc_fence_after();
+                    products(s, 0, 0, u == 0);
+                }
+                if (tail == 0) commit(&bars.acc_full[0]);
+                LOSS_WAIT(&bars.acc_empty[1], (cnt & 1) ^ 1, 1, i);
+                tc_fence_after();
+                for (int u = 0; u < head; ++u, ++it) {
+                    products(it % kS, 1, 1, u == 0);
+                    commit(&bars.empty[it % kS]);
+                }
+                for (int u = head; u < n - tail; ++u, ++it) {
+                    const uint32_t s = it % kS;
+                    LOSS_WAIT(&bars.full[s], (it / kS) & 1, 2, u);
+                    tc_fence_after();
+                    products(s, 0, 0, false);
+                    products(s, 1, 1, false);
+                    commit(&bars.empty[s]);
+                }
+                for (int u = 0; u < tail; ++u) {
+                    const uint32_t s = (it + u) % kS;
+                    LOSS_WAIT(&bars.full[s], ((it + u) / kS) & 1, 2, u);
+                    tc_fence_after();
+                    products(s, 0, 0, false);
+                }
+                if (tail > 0) commit(&bars.acc_full[0]);
+                for (int u = 0; u < tail; ++u, ++it) {
+                    products(it % kS, 1, 1, false);
+                    commit(&bars.empty[it % kS]);
+                }
+                commit(&bars.acc_full[1]);
+            }
         }
     } else {
-        // ------------------------------------------------------------------ epilogue (warps 2..5)
+        // ------------------------------------------------------------------ epilogue (the other warps)
         const int quarter = warp & 3;                       // the TMEM lanes this warp can reach
         const int row = quarter * 32 + lane;
         const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
         uint32_t cnt = 0;
-        for (int i = blockIdx.x; i < total; i += gridDim.x, ++cnt) {
+        float scale = 1.f;
+        if constexpr (kKind == kDx || kKind == kDw) scale = __uint_as_float(*p.scale);
+        for (int i = first; i < total; i += step, ++cnt) {
             const Item t = item_of<kKind>(p, i);
-            const uint32_t acc = cnt & 1;
-            const uint32_t src = tmem + acc * kBN + lane_addr;
-            const int prow = t.m * kBM + row;
-            const int col0 = t.n * kBN;
+            const uint32_t acc = kPair ? (warp - 2) >> 2 : cnt & 1, parity = kPair ? cnt & 1 : (cnt >> 1) & 1;
+            // a pair's warp takes all columns of its accumulator, a single CTA's four warps each take half of them
+            constexpr int kCols = kPair ? kBN : kBN / 2;
+            const int side = kPair ? 0 : ((warp - 2) >> 2) * kCols;
+            const uint32_t src = tmem + acc * kBN + side + lane_addr;
+            const int prow = t.m * kTileM<kPair> + half * kRows + (kPair ? acc * kBM : 0) + row;
+            auto hand_back = [&] {                          // the accumulator is in registers
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (kPair) mbar_arrive_at(map_to_rank(&bars.acc_empty[acc], 0));
+                    else mbar_arrive(&bars.acc_empty[acc]);
+                }
+            };
+            const int col0 = t.n * kBN + side;
             if constexpr (kKind == kStats || kKind == kLogits) {
                 const Token tok = token_of(p.rows, prow);
                 const long long label = tok.valid ? p.label[tok.rank][tok.row] : -1;
                 // the target's column in this tile, or -1
-                const int hit = label >= col0 && label < p.vocab && label < col0 + kBN ? (int)(label - col0) : -1;
-                const int cols = min(kBN, p.vocab - col0);
-                LOSS_WAIT(&bars.acc_full[acc], (cnt >> 1) & 1, 3, i);
+                const int hit = label >= col0 && label < p.vocab && label < col0 + kCols ? (int)(label - col0) : -1;
+                const bool stored = prow < p.piece_rows;            // not the second half of an odd last tile
+                LOSS_WAIT(&bars.acc_full[acc], parity, 3, i);
                 tc_fence_after();
-                float m = -INFINITY;
-                for (int c = 0; c < kBN / 32; ++c) {
-                    uint32_t v[32];
-                    tmem_ld_x32(src + c * 32, v);
-                    tmem_wait_ld();
-                    const bool special = __any_sync(0xffffffffu, (hit >> 5) == c) || cols < c * 32 + 32;
-                    if (!special) {
+                uint16_t *dst = p.codes + (size_t)prow * p.pitch + col0;
+#pragma unroll 1
+                for (int g = 0; g < kCols / kStatCols; ++g) {
+                    uint32_t v[kStatCols / 32][32];
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) m = max3(m, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
-                    } else {
+                    for (int c = 0; c < kStatCols / 32; ++c) tmem_ld_x32(src + g * kStatCols + c * 32, v[c]);
+                    tmem_wait_ld();
+                    if (g == kCols / kStatCols - 1) hand_back();
+                    // columns that do not count (the target, columns past the vocabulary) become -inf
+                    const int at = hit - g * kStatCols, cols = p.vocab - col0 - g * kStatCols;
+                    if (__any_sync(0xffffffffu, (at >= 0 && at < kStatCols) || cols < kStatCols)) {
+#pragma unroll
+                        for (int c = 0; c < kStatCols / 32; ++c)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (c * 32 + e == at || c * 32 + e >= cols) v[c][e] = 0xff800000u;
+                    }
+                    float m = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < kStatCols / 32; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) m = max3(m, __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
+                    // nothing but the target: distances are infinite.  The rounding of top (2^-24 of some 20) shifts all
+                    // terms alike, by 1e-6 of the sum
+                    const float top = (m == -INFINITY ? 0.f : m) * -kLog2e;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < kStatCols / 32; ++c) {
+                        uint32_t out[16];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
-                            const float z = __uint_as_float(v[e]);
-                            if (c * 32 + e == hit) p.target[prow] = z;
-                            else if (c * 32 + e < cols) m = fmaxf(m, z);
+                            const float d = fmaf(__uint_as_float(v[c][e]), kLog2e, top);    // log2 of the term, <= 0
+                            sum[e & 3] += exp2_approx(d);
+                            if constexpr (kKind == kLogits) {
+                                // + 2^23: the nearest whole number in the low bits
+                                const uint32_t code = __float_as_uint(fminf(fmaf(d, -kCodeStep, 8388608.f), 8388608.f + kCodeMax));
+                                if (e & 1) out[e / 2] = __byte_perm(out[e / 2], code, 0x5410);
+                                else out[e / 2] = code;
+                            }
                         }
-                    }
-                }
-                const float top = m == -INFINITY ? 0.f : m;         // nothing but the target: distances are infinite
-                float sum = 0.f;
-                uint16_t *dst = p.codes + (size_t)prow * p.pitch + col0;
-                for (int c = 0; c < kBN / 32; ++c) {
-                    uint32_t v[32];
-                    tmem_ld_x32(src + c * 32, v);
-                    tmem_wait_ld();
-                    if (c == kBN / 32 - 1) {                        // the accumulator is in registers: hand it back
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&bars.acc_empty[acc]);
-                    }
-                    const bool special = __any_sync(0xffffffffu, (hit >> 5) == c) || cols < c * 32 + 32;
-                    uint32_t out[16];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float d = (top - __uint_as_float(v[e])) * kLog2e;
-                        if (special && (c * 32 + e == hit || c * 32 + e >= cols)) d = INFINITY;
-                        sum += exp2_approx(-d);
                         if constexpr (kKind == kLogits) {
-                            // + 2^23: the nearest whole number in the low bits
-                            const uint32_t code = __float_as_uint(fminf(d * kCodeStep, kCodeMax) + 8388608.f);
-                            if (e & 1) out[e / 2] = __byte_perm(out[e / 2], code, 0x5410);
-                            else out[e / 2] = code;
+                            if (stored) {
+#pragma unroll
+                                for (int q = 0; q < 4; ++q)
+                                    *reinterpret_cast<uint4 *>(dst + g * kStatCols + c * 32 + 8 * q) =
+                                        make_uint4(out[4 * q], out[4 * q + 1], out[4 * q + 2], out[4 * q + 3]);
+                            }
                         }
                     }
-                    if constexpr (kKind == kLogits) {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            *reinterpret_cast<uint4 *>(dst + c * 32 + 8 * q) = make_uint4(out[4 * q], out[4 * q + 1], out[4 * q + 2], out[4 * q + 3]);
-                    }
+                    if (stored)
+                        p.stats[(size_t)(col0 / kStatCols + g) * p.piece_rows + prow] =
+                            make_float2(m, (sum[0] + sum[1]) + (sum[2] + sum[3]));
                 }
-                p.stats[(size_t)t.n * p.piece_rows + prow] = make_float2(m, sum);
             } else {
-                const int width = min(kBN, p.hidden - col0);        // a multiple of 8
+                const int width = min(kCols, p.hidden - col0);      // a multiple of 8
                 Token tok{0, prow, prow < p.vocab};
                 if constexpr (kKind == kDx) tok = token_of(p.rows, prow);
-                LOSS_WAIT(&bars.acc_full[acc], (cnt >> 1) & 1, 3, i);
+                LOSS_WAIT(&bars.acc_full[acc], parity, 3, i);
                 tc_fence_after();
-                for (int c = 0; c < kBN / 32; ++c) {
+                for (int c = 0; c < kCols / 32; ++c) {
                     uint32_t raw[32];
                     tmem_ld_x32(src + c * 32, raw);
                     tmem_wait_ld();
-                    if (c == kBN / 32 - 1) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&bars.acc_empty[acc]);
-                    }
+                    if (c == kCols / 32 - 1) hand_back();
                     const int cols = min(32, width - c * 32);
                     if (!tok.valid || cols <= 0) continue;
                     float v[32];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(raw[e]);
+                    for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(raw[e]) * scale;
                     if constexpr (kKind == kDx) {
                         if (p.splits == 1) {
-                            store_bf16x32(p.dx[tok.rank] + (size_t)tok.row * p.hidden + col0 + c * 32, v, cols);
+                            store_bf16x32(p.dx[tok.rank] + (size_t)tok.row * p.hidden + col0 + c * 32, v, cols, p.wide);
                         } else {
                             float *dst = p.partial + ((size_t)t.split * p.piece_rows + prow) * p.hidden + col0 + c * 32;
 #pragma unroll
@@ -356,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                             for (int q = 0; q < 8; ++q)
                                 if (4 * q < cols) *reinterpret_cast<float4 *>(p.acc_out + at + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
                         } else {
-                            store_bf16x32(p.dw + at, v, cols);
+                            store_bf16x32(p.dw + at, v, cols, p.wide);
                         }
                     }
                 }
@@ -372,14 +473,18 @@ gemm_done:
         while (globaltimer_ns() - t0 < 200000ull) { }
         __syncthreads();
     }
-    if (warp == 1) tmem_dealloc(tmem, 512);
+    if constexpr (kPair) cluster_sync();                   // the other CTA may still signal this one's barriers
+    if (warp == 1) {
+        if constexpr (kPair) tmem_dealloc_pair(tmem, 512);
+        else tmem_dealloc(tmem, 512);
+    }
 }
 
 #undef LOSS_WAIT
 
 // ------------------------------------------------------------------------------------------------ statistics of the rows
 struct RowInfo {               // what the element-wise pass needs of a row
-    float lse, weight, target_dz;
+    float lse, weight, target_dz;                  // target_dz: without the weight
     int label;                 // -1: none
 };
 
@@ -387,11 +492,12 @@ template <int R>
 struct MergeParams {
     const long long *label[R];
     const float *weight[R];    // a NULL table entry: weight 1
+    const __nv_bfloat16 *x[R], *w;
     float *loss[R], *lse[R];
     Rows rows;
-    int tiles_n, piece_rows, vocab;
+    int groups, piece_rows, vocab, hidden;
     const float2 *stats;
-    const float *target;
+    unsigned *scale;
     RowInfo *info;             // NULL: not wanted
 };
 
@@ -401,54 +507,95 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
     m = top;
 }
 
-// A block takes 32 rows; its 32 warps share the tiles of a row (neighbouring lanes read neighbouring rows).
+// A block takes 32 rows.  Its 32 warps share the column groups (neighbouring lanes read neighbouring rows), then each takes one
+// row: the target's logit, the join of the warps' sums, the loss.
 template <int R>
 __global__ void __launch_bounds__(1024) lm_merge_kernel(const __grid_constant__ MergeParams<R> p) {
     __shared__ float2 part[32][33];
+    __shared__ unsigned scale;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int i = blockIdx.x * 32 + lane;
-    float m = -INFINITY, s = 0.f;
-    constexpr int kBatch = 8;                      // loads in flight
-    for (int n0 = warp; n0 < p.tiles_n; n0 += 32 * kBatch) {
-        float2 v[kBatch];
+    if (threadIdx.x == 0) scale = 0;
+    const int row = blockIdx.x * 32 + warp;
+    const Token tok = token_of(p.rows, row);
+    const long long label = tok.valid ? p.label[tok.rank][tok.row] : -1;
+    const bool counts = label >= 0 && label < p.vocab;
+    {
+        const int i = blockIdx.x * 32 + lane;
+        float m = -INFINITY, s = 0.f;
+        constexpr int kBatch = 8;                  // loads in flight
+        for (int n0 = warp; n0 < p.groups; n0 += 32 * kBatch) {
+            float2 v[kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const int n = n0 + 32 * u;
-            v[u] = n < p.tiles_n ? p.stats[(size_t)n * p.piece_rows + i] : make_float2(-INFINITY, 0.f);
+            for (int u = 0; u < kBatch; ++u) {
+                const int n = n0 + 32 * u;
+                v[u] = n < p.groups ? p.stats[(size_t)n * p.piece_rows + i] : make_float2(-INFINITY, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) join(m, s, v[u].x, v[u].y);
         }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) join(m, s, v[u].x, v[u].y);
+        part[warp][lane] = make_float2(m, s);
     }
-    part[warp][lane] = make_float2(m, s);
-    __syncthreads();
-    if (warp != 0) return;
-    for (int w = 1; w < 32; ++w) join(m, s, part[w][lane].x, part[w][lane].y);
-    const Token tok = token_of(p.rows, i);
-    RowInfo info{0.f, 0.f, 0.f, -1};
-    if (tok.valid) {
-        const float others = m + logf(s);          // -inf where the target is the only word
-        const long long label = p.label[tok.rank][tok.row];
-        float loss = 0.f, lse = others;
-        if (label >= 0 && label < p.vocab) {
-            const float z = p.target[i], away = others - z, tail = log1pf(expf(-fabsf(away)));
-            loss = (away > 0.f ? away : 0.f) + tail;
-            lse = (away > 0.f ? others : z) + tail;
-            if (p.info) {
-                const float g = p.weight[tok.rank] ? p.weight[tok.rank][tok.row] : 1.f;
-                info.weight = g;
-                info.target_dz = -g / (1.f + expf(-away));
-                info.label = (int)label;
+    // the target's logit in fp32 operations rounded to nearest: the tensor cores' sum of a large logit (they cut off what does
+    // not fit) would be the largest error of the loss
+    float z = 0.f;
+    if (counts) {
+        const uint4 *x = reinterpret_cast<const uint4 *>(p.x[tok.rank] + (size_t)tok.row * p.hidden);
+        const uint4 *w = reinterpret_cast<const uint4 *>(p.w + (size_t)label * p.hidden);
+        float a[8] = {};
+#pragma unroll 8
+        for (int c = lane; c < p.hidden / 8; c += 32) {
+            const uint4 u = __ldg(x + c), v = __ldg(w + c);
+            const uint32_t us[4] = {u.x, u.y, u.z, u.w}, vs[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                a[2 * q] = fmaf(__uint_as_float(us[q] << 16), __uint_as_float(vs[q] << 16), a[2 * q]);
+                a[2 * q + 1] = fmaf(__uint_as_float(us[q] & 0xffff0000u), __uint_as_float(vs[q] & 0xffff0000u), a[2 * q + 1]);
             }
         }
-        info.lse = lse;
-        p.loss[tok.rank][tok.row] = loss;
-        if (p.lse[tok.rank]) p.lse[tok.rank][tok.row] = lse;
+        z = ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
     }
-    if (p.info) p.info[i] = info;
+    __syncthreads();
+    const float2 mine = part[lane][warp];
+    float m = mine.x, s = 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        z += __shfl_xor_sync(0xffffffffu, z, o);
+    }
+    s = mine.y * exp2f((mine.x - (m == -INFINITY ? 0.f : m)) * kLog2e);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) {
+        RowInfo info{0.f, 0.f, 0.f, -1};
+        if (tok.valid) {
+            const float others = m + logf(s);      // -inf where the target is the only word
+            float loss = 0.f, lse = others;
+            if (counts) {
+                const float away = others - z, tail = log1pf(expf(-fabsf(away)));
+                loss = (away > 0.f ? away : 0.f) + tail;
+                lse = (away > 0.f ? others : z) + tail;
+                if (p.info) {
+                    info.weight = p.weight[tok.rank] ? p.weight[tok.rank][tok.row] : 1.f;
+                    info.target_dz = -1.f / (1.f + expf(-away));
+                    info.label = (int)label;
+                }
+            }
+            info.lse = lse;
+            p.loss[tok.rank][tok.row] = loss;
+            if (p.lse[tok.rank]) p.lse[tok.rank][tok.row] = lse;
+        }
+        if (p.info) {
+            p.info[row] = info;
+            atomicMax(&scale, __float_as_uint(fabsf(info.weight)));
+        }
+    }
+    if (!p.info) return;
+    __syncthreads();
+    if (threadIdx.x == 0) atomicMax(p.scale, scale);
 }
 
 // ------------------------------------------------------------------------------------------------ 16-bit distances -> bf16 dz
-// In place.  A warp takes 256-column tiles of one row (the tile's maximum is one value for the warp), a lane 8 columns.  A row
+// In place.  A warp takes 256 columns of one row at a time (two column groups), a lane 8 columns.  A row
 // without weight is written as zeros and not read: nothing of it, NaN neither, reaches the gradients.  The row's last block
 // copies x.
 constexpr int kDzTiles = 4;    // tiles per warp
@@ -461,6 +608,7 @@ struct DzParams {
     size_t pitch;
     const RowInfo *info;
     const float2 *stats;
+    const unsigned *scale;
     int tiles_n, piece_rows, hidden, blocks;       // blocks: of a row's logits
 };
 template <int R>
@@ -477,6 +625,7 @@ __global__ void __launch_bounds__(256) lm_dz_kernel(const __grid_constant__ DzPa
         return;
     }
     const int tiles_n = p.tiles_n, piece_rows = p.piece_rows;
+    const float weight = __fdiv_rn(info.weight, __uint_as_float(*p.scale));     // exactly 1 where all are equal
     const int n0 = (blockIdx.x * 8 + warp) * kDzTiles;
     uint4 v[kDzTiles];
     float m[kDzTiles];
@@ -486,7 +635,7 @@ __global__ void __launch_bounds__(256) lm_dz_kernel(const __grid_constant__ DzPa
         for (int u = 0; u < kDzTiles; ++u)
             if (n0 + u < tiles_n) {
                 v[u] = at[u * 32];
-                m[u] = __ldg(&p.stats[(size_t)(n0 + u) * piece_rows + row].x);
+                m[u] = __ldg(&p.stats[(size_t)((n0 + u) * (kBN / kStatCols) + lane / (kStatCols / 8)) * piece_rows + row].x);
             }
     }
 #pragma unroll
@@ -505,7 +654,7 @@ __global__ void __launch_bounds__(256) lm_dz_kernel(const __grid_constant__ DzPa
                 for (int e = 0; e < 2; ++e) {
                     const uint32_t code = e ? w[q] >> 16 : w[q] & 0xffffu;
                     const float dist = code == 65535u ? INFINITY : (float)code * (1.f / kCodeStep);
-                    d[e] = 2 * q + e == target ? info.target_dz : exp2_approx(c - dist) * info.weight;
+                    d[e] = (2 * q + e == target ? info.target_dz : exp2_approx(c - dist)) * weight;
                 }
                 r[q] = pack_bf16x2(d[0], d[1]);
             }
@@ -555,16 +704,24 @@ struct Sizes {
     size_t pitch;
 };
 
+// Per 128 x 256 x 64 products a single CTA's tile fetches 48 KiB from L2, a pair's 24 KiB; under the power limit that is time.  A
+// pair's tile wants its 512 rows.
+bool use_pair(int rows) { return rows > 2 * kBM; }
+
 // How often the vocabulary is split in dx = dz W: the time of `waves` rounds of tiles over the SMs, a tile costing its K
 // blocks plus a start and an epilogue (8 blocks), plus writing and reading the partial sums.
 int dx_splits(int tiles_m, int tiles_h, int k_blocks, int hidden) {
     const double block_us = 0.43;                  // 128 x 256 x 64 at the sustained rate of one SM
+    const bool pair = use_pair(tiles_m * kBM);
     int best = 1;
     double best_us = 1e30;
     for (int s = 1; s <= 64 && (s == 1 || k_blocks / s >= 8); ++s) {
         const double bytes = (double)s * tiles_m * kBM * hidden * 4;
-        if (s > 1 && bytes > 256e6) break;
-        const double us = (double)cdiv((long long)tiles_m * tiles_h * s, kSms) * (cdiv(k_blocks, s) + 8) * block_us +
+        if (s > 1 && bytes > 768e6) break;
+        // rounds of items over SMs or pairs; a pair's block is four times the work of two SMs
+        const double us = (double)(pair ? cdiv((long long)cdiv(tiles_m, 4) * tiles_h * s, kSms / 2)
+                                        : cdiv((long long)tiles_m * tiles_h * s, kSms)) *
+                              (cdiv(k_blocks, s) + 8) * (pair ? 2 * block_us : block_us) +
                           (s > 1 ? 4.0 + 2 * bytes / 6.0e6 : 0.0);
         if (us < best_us) { best_us = us; best = s; }
     }
@@ -592,16 +749,16 @@ int sizes_of(const basp_plan *p, int hidden, int vocab, int piece_rows, Sizes *z
 }
 
 struct Workspace {
-    size_t stats, target, codes, info, kept, partial, acc, bytes;
+    size_t stats, scale, codes, info, kept, partial, acc, bytes;
 };
 Workspace workspace_of(const Sizes &z, int hidden, int vocab, bool grad) {
     Workspace w{};
     const size_t rows = (size_t)z.piece_tiles * kBM;
     size_t at = 0;
     auto take = [&](size_t n) { const size_t o = at; at += up256(n); return o; };
-    w.stats = take(rows * z.tiles_v * sizeof(float2));
-    w.target = take(rows * sizeof(float));
+    w.stats = take(rows * z.tiles_v * (kBN / kStatCols) * sizeof(float2));
     if (grad) {
+        w.scale = take(sizeof(unsigned));
         w.codes = take(rows * z.pitch * 2);
         w.info = take(rows * sizeof(RowInfo));
         w.kept = take(rows * hidden * 2);
@@ -618,18 +775,44 @@ Workspace workspace_of(const Sizes &z, int hidden, int vocab, bool grad) {
     return w;
 }
 
-template <int kKind, int R>
-int launch_gemm(const LossParams<R> &prm, cudaStream_t st) {
+// 8192 rows of 4096: 6.83 / 6.31 / 6.14 / 5.98 / 6.26 ms with 1 / 2 / 4 / 8 / 16 row tiles (4 MiB each) in a group
+constexpr long long kGroupBytes = 34 << 20;
+constexpr int kPairBlocks = 8;
+
+template <int kKind, int R, bool kPair>
+int launch_as(const LossParams<R> &prm, cudaStream_t st) {
     int dev = 0, sms = 0;
     BASP_CUDA_TRY(cudaGetDevice(&dev));
     BASP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    const long long items = (long long)prm.tiles_m * prm.tiles_n * prm.splits;
-    const int smem = kStages * (kABytes + kBBytes) + 1024;
-    BASP_CUDA_TRY(cudaFuncSetAttribute(lm_gemm_kernel<kKind, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    lm_gemm_kernel<kKind, R><<<(int)(items < sms ? items : sms), kThreads, smem, st>>>(prm);
-    BASP_CUDA_TRY(cudaGetLastError());
+    const long long items = (long long)prm.tiles_m * prm.tiles_n * prm.splits, slots = kPair ? sms / 2 : sms;
+    const int smem = kStages * kStageBytes + 1024;
+    BASP_CUDA_TRY(cudaFuncSetAttribute(lm_gemm_kernel<kKind, R, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(items < slots ? items : slots) * (kPair ? 2 : 1));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = kPair ? 2 : 1; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    BASP_CUDA_TRY(cudaLaunchKernelEx(&cfg, lm_gemm_kernel<kKind, R, kPair>, prm));
     basp_count_launch(1);
     return BASP_OK;
+}
+
+// `rows`: of the product's first operand
+template <int kKind, int R>
+int launch_gemm(LossParams<R> &prm, int rows, cudaStream_t st) {
+    // dW of few rows is all epilogue, and only single CTAs' tiles run one under the next tile's loads
+    const bool pair = use_pair(rows) && !(kKind == kDw && prm.k_blocks < kPairBlocks);
+    prm.tiles_m = cdiv(rows, pair ? kTileM<true> : kTileM<false>);
+    // (1): as many row tiles as leave their x in L2 while W streams by; (2), (3): one, its dz streams once
+    const long long tile_bytes = (long long)(pair ? kTileM<true> : kTileM<false>) * prm.hidden * 2;
+    prm.group = kKind == kStats || kKind == kLogits ? (int)(kGroupBytes / tile_bytes) : 1;
+    prm.group = prm.group < 1 ? 1 : (prm.group > prm.tiles_m ? prm.tiles_m : prm.group);
+    return pair ? launch_as<kKind, R, true>(prm, st) : launch_as<kKind, R, false>(prm, st);
 }
 
 struct Args {
@@ -656,36 +839,39 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
     if (!prm.status) return BASP_ERR_CUDA;
     prm.rows.slot_log2 = z.slot_log2; prm.rows.per_rank = z.per_rank; prm.rows.K = p->K; prm.rows.M = M; prm.rows.M_last = M_last;
     prm.vocab = a.vocab; prm.hidden = a.hidden; prm.pitch = z.pitch; prm.piece_rows = rows;
-    prm.stats = (float2 *)(a.ws + w.stats); prm.target = (float *)(a.ws + w.target);
+    prm.stats = (float2 *)(a.ws + w.stats); prm.scale = (unsigned *)(a.ws + w.scale);
     prm.codes = (uint16_t *)(a.ws + w.codes); prm.partial = (float *)(a.ws + w.partial);
     prm.dw = (__nv_bfloat16 *)a.dw;
     for (int r = 0; r < p->N; ++r) {
         prm.label[r] = a.labels[r];
         prm.dx[r] = a.dx ? (__nv_bfloat16 *)a.dx[r] : nullptr;
         merge.label[r] = a.labels[r];
+        merge.x[r] = (const __nv_bfloat16 *)a.x[r];
         merge.weight[r] = a.weights ? a.weights[r] : nullptr;
         merge.loss[r] = a.loss[r];
         merge.lse[r] = a.lse ? a.lse[r] : nullptr;
     }
-    merge.tiles_n = z.tiles_v; merge.piece_rows = rows; merge.vocab = a.vocab;
-    merge.stats = prm.stats; merge.target = prm.target;
+    merge.groups = z.tiles_v * (kBN / kStatCols); merge.piece_rows = rows; merge.vocab = a.vocab;
+    merge.stats = prm.stats; merge.scale = prm.scale; merge.hidden = a.hidden; merge.w = (const __nv_bfloat16 *)a.w;
     merge.info = grad ? (RowInfo *)(a.ws + w.info) : nullptr;
-    CUtensorMap w_k, w_mn, dz_k, dz_mn;
+    CUtensorMap w_k[2], w_mn, dz_k, dz_mn;     // w_k: of a single CTA, of a pair's
     for (int r = 0; r < p->N; ++r) {
         const uint64_t n = (uint64_t)p->Bl * basp_rank_tokens(p, r % p->K);
         BASP_TRY(tmap::encode_rows_heads_d(&prm.x[r], a.x[r], n, 1, a.hidden, slot));
     }
-    BASP_TRY(tmap::encode_rows_heads_d(&w_k, a.w, a.vocab, 1, a.hidden, kBN));
+    for (int pair = 0; pair < 2; ++pair) BASP_TRY(tmap::encode_rows_heads_d(&w_k[pair], a.w, a.vocab, 1, a.hidden, kBN >> pair));
     if (grad) {
         BASP_TRY(tmap::encode_rows_heads_d(&w_mn, a.w, a.vocab, 1, a.hidden, kBK));
         BASP_TRY(tmap::encode_rows_heads_d(&dz_k, prm.codes, rows, 1, z.pitch, kBM));
         BASP_TRY(tmap::encode_rows_heads_d(&dz_mn, prm.codes, rows, 1, z.pitch, kBK));
         BASP_TRY(tmap::encode_rows_heads_d(&prm.kept, a.ws + w.kept, rows, 1, a.hidden, kBK));
     }
+    bool wide_dx = a.hidden % 16 == 0;
+    for (int r = 0; a.dx && r < p->N; ++r) wide_dx = wide_dx && (uintptr_t)a.dx[r] % 32 == 0;
     DzParams<R> dz;
     memset(&dz, 0, sizeof(dz));
     for (int r = 0; r < p->N; ++r) dz.x[r] = (const __nv_bfloat16 *)a.x[r];
-    dz.kept = (__nv_bfloat16 *)(a.ws + w.kept); dz.codes = prm.codes; dz.pitch = z.pitch; dz.info = merge.info; dz.stats = prm.stats;
+    dz.kept = (__nv_bfloat16 *)(a.ws + w.kept); dz.codes = prm.codes; dz.pitch = z.pitch; dz.info = merge.info; dz.stats = prm.stats; dz.scale = prm.scale;
     dz.tiles_n = z.tiles_v; dz.piece_rows = rows; dz.hidden = a.hidden; dz.blocks = cdiv(z.tiles_v, 8 * kDzTiles);
     for (int piece = 0; piece < z.pieces; ++piece) {
         const int tile0 = piece * z.piece_tiles, tiles = tile0 + z.piece_tiles < z.tiles_m ? z.piece_tiles : z.tiles_m - tile0;
@@ -694,10 +880,10 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
         prm.rows.slots = z.slots - prm.rows.slot_begin < tiles * per_tile ? z.slots - prm.rows.slot_begin : tiles * per_tile;
         merge.rows = prm.rows;
         // (1)
-        prm.w = w_k;
-        prm.tiles_m = tiles; prm.tiles_n = z.tiles_v; prm.splits = 1; prm.k_blocks = cdiv(a.hidden, kBK);
-        if (grad) BASP_TRY((launch_gemm<kLogits, R>(prm, st)));
-        else BASP_TRY((launch_gemm<kStats, R>(prm, st)));
+        prm.tiles_n = z.tiles_v; prm.splits = 1; prm.k_blocks = cdiv(a.hidden, kBK);
+        prm.w = w_k[use_pair(tiles * kBM)];
+        if (grad) BASP_TRY((launch_gemm<kLogits, R>(prm, tiles * kBM, st)));
+        else BASP_TRY((launch_gemm<kStats, R>(prm, tiles * kBM, st)));
         lm_merge_kernel<R><<<tiles * kBM / 32, 1024, 0, st>>>(merge);
         BASP_CUDA_TRY(cudaGetLastError());
         basp_count_launch(1);
@@ -710,9 +896,9 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
         if (a.dx) {
             prm.w = w_mn;
             prm.dz = dz_k;
-            prm.tiles_n = z.tiles_h; prm.k_blocks = cdiv(a.vocab, kBK);
+            prm.tiles_n = z.tiles_h; prm.k_blocks = cdiv(a.vocab, kBK); prm.wide = wide_dx;
             prm.splits = dx_splits(tiles, z.tiles_h, prm.k_blocks, a.hidden);
-            BASP_TRY((launch_gemm<kDx, R>(prm, st)));
+            BASP_TRY((launch_gemm<kDx, R>(prm, tiles * kBM, st)));
             if (prm.splits > 1) {
                 JoinParams<R> join;
                 memcpy(join.dx, prm.dx, sizeof(join.dx));
@@ -725,11 +911,11 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
         // (3)
         if (a.dw) {
             prm.dz = dz_mn;
-            prm.tiles_m = cdiv(a.vocab, kBM); prm.tiles_n = z.tiles_h; prm.splits = 1;
+            prm.tiles_n = z.tiles_h; prm.splits = 1; prm.wide = a.hidden % 16 == 0 && (uintptr_t)a.dw % 32 == 0;
             prm.k_blocks = cdiv((long long)prm.rows.slots << z.slot_log2, kBK);
             prm.acc_in = piece > 0 ? (const float *)(a.ws + w.acc) : nullptr;
             prm.acc_out = piece + 1 < z.pieces ? (float *)(a.ws + w.acc) : nullptr;
-            BASP_TRY((launch_gemm<kDw, R>(prm, st)));
+            BASP_TRY((launch_gemm<kDw, R>(prm, a.vocab, st)));
         }
     }
     return BASP_OK;
