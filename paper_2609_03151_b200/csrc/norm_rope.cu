@@ -4,26 +4,38 @@
 //   r = (mean x^2 + eps)^(-1/2),   z = r x w,   y = R(pos) z        (rotate-half: feature j < D/2 pairs with j + D/2)
 //   backward:  u = R(pos)^T dy,   dw += r x u  (over all tokens and heads),   dx = r w u - x r^3 (x . w u) / D
 //
-// HBM-bound: 2 bytes read and 2 written per element forward, 4 read and 2 written backward, a few operations each.  A
-// vector is held by D/16 neighbouring lanes, lane i with features 8i..8i+7 and the partners D/2 + 8i .. of the rotation,
-// so that both halves of every pair are in one thread, every load and store is 16 bytes, and the sums of a vector cross
-// at most three shuffles.  Where D/16 is no power of two the group of lanes is the next one and its last lanes idle.  A
-// group owns one token and walks over heads: the token's cos and sin are fetched once for all of them.
+// HBM-bound: 2 bytes read and 2 written per element forward, 4 read and 2 written backward.  All loads and stores are 16 bytes
+// (eight features); the arithmetic is fp32 on packed pairs.  A token's cos and sin are fetched once for the heads of a work item.
+// What the kernels wait for is memory latency, so they are laid out by the bytes in flight per SM that the registers allow:
+//   forward   a lane holds eight features, D/8 lanes a vector, a warp 32 / (D/8) neighbouring heads of one token (of 512 bytes at
+//             D = 128); the rotation's partner comes by shuffle.  80 registers, three blocks of 256 threads per SM.
+//             2 x 8K tokens, 64 heads of 128: 93 us (5.8 TB/s); with the backward's layout 104 us.
+//   backward  a lane holds eight features and their eight partners, so D/16 lanes (rounded up to a power of two) a vector, no
+//             shuffle but the sums; the groups of lanes hold neighbouring tokens.  126 registers, two blocks per SM.
+//             128K tokens, 40 heads of 128: 700 us (5.8 TB/s); with the forward's layout 727 us.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
+#include "ptx.cuh"
 #include "spans.h"
 
 namespace {
 
-constexpr int kThreads = 256;
+using namespace ptx;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kFwdBlocks = 3, kBwdBlocks = 2;      // per SM
+constexpr int kFwdUnroll = 4, kBwdUnroll = 2;      // vectors in flight per lane: 64 and 128 bytes
 
 struct HeadSet {               // one of the two tensors (Q or K) of all ranks
     const __nv_bfloat16 *x[BASP_MAX_RANKS];
     const __nv_bfloat16 *dy[BASP_MAX_RANKS];      // backward only
     __nv_bfloat16 *out[BASP_MAX_RANKS];           // y, or dx
     const __nv_bfloat16 *w;
-    int heads, chunks;         // heads per token; head chunks per token tile
+    uint32_t heads, chunks;    // heads per token, chunks of heads
+    uint32_t items;            // token tiles of all ranks x chunks
 };
 
 struct NormRopeParams {
@@ -31,12 +43,9 @@ struct NormRopeParams {
     const float *cos, *sin;    // [D/2][S]
     float *partial;            // backward: [blocks][D] sums of dw
     float eps, inv_D;
-    int D, S, T, T_last, K, Bl, N;
-    int chunk_heads;           // heads per chunk
-    int tiles;                 // token tiles per rank
-    int q_items, items;        // work items of the first tensor, and of both
-    int q_blocks;              // backward: blocks that work on the first tensor (the others on the second)
-    FastDiv div_T, div_T_last;
+    int D, S, T, T_last, K, Bl;
+    uint32_t tiles, tile_tokens, chunk_heads;      // token tiles per rank and their tokens; heads per work item
+    int q_blocks;              // blocks that work on the first tensor (the others on the second)
 };
 
 __device__ __forceinline__ uint4 ld16(const __nv_bfloat16 *p) {
@@ -47,184 +56,217 @@ __device__ __forceinline__ uint4 ld16(const __nv_bfloat16 *p) {
 __device__ __forceinline__ void st16(__nv_bfloat16 *p, const uint4 &v) {
     asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" :: "l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ void widen(const uint4 &v, float (&f)[8]) {
+// Eight features as four packed pairs of fp32 (one instruction of the fp32 pipe works on a pair).
+struct F8 { uint64_t p[4]; };
+__device__ __forceinline__ F8 widen(const uint4 &v) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    F8 f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    for (int i = 0; i < 4; ++i) f.p[i] = pack_f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    return f;
 }
-__device__ __forceinline__ uint4 narrow(const float (&f)[8]) {
+__device__ __forceinline__ uint4 narrow(const F8 &f) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        float lo, hi;
+        unpack_f2(f.p[i], lo, hi);
+        w[i] = pack_bf16x2(lo, hi);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-template <int L>
-__device__ __forceinline__ float group_sum(float v) {
+__device__ __forceinline__ float sum2(uint64_t v) {
+    float lo, hi;
+    unpack_f2(v, lo, hi);
+    return lo + hi;
+}
+// Sum over the N lanes that hold a vector; `lane`: this one's place among them.  N up to 16, not only powers of two.
+template <int N>
+__device__ __forceinline__ float group_sum(float v, int lane) {
+    if constexpr ((N & (N - 1)) == 0) {
 #pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o, L);
-    return v;
+        for (int o = N / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    } else {
+#pragma unroll
+        for (int o = N > 8 ? 8 : 4; o > 0; o >>= 1) {
+            const float far = __shfl_down_sync(0xffffffffu, v, o);
+            if (lane + o < N) v += far;
+        }
+        return __shfl_sync(0xffffffffu, v, (threadIdx.x & 31) - lane);
+    }
 }
 
-// The token tile and head chunk of a work item, and this thread's share of it.
-struct Place {
-    int rank, row, head_begin, head_end;
-    bool active;               // this lane has features of a token of the tile
+// A work item: up to chunk_heads heads of a tile of neighbouring tokens of one rank.  The blocks of a tensor take its items in turn,
+// so that at any time they read and write neighbouring memory.
+struct Share {
+    int which;
+    uint32_t item, end, step;
 };
-
-template <int L>
-__device__ __forceinline__ Place place_of(const NormRopeParams &p, const HeadSet &t, int item, int group, int lane, int &pos) {
-    constexpr int kTokens = kThreads / L;
-    Place o;
-    const int chunk = item % t.chunks, tile = item / t.chunks;
-    o.rank = tile / p.tiles;
-    const int l = o.rank % p.K;
-    const bool last = l == p.K - 1;
-    const int Tr = last ? p.T_last : p.T;
-    o.row = (tile - o.rank * p.tiles) * kTokens + group;
-    o.active = o.row < p.Bl * Tr && lane * 16 < p.D;
-    const int bl = (int)fdiv((uint32_t)o.row, last ? p.div_T_last : p.div_T);
-    pos = l * p.T + (o.row - bl * Tr);
-    o.head_begin = chunk * p.chunk_heads;
-    o.head_end = min(t.heads, o.head_begin + p.chunk_heads);
+__device__ __forceinline__ Share share_of(const NormRopeParams &p) {
+    Share o;
+    o.which = (int)blockIdx.x >= p.q_blocks;
+    o.item = o.which ? blockIdx.x - p.q_blocks : blockIdx.x;
+    o.step = o.which ? gridDim.x - p.q_blocks : p.q_blocks;
+    o.end = p.t[o.which].items;
     return o;
 }
 
-// cos and sin of this thread's eight features at position pos (feature-major tables: the tile's tokens are neighbours).
-__device__ __forceinline__ void load_angles(const NormRopeParams &p, int lane, int pos, float (&c)[8], float (&s)[8]) {
+// The heads of an item and the tile's token number `token`.
+struct Place {
+    uint32_t rank;
+    int count, pos;
+    size_t off;                // the token's first element of the first of the heads in the rank's shard
+    bool valid;                // the rank has such a token
+};
+__device__ __forceinline__ Place place_of(const NormRopeParams &p, const HeadSet &t, uint32_t item, uint32_t token) {
+    Place o;
+    const uint32_t tile = item / t.chunks, head = (item - tile * t.chunks) * p.chunk_heads;
+    o.count = (int)min(p.chunk_heads, t.heads - head);
+    o.rank = tile / p.tiles;
+    const uint32_t row = (tile - o.rank * p.tiles) * p.tile_tokens + token, l = o.rank % p.K;
+    const uint32_t Tr = (int)l == p.K - 1 ? p.T_last : p.T;
+    o.pos = (int)(l * p.T + row % Tr);
+    o.off = ((size_t)row * t.heads + head) * p.D;
+    o.valid = row < p.Bl * Tr;
+    return o;
+}
+
+// Eight features of a feature-major table at position pos.  The row pitch is kept from the optimiser: it would compute the eight
+// offsets once for all items and spill them.
+__device__ __forceinline__ F8 load_feature_major(const float *table, int S, int lane, int pos) {
+    size_t pitch = (size_t)S;
+    asm volatile("" : "+l"(pitch));
+    const float *at = table + (size_t)(8 * lane) * pitch + pos;
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const size_t at = (size_t)(8 * lane + e) * p.S + pos;
-        c[e] = __ldg(p.cos + at);
-        s[e] = __ldg(p.sin + at);
+    for (int e = 0; e < 8; ++e) v[e] = __ldg(at + e * pitch);
+    F8 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.p[i] = pack_f2(v[2 * i], v[2 * i + 1]);
+    return f;
+}
+
+// What a lane needs of another one: the eight features that the rotation pairs with its own, D/2 away.
+__device__ __forceinline__ uint4 partner(const uint4 &v, int src) {
+    return make_uint4(__shfl_sync(0xffffffffu, v.x, src), __shfl_sync(0xffffffffu, v.y, src), __shfl_sync(0xffffffffu, v.z, src),
+                      __shfl_sync(0xffffffffu, v.w, src));
+}
+
+// N = D / 8 lanes hold a vector, a warp 32 / N neighbouring heads of its token.
+template <int N>
+__global__ void __launch_bounds__(kThreads, kFwdBlocks) norm_rope_kernel(const __grid_constant__ NormRopeParams p) {
+    constexpr int kUnroll = kFwdUnroll, kVectors = 32 / N;
+    const int warp_lane = threadIdx.x & 31, vec = warp_lane / N, lane = warp_lane - vec * N;
+    const bool low = lane < N / 2, mine = vec < kVectors;
+    const int other = low ? lane + N / 2 : lane - N / 2, src = vec * N + other;
+    const Share share = share_of(p);
+    const HeadSet &t = p.t[share.which];
+    for (uint32_t item = share.item; item < share.end; item += share.step) {
+        const Place at = place_of(p, t, item, threadIdx.x / 32);
+        if (!at.valid) continue;
+        const __nv_bfloat16 *x = t.x[at.rank] + at.off + warp_lane * 8;
+        __nv_bfloat16 *y = t.out[at.rank] + at.off + warp_lane * 8;
+        const int count = at.count - vec;     // heads from this lane's first one on
+        // weights folded into the rotation: y = r (x a + x' b) with x' the partner's and b's sign by the half
+        F8 fa{}, fb{};
+        for (int h = 0; h < at.count; h += kUnroll * kVectors) {
+            uint4 raw[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                raw[u] = make_uint4(0, 0, 0, 0);
+                if (mine && h + u * kVectors < count) raw[u] = ld16(x + u * (kVectors * N * 8));
+            }
+            if (h == 0 && mine) {                  // behind the first loads of x: their latencies overlap
+                const F8 cv = load_feature_major(p.cos, p.S, low ? lane : other, at.pos);
+                const F8 sv = load_feature_major(p.sin, p.S, low ? lane : other, at.pos);
+                const F8 w = widen(ld16(t.w + 8 * lane)), wo = widen(ld16(t.w + 8 * other));
+                const uint64_t sign = low ? pack_f2(-1.f, -1.f) : pack_f2(1.f, 1.f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    fa.p[e] = mul2(w.p[e], cv.p[e]);
+                    fb.p[e] = mul2(mul2(wo.p[e], sv.p[e]), sign);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const F8 own = widen(raw[u]), far = widen(partner(raw[u], src));
+                uint64_t sq = mul2(own.p[0], own.p[0]);
+#pragma unroll
+                for (int e = 1; e < 4; ++e) sq = fma2(own.p[e], own.p[e], sq);
+                const float r = rsqrtf(fmaf(group_sum<N>(sum2(sq), lane), p.inv_D, p.eps));
+                if (!mine || h + u * kVectors >= count) continue;
+                const uint64_t r2 = pack_f2(r, r);
+                F8 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o.p[e] = fma2(mul2(own.p[e], r2), fa.p[e], mul2(mul2(far.p[e], r2), fb.p[e]));
+                st16(y + u * (kVectors * N * 8), narrow(o));
+            }
+            x += kUnroll * kVectors * N * 8;
+            y += kUnroll * kVectors * N * 8;
+        }
     }
 }
 
+// Backward: L lanes hold a vector (those past D/16 idle).  A block keeps the dw sums of its features in registers, at the end adds
+// its groups together in shared memory and writes one partial row, in a fixed order (the result does not depend on timing).
 template <int L>
-__global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_constant__ NormRopeParams p) {
-    constexpr int kUnroll = 4;                     // heads in flight: 128 bytes per thread
-    const int group = threadIdx.x / L, lane = threadIdx.x % L;
-    int item = blockIdx.x;
-    const HeadSet &t = p.t[item >= p.q_items];
-    if (item >= p.q_items) item -= p.q_items;
-    int pos;
-    const Place at = place_of<L>(p, t, item, group, lane, pos);
-    const int half = p.D / 2;
-    const size_t row_elems = (size_t)t.heads * p.D;
-    const size_t base = (size_t)at.row * row_elems + 8 * lane;
-    const __nv_bfloat16 *x = t.x[at.rank] + base;
-    __nv_bfloat16 *y = t.out[at.rank] + base;
-    // weights folded into the rotation: y_lo = r (x_lo a - x_hi b), y_hi = r (x_hi c + x_lo d)
-    float a[8], b[8], c[8], d[8];
-    bool first = true;
-    for (int h = at.head_begin; h < at.head_end; h += kUnroll) {
-        uint4 lo[kUnroll], hi[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            lo[u] = hi[u] = make_uint4(0, 0, 0, 0);
-            if (at.active && h + u < at.head_end) {
-                lo[u] = ld16(x + (size_t)(h + u) * p.D);
-                hi[u] = ld16(x + (size_t)(h + u) * p.D + half);
-            }
-        }
-        if (first && at.active) {                  // behind the first loads of x: their latencies overlap
-            float cv[8], sv[8], wl[8], wh[8];
-            load_angles(p, lane, pos, cv, sv);
-            widen(ld16(t.w + 8 * lane), wl);
-            widen(ld16(t.w + half + 8 * lane), wh);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { a[e] = wl[e] * cv[e]; b[e] = wh[e] * sv[e]; c[e] = wh[e] * cv[e]; d[e] = wl[e] * sv[e]; }
-        }
-        first = false;
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            float xl[8], xh[8], sum = 0.f;
-            widen(lo[u], xl);
-            widen(hi[u], xh);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(xl[e], xl[e], fmaf(xh[e], xh[e], sum));
-            const float r = rsqrtf(fmaf(group_sum<L>(sum), p.inv_D, p.eps));
-            if (!at.active || h + u >= at.head_end) continue;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float l = xl[e] * r, g = xh[e] * r;
-                xl[e] = l * a[e] - g * b[e];
-                xh[e] = g * c[e] + l * d[e];
-            }
-            st16(y + (size_t)(h + u) * p.D, narrow(xl));
-            st16(y + (size_t)(h + u) * p.D + half, narrow(xh));
-        }
-    }
-}
-
-// Backward.  Persistent: a block walks over the items of ONE tensor and keeps the dw sums of its features in registers;
-// at the end it adds its groups together in shared memory and writes one partial row, in a fixed order (the result does
-// not depend on timing).
-template <int L>
-__global__ void __launch_bounds__(kThreads, 2) norm_rope_bwd_kernel(const __grid_constant__ NormRopeParams p) {
-    constexpr int kUnroll = 2;
-    __shared__ float part[kThreads / 32][128];
-    const int group = threadIdx.x / L, lane = threadIdx.x % L;
-    const int which = (int)blockIdx.x >= p.q_blocks;
-    const HeadSet &t = p.t[which];
-    const int n_items = which ? p.items - p.q_items : p.q_items;
-    const int step = which ? (int)gridDim.x - p.q_blocks : p.q_blocks;
-    const int half = p.D / 2;
-    const size_t row_elems = (size_t)t.heads * p.D;
-    float wl[8], wh[8], gl[8], gh[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) gl[e] = gh[e] = wl[e] = wh[e] = 0.f;
-    if (lane * 16 < p.D) {
-        widen(ld16(t.w + 8 * lane), wl);
-        widen(ld16(t.w + half + 8 * lane), wh);
-    }
-    for (int item = (int)blockIdx.x - (which ? p.q_blocks : 0); item < n_items; item += step) {
-        int pos;
-        const Place at = place_of<L>(p, t, item, group, lane, pos);
-        const size_t base = (size_t)at.row * row_elems + 8 * lane;
-        const __nv_bfloat16 *x = t.x[at.rank] + base, *dy = t.dy[at.rank] + base;
-        __nv_bfloat16 *dx = t.out[at.rank] + base;
-        float cv[8], sv[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) cv[e] = sv[e] = 0.f;
-        if (at.active) load_angles(p, lane, pos, cv, sv);
-        for (int h = at.head_begin; h < at.head_end; h += kUnroll) {
+__global__ void __launch_bounds__(kThreads, kBwdBlocks) norm_rope_bwd_kernel(const __grid_constant__ NormRopeParams p) {
+    constexpr int kUnroll = kBwdUnroll;
+    __shared__ float part[kWarps][128];
+    const int lane = threadIdx.x % L, half = p.D / 2;
+    const Share share = share_of(p);
+    const HeadSet &t = p.t[share.which];
+    const bool mine = lane * 16 < p.D;
+    const uint64_t minus = pack_f2(-1.f, -1.f);
+    F8 wl{}, wh{}, gl{}, gh{};
+    if (mine) { wl = widen(ld16(t.w + 8 * lane)); wh = widen(ld16(t.w + half + 8 * lane)); }
+    for (uint32_t item = share.item; item < share.end; item += share.step) {
+        const Place at = place_of(p, t, item, threadIdx.x / L);
+        const bool active = at.valid && mine;
+        const __nv_bfloat16 *x = t.x[at.rank] + at.off + 8 * lane, *dy = t.dy[at.rank] + at.off + 8 * lane;
+        __nv_bfloat16 *dx = t.out[at.rank] + at.off + 8 * lane;
+        F8 cv{}, sv{};
+        for (int h = 0; h < at.count; h += kUnroll) {
             uint4 rx[kUnroll][2], ry[kUnroll][2];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
                 rx[u][0] = rx[u][1] = ry[u][0] = ry[u][1] = make_uint4(0, 0, 0, 0);
-                if (at.active && h + u < at.head_end) {
+                if (active && h + u < at.count) {
                     const size_t o = (size_t)(h + u) * p.D;
                     rx[u][0] = ld16(x + o); rx[u][1] = ld16(x + o + half);
                     ry[u][0] = ld16(dy + o); ry[u][1] = ld16(dy + o + half);
                 }
             }
+            if (h == 0 && active) {                // behind the first loads: their latencies overlap
+                cv = load_feature_major(p.cos, p.S, lane, at.pos);
+                sv = load_feature_major(p.sin, p.S, lane, at.pos);
+            }
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
-                float xl[8], xh[8], ul[8], uh[8], sq = 0.f, dot = 0.f;
-                widen(rx[u][0], xl); widen(rx[u][1], xh);
-                widen(ry[u][0], ul); widen(ry[u][1], uh);
+                const F8 xl = widen(rx[u][0]), xh = widen(rx[u][1]);
+                F8 ul = widen(ry[u][0]), uh = widen(ry[u][1]);
+                uint64_t sq = 0, dot = 0;          // pairs of zeros
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {      // u = R^T dy
-                    const float l = ul[e] * cv[e] + uh[e] * sv[e], g = uh[e] * cv[e] - ul[e] * sv[e];
-                    ul[e] = l; uh[e] = g;
-                    sq = fmaf(xl[e], xl[e], fmaf(xh[e], xh[e], sq));
-                    dot = fmaf(xl[e], l * wl[e], fmaf(xh[e], g * wh[e], dot));
+                for (int e = 0; e < 4; ++e) {      // u = R^T dy
+                    const uint64_t l = fma2(ul.p[e], cv.p[e], mul2(uh.p[e], sv.p[e]));
+                    const uint64_t g = fma2(uh.p[e], cv.p[e], mul2(mul2(ul.p[e], minus), sv.p[e]));
+                    ul.p[e] = l; uh.p[e] = g;
+                    sq = fma2(xl.p[e], xl.p[e], fma2(xh.p[e], xh.p[e], sq));
+                    dot = fma2(xl.p[e], mul2(l, wl.p[e]), fma2(xh.p[e], mul2(g, wh.p[e]), dot));
                 }
-                sq = group_sum<L>(sq);
-                dot = group_sum<L>(dot);
-                const float r = rsqrtf(fmaf(sq, p.inv_D, p.eps));
-                const float k = r * r * r * dot * p.inv_D;
-                if (!at.active || h + u >= at.head_end) continue;
+                const float s1 = group_sum<L>(sum2(sq), lane), s2 = group_sum<L>(sum2(dot), lane);
+                const float r = rsqrtf(fmaf(s1, p.inv_D, p.eps));
+                if (!active || h + u >= at.count) continue;
+                const float k = -r * r * r * s2 * p.inv_D;
+                const uint64_t r2 = pack_f2(r, r), k2 = pack_f2(k, k);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    ul[e] *= r; uh[e] *= r;
-                    gl[e] = fmaf(xl[e], ul[e], gl[e]);
-                    gh[e] = fmaf(xh[e], uh[e], gh[e]);
-                    ul[e] = ul[e] * wl[e] - xl[e] * k;
-                    uh[e] = uh[e] * wh[e] - xh[e] * k;
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t l = mul2(ul.p[e], r2), g = mul2(uh.p[e], r2);
+                    gl.p[e] = fma2(xl.p[e], l, gl.p[e]);
+                    gh.p[e] = fma2(xh.p[e], g, gh.p[e]);
+                    ul.p[e] = fma2(wl.p[e], l, mul2(xl.p[e], k2));
+                    uh.p[e] = fma2(wh.p[e], g, mul2(xh.p[e], k2));
                 }
                 const size_t o = (size_t)(h + u) * p.D;
                 st16(dx + o, narrow(ul));
@@ -232,26 +274,29 @@ __global__ void __launch_bounds__(kThreads, 2) norm_rope_bwd_kernel(const __grid
             }
         }
     }
+    float sums[2][8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { unpack_f2(gl.p[e], sums[0][2 * e], sums[0][2 * e + 1]); unpack_f2(gh.p[e], sums[1][2 * e], sums[1][2 * e + 1]); }
     // groups of a warp, then the warps
 #pragma unroll
     for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int o = 16; o >= L; o >>= 1) {
-            gl[e] += __shfl_xor_sync(0xffffffffu, gl[e], o);
-            gh[e] += __shfl_xor_sync(0xffffffffu, gh[e], o);
+            sums[0][e] += __shfl_xor_sync(0xffffffffu, sums[0][e], o);
+            sums[1][e] += __shfl_xor_sync(0xffffffffu, sums[1][e], o);
         }
-    if (threadIdx.x % 32 < L && lane * 16 < p.D) {
+    if (threadIdx.x % 32 < L && mine) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            part[threadIdx.x / 32][8 * lane + e] = gl[e];
-            part[threadIdx.x / 32][half + 8 * lane + e] = gh[e];
+            part[threadIdx.x / 32][8 * lane + e] = sums[0][e];
+            part[threadIdx.x / 32][half + 8 * lane + e] = sums[1][e];
         }
     }
     __syncthreads();
     if ((int)threadIdx.x < p.D) {
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) s += part[w][threadIdx.x];
+        for (int w = 0; w < kWarps; ++w) s += part[w][threadIdx.x];
         p.partial[(size_t)blockIdx.x * p.D + threadIdx.x] = s;
     }
 }
@@ -272,42 +317,40 @@ __global__ void __launch_bounds__(256) dw_kernel(const float *partial, int D, in
     }
 }
 
-int lanes_of(int D) {
-    int l = 1;
-    while (l * 16 < D) l *= 2;
-    return l;
-}
-
-constexpr int kBwdBlocks = 148 * 2;                // one wave at two blocks per SM
-
-// What both directions share: supported sizes, the geometry and the split into work items.
-int fill(const basp_plan *p, const void *w_q, const void *w_k, const float *cos, const float *sin, float eps, int want_blocks,
-         NormRopeParams *prm) {
-    if (p->D % 16 != 0 || p->D > 128) return BASP_ERR_UNSUPPORTED;
-    if (!(eps > 0.f) || !(eps <= 3.0e38f)) return BASP_ERR_INVALID;
-    if ((long long)p->Bl * p->T >= (1ll << 30)) return BASP_ERR_UNSUPPORTED;
+// What both directions share: supported sizes, the geometry and the split of the work into items of tile_tokens tokens and
+// chunk_heads heads (a multiple of `batch`, the heads that a warp has in flight).
+int fill(const basp_plan *p, const void *w_q, const void *w_k, const float *cos, const float *sin, float eps, int tile_tokens,
+         int batch, int items_per_block, int wave, NormRopeParams *prm, int *blocks) {
+    const long long rows = (long long)p->Bl * p->T, tiles = (rows + tile_tokens - 1) / tile_tokens;
+    if (tiles * tile_tokens >= (1ll << 31) || tiles * p->N * p->Hq >= (1ll << 31)) return BASP_ERR_UNSUPPORTED;     // 31-bit rows, items
     prm->cos = cos; prm->sin = sin; prm->eps = eps; prm->inv_D = 1.0f / (float)p->D;
-    prm->D = p->D; prm->S = p->S; prm->T = p->T; prm->T_last = p->T_last; prm->K = p->K; prm->Bl = p->Bl; prm->N = p->N;
-    prm->div_T = make_fastdiv((uint32_t)p->T); prm->div_T_last = make_fastdiv((uint32_t)p->T_last);
+    prm->D = p->D; prm->S = p->S; prm->T = p->T; prm->T_last = p->T_last; prm->K = p->K; prm->Bl = p->Bl;
+    prm->tiles = (uint32_t)tiles; prm->tile_tokens = (uint32_t)tile_tokens;
     prm->t[0].w = (const __nv_bfloat16 *)w_q; prm->t[0].heads = p->Hq;
     prm->t[1].w = (const __nv_bfloat16 *)w_k; prm->t[1].heads = p->Hkv;
-    const int tokens = kThreads / lanes_of(p->D);
-    prm->tiles = (p->Bl * p->T + tokens - 1) / tokens;
-    // Few tokens: a token's heads are spread over blocks until the grid is want_blocks; many: one block takes them all
-    const long long units = (long long)p->N * prm->tiles;
-    const int heads = p->Hq + p->Hkv;
-    long long per = units * heads / want_blocks;
-    per = per < 1 ? 1 : (per > heads ? heads : per);
-    prm->chunk_heads = (int)per;
-    long long items = 0;
+    // A token's heads together where there are many tokens; with fewer the heads are spread over more items, so that a block has
+    // several and the last round of them is short
+    const long long per = tiles * p->N * (p->Hq + p->Hkv) / ((long long)items_per_block * wave);
+    prm->chunk_heads = (uint32_t)(per < batch ? batch : per / batch * batch);
+    if (prm->chunk_heads > (uint32_t)p->Hq) prm->chunk_heads = p->Hq;
     for (HeadSet &t : prm->t) {
         t.chunks = (t.heads + prm->chunk_heads - 1) / prm->chunk_heads;
-        items += units * t.chunks;
-        if (&t == &prm->t[0]) prm->q_items = (int)items;
+        t.items = (uint32_t)(tiles * p->N * t.chunks);
     }
-    if (items >= (1ll << 31)) return BASP_ERR_UNSUPPORTED;
-    prm->items = (int)items;
+    // blocks in proportion to the heads, at least one per tensor, none without an item
+    const long long all = (long long)prm->t[0].items + prm->t[1].items, total = all < wave ? all : wave;
+    long long q = (total * p->Hq + (p->Hq + p->Hkv) / 2) / (p->Hq + p->Hkv);
+    if (total - q > prm->t[1].items) q = total - prm->t[1].items;
+    if (q > prm->t[0].items) q = prm->t[0].items;
+    q = q < 1 ? 1 : (q > total - 1 ? total - 1 : q);
+    prm->q_blocks = (int)q;
+    *blocks = (int)total;
     return BASP_OK;
+}
+
+int supported(const basp_plan *p, float eps) {
+    if (p->D % 16 != 0 || p->D > 128) return BASP_ERR_UNSUPPORTED;
+    return eps > 0.f && eps <= 3.0e38f ? BASP_OK : BASP_ERR_INVALID;
 }
 
 // Adds the shards of one tensor to the spans and the parameter block.
@@ -330,14 +373,18 @@ int add_tables(const basp_plan *p, SpanSet *s, const void *w_q, const void *w_k,
     return s->add_in(sin, table, 4);
 }
 
-template <typename F>
-int by_lanes(int D, F &&f) {
-    switch (lanes_of(D)) {
-        case 1: return f(std::integral_constant<int, 1>{});
-        case 2: return f(std::integral_constant<int, 2>{});
-        case 4: return f(std::integral_constant<int, 4>{});
-        default: return f(std::integral_constant<int, 8>{});
-    }
+// f(the number as a type) for one of the listed numbers
+template <int... kN, typename F>
+int dispatch(int n, F &&f) {
+    int rc = BASP_ERR_UNSUPPORTED;
+    ((n == kN ? (void)(rc = f(std::integral_constant<int, kN>{})) : (void)0), ...);
+    return rc;
+}
+
+int bwd_lanes(int D) {
+    int l = 1;
+    while (l * 16 < D) l *= 2;
+    return l;
 }
 
 }  // namespace
@@ -347,7 +394,9 @@ extern "C" int basp_qk_norm_rope(const basp_plan *p, const void *const *q_seq, c
                                  void *const *k_out, void *stream) {
     if (!p) return BASP_ERR_NULL;
     NormRopeParams prm;
-    BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, 148 * 16, &prm));
+    int blocks = 0;
+    BASP_TRY(supported(p, eps));
+    BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kWarps, kFwdUnroll * (32 / (p->D / 8)), 8, 148 * kFwdBlocks, &prm, &blocks));
     SpanSet spans;
     BASP_TRY(add_tables(p, &spans, w_q, w_k, rope_cos, rope_sin));
     BASP_TRY(add_shards(p, &spans, p->Hq, q_seq, false, 0, prm.t[0].x));
@@ -355,8 +404,8 @@ extern "C" int basp_qk_norm_rope(const basp_plan *p, const void *const *q_seq, c
     BASP_TRY(add_shards(p, &spans, p->Hq, q_out, true, 0, const_cast<const __nv_bfloat16 **>(prm.t[0].out)));
     BASP_TRY(add_shards(p, &spans, p->Hkv, k_out, true, 1, const_cast<const __nv_bfloat16 **>(prm.t[1].out)));
     BASP_TRY(spans.overlaps());
-    return by_lanes(p->D, [&](auto lanes) -> int {
-        norm_rope_kernel<decltype(lanes)::value><<<prm.items, kThreads, 0, (cudaStream_t)stream>>>(prm);
+    return dispatch<2, 4, 6, 8, 10, 12, 14, 16>(p->D / 8, [&](auto lanes) -> int {
+        norm_rope_kernel<decltype(lanes)::value><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(prm);
         BASP_CUDA_TRY(cudaGetLastError());
         basp_count_launch(1);
         return BASP_OK;
@@ -364,7 +413,7 @@ extern "C" int basp_qk_norm_rope(const basp_plan *p, const void *const *q_seq, c
 }
 
 extern "C" size_t basp_qk_norm_rope_bwd_workspace_bytes(const basp_plan *p) {
-    return p ? (size_t)(kBwdBlocks + 1) * p->D * 4 : 0;
+    return p ? (size_t)148 * kBwdBlocks * p->D * 4 : 0;
 }
 
 extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *w_q,
@@ -374,7 +423,9 @@ extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_se
                                      void *stream) {
     if (!p) return BASP_ERR_NULL;
     NormRopeParams prm;
-    BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kBwdBlocks * 4, &prm));
+    int blocks = 0;
+    BASP_TRY(supported(p, eps));
+    BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kThreads / bwd_lanes(p->D), kBwdUnroll, 4, 148 * kBwdBlocks, &prm, &blocks));
     SpanSet spans;
     BASP_TRY(add_tables(p, &spans, w_q, w_k, rope_cos, rope_sin));
     BASP_TRY(add_shards(p, &spans, p->Hq, q_seq, false, -1, prm.t[0].x));
@@ -388,19 +439,11 @@ extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_se
     BASP_TRY(spans.add_out(workspace, basp_qk_norm_rope_bwd_workspace_bytes(p)));
     if (workspace_bytes < basp_qk_norm_rope_bwd_workspace_bytes(p)) return BASP_ERR_WORKSPACE;
     BASP_TRY(spans.overlaps());
-    // blocks in proportion to the tensors' vectors, at least one each
-    const int total = prm.items < kBwdBlocks ? prm.items : kBwdBlocks;
-    int q_blocks = (int)((long long)total * p->Hq / (p->Hq + p->Hkv));
-    q_blocks = q_blocks < 1 ? 1 : (q_blocks > prm.q_items ? prm.q_items : q_blocks);
-    int k_blocks = total - q_blocks;
-    k_blocks = k_blocks < 1 ? 1 : (k_blocks > prm.items - prm.q_items ? prm.items - prm.q_items : k_blocks);
-    prm.q_blocks = q_blocks;
     prm.partial = (float *)workspace;
-    const int blocks = q_blocks + k_blocks;
-    return by_lanes(p->D, [&](auto lanes) -> int {
+    return dispatch<1, 2, 4, 8>(bwd_lanes(p->D), [&](auto lanes) -> int {
         norm_rope_bwd_kernel<decltype(lanes)::value><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(prm);
         BASP_CUDA_TRY(cudaGetLastError());
-        dw_kernel<<<dim3(p->D / 8, 2), 256, 0, (cudaStream_t)stream>>>(prm.partial, p->D, q_blocks, blocks, dw_q, dw_k);
+        dw_kernel<<<dim3(p->D / 8, 2), 256, 0, (cudaStream_t)stream>>>(prm.partial, p->D, prm.q_blocks, blocks, dw_q, dw_k);
         BASP_CUDA_TRY(cudaGetLastError());
         basp_count_launch(2);
         return BASP_OK;
