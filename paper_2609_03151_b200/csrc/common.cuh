@@ -36,6 +36,22 @@ __device__ __forceinline__ uint32_t fdiv(uint32_t n, const FastDiv &f) {
     return f.d == 1 ? n : (__umulhi(n, f.mul) >> f.shr);
 }
 
+// Launches a kernel that may start before the previous one of the stream has finished: it reads what that one writes only behind
+// ptx::wait_previous_kernel().
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, cudaStream_t stream, const Args &...args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 static inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 // A softmax scale the kernels accept: 0 (= 1/sqrt(D)) or a positive finite number (not NaN, not negative, not infinite).
 static inline bool scale_ok(float s) { return s >= 0.f && s <= 3.0e38f; }

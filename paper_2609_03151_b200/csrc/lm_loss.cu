@@ -53,6 +53,7 @@ constexpr int kRowsPerCta = kPair ? 2 * kBM : kBM;
 template <bool kPair>
 constexpr int kTileM = kPair ? 4 * kBM : kBM;
 constexpr int kThreads = 320;                      // TMA warp, MMA warp, eight epilogue warps
+constexpr int kStagingBytes = 4 << 10;             // of an epilogue warp: 32 rows of 128 bytes
 constexpr int kStages = 4, kStageBytes = 48 << 10; // A 128 and B 256 rows of 128 bytes, or A 256 and half of B
 constexpr int kMnBlock = kBK * 64 * 2;             // one 64-column block of an MN-major operand: 64 rows of 128 bytes
 constexpr int kSms = 148;                          // of the GPU this code is written for; plans the split, not the grid
@@ -87,13 +88,14 @@ template <int R>
 struct LossParams {
     CUtensorMap x[R];          // (1): boxes of one slot
     CUtensorMap w, dz;
+    CUtensorMap dw;            // (3): boxes of a warp's 32 rows
     CUtensorMap kept;          // (3): the piece's rows of x, zero where a row has no part in the gradients
     const long long *label[R];
     __nv_bfloat16 *dx[R];
     Rows rows;
     int tiles_m, tiles_n, k_blocks, splits, group;
     int vocab, hidden;
-    bool wide;                 // (2), (3): every row of the result starts on a multiple of 32 bytes
+    bool wide;                 // (2): every row of the result starts on a multiple of 32 bytes
     size_t pitch;              // columns of a row of 16-bit logits
     int piece_rows;
     float2 *stats;             // [groups of kStatCols columns][piece_rows]: maximum, sum
@@ -103,7 +105,6 @@ struct LossParams {
     float *partial;            // (2) with splits > 1: [splits][piece_rows][hidden]
     const float *acc_in;       // (3) sum of the earlier pieces, or NULL
     float *acc_out;            // (3) sum so far, or NULL: the result
-    __nv_bfloat16 *dw;
     int *status;
 };
 
@@ -204,6 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
     if constexpr (kPair) cluster_sync();                   // both CTAs' barriers and tensor memory are there
     tc_fence_after();
     const uint32_t tmem = bars.tmem_base;
+    allow_next_kernel();                                   // the pass behind this product has work of its own to start with
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer (lane 0 issues)
@@ -336,6 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
         const int quarter = warp & 3;                       // the TMEM lanes this warp can reach
         const int row = quarter * 32 + lane;
         const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
+        uint8_t *staging = smem + kStages * kStageBytes + (warp - 2) * kStagingBytes;       // (3)
         uint32_t cnt = 0;
         float scale = 1.f;
         if constexpr (kKind == kDx || kKind == kDw) scale = __uint_as_float(*p.scale);
@@ -429,11 +432,12 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                     tmem_wait_ld();
                     if (c == kCols / 32 - 1) hand_back();
                     const int cols = min(32, width - c * 32);
-                    if (!tok.valid || cols <= 0) continue;
+                    const bool live = tok.valid && cols > 0;
                     float v[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(raw[e]) * scale;
                     if constexpr (kKind == kDx) {
+                        if (!live) continue;
                         if (p.splits == 1) {
                             store_bf16x32(p.dx[tok.rank] + (size_t)tok.row * p.hidden + col0 + c * 32, v, cols, p.wide);
                         } else {
@@ -444,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                         }
                     } else {
                         const size_t at = (size_t)prow * p.hidden + col0 + c * 32;
-                        if (p.acc_in) {
+                        if (p.acc_in && live) {
 #pragma unroll
                             for (int q = 0; q < 8; ++q)
                                 if (4 * q < cols) {
@@ -453,16 +457,37 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                                 }
                         }
                         if (p.acc_out) {
+                            if (!live) continue;
 #pragma unroll
                             for (int q = 0; q < 8; ++q)
                                 if (4 * q < cols) *reinterpret_cast<float4 *>(p.acc_out + at + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
                         } else {
-                            store_bf16x32(p.dw + at, v, cols, p.wide);
+                            // 64 columns of the warp's 32 rows at a time through shared memory: stored by lanes, each in a row of
+                            // its own, they keep the load/store unit busy for one line per lane (dW of 48 tokens: 68 us)
+                            if (c % 2 == 0) {
+                                if (lane == 0) tma_store_wait_read<0>();
+                                __syncwarp();
+                            }
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                *reinterpret_cast<uint4 *>(staging + lane * 128 + ((((c & 1) * 4 + q) ^ (lane & 7)) << 4)) =
+                                    make_uint4(pack_bf16x2(v[8 * q], v[8 * q + 1]), pack_bf16x2(v[8 * q + 2], v[8 * q + 3]),
+                                               pack_bf16x2(v[8 * q + 4], v[8 * q + 5]), pack_bf16x2(v[8 * q + 6], v[8 * q + 7]));
+                            if (c % 2 == 1) {
+                                fence_proxy_async_smem();
+                                __syncwarp();
+                                const int first_col = col0 + (c - 1) * 32, first_row = prow - lane;
+                                if (lane == 0 && first_col < p.hidden && first_row < p.vocab) {     // the ends are cut off by the copy
+                                    tma_store_3d(&p.dw, staging, first_col, 0, first_row);
+                                    tma_store_commit();
+                                }
+                            }
                         }
                     }
                 }
             }
         }
+        if (kKind == kDw && lane == 0) tma_store_wait<0>();
     }
 
 gemm_done:
@@ -519,22 +544,6 @@ __global__ void __launch_bounds__(1024) lm_merge_kernel(const __grid_constant__ 
     const Token tok = token_of(p.rows, row);
     const long long label = tok.valid ? p.label[tok.rank][tok.row] : -1;
     const bool counts = label >= 0 && label < p.vocab;
-    {
-        const int i = blockIdx.x * 32 + lane;
-        float m = -INFINITY, s = 0.f;
-        constexpr int kBatch = 8;                  // loads in flight
-        for (int n0 = warp; n0 < p.groups; n0 += 32 * kBatch) {
-            float2 v[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int n = n0 + 32 * u;
-                v[u] = n < p.groups ? p.stats[(size_t)n * p.piece_rows + i] : make_float2(-INFINITY, 0.f);
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) join(m, s, v[u].x, v[u].y);
-        }
-        part[warp][lane] = make_float2(m, s);
-    }
     // the target's logit in fp32 operations rounded to nearest: the tensor cores' sum of a large logit (they cut off what does
     // not fit) would be the largest error of the loss
     float z = 0.f;
@@ -553,6 +562,23 @@ __global__ void __launch_bounds__(1024) lm_merge_kernel(const __grid_constant__ 
             }
         }
         z = ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+    }
+    wait_previous_kernel();                        // up to here only the call's inputs were read
+    {
+        const int i = blockIdx.x * 32 + lane;
+        float m = -INFINITY, s = 0.f;
+        constexpr int kBatch = 8;                  // loads in flight
+        for (int n0 = warp; n0 < p.groups; n0 += 32 * kBatch) {
+            float2 v[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int n = n0 + 32 * u;
+                v[u] = n < p.groups ? p.stats[(size_t)n * p.piece_rows + i] : make_float2(-INFINITY, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) join(m, s, v[u].x, v[u].y);
+        }
+        part[warp][lane] = make_float2(m, s);
     }
     __syncthreads();
     const float2 mine = part[lane][warp];
@@ -677,6 +703,7 @@ __global__ void __launch_bounds__(256) lm_dx_join_kernel(const __grid_constant__
     const int per_row = p.hidden / 8;
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     const int row = (int)(i / per_row), c = (int)(i - (long long)row * per_row) * 8;
+    wait_previous_kernel();
     if (row >= p.piece_rows) return;
     const Token tok = token_of(p.rows, row);
     if (!tok.valid) return;
@@ -785,7 +812,7 @@ int launch_as(const LossParams<R> &prm, cudaStream_t st) {
     BASP_CUDA_TRY(cudaGetDevice(&dev));
     BASP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     const long long items = (long long)prm.tiles_m * prm.tiles_n * prm.splits, slots = kPair ? sms / 2 : sms;
-    const int smem = kStages * kStageBytes + 1024;
+    const int smem = kStages * kStageBytes + (kKind == kDw ? 8 * kStagingBytes : 0) + 1024;
     BASP_CUDA_TRY(cudaFuncSetAttribute(lm_gemm_kernel<kKind, R, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(items < slots ? items : slots) * (kPair ? 2 : 1));
@@ -841,7 +868,6 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
     prm.vocab = a.vocab; prm.hidden = a.hidden; prm.pitch = z.pitch; prm.piece_rows = rows;
     prm.stats = (float2 *)(a.ws + w.stats); prm.scale = (unsigned *)(a.ws + w.scale);
     prm.codes = (uint16_t *)(a.ws + w.codes); prm.partial = (float *)(a.ws + w.partial);
-    prm.dw = (__nv_bfloat16 *)a.dw;
     for (int r = 0; r < p->N; ++r) {
         prm.label[r] = a.labels[r];
         prm.dx[r] = a.dx ? (__nv_bfloat16 *)a.dx[r] : nullptr;
@@ -864,6 +890,7 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
         BASP_TRY(tmap::encode_rows_heads_d(&w_mn, a.w, a.vocab, 1, a.hidden, kBK));
         BASP_TRY(tmap::encode_rows_heads_d(&dz_k, prm.codes, rows, 1, z.pitch, kBM));
         BASP_TRY(tmap::encode_rows_heads_d(&dz_mn, prm.codes, rows, 1, z.pitch, kBK));
+        if (a.dw) BASP_TRY(tmap::encode_rows_heads_d(&prm.dw, a.dw, a.vocab, 1, a.hidden, 32));
         BASP_TRY(tmap::encode_rows_heads_d(&prm.kept, a.ws + w.kept, rows, 1, a.hidden, kBK));
     }
     bool wide_dx = a.hidden % 16 == 0;
@@ -884,8 +911,7 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
         prm.w = w_k[use_pair(tiles * kBM)];
         if (grad) BASP_TRY((launch_gemm<kLogits, R>(prm, tiles * kBM, st)));
         else BASP_TRY((launch_gemm<kStats, R>(prm, tiles * kBM, st)));
-        lm_merge_kernel<R><<<tiles * kBM / 32, 1024, 0, st>>>(merge);
-        BASP_CUDA_TRY(cudaGetLastError());
+        BASP_CUDA_TRY(launch_early(lm_merge_kernel<R>, dim3(tiles * kBM / 32), 1024, st, merge));
         basp_count_launch(1);
         if (!grad) continue;
         dz.rows = prm.rows;
@@ -903,15 +929,14 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
                 JoinParams<R> join;
                 memcpy(join.dx, prm.dx, sizeof(join.dx));
                 join.rows = prm.rows; join.partial = prm.partial; join.splits = prm.splits; join.piece_rows = rows; join.hidden = a.hidden;
-                lm_dx_join_kernel<R><<<cdiv((long long)tiles * kBM * (a.hidden / 8), 256), 256, 0, st>>>(join);
-                BASP_CUDA_TRY(cudaGetLastError());
+                BASP_CUDA_TRY(launch_early(lm_dx_join_kernel<R>, dim3(cdiv((long long)tiles * kBM * (a.hidden / 8), 256)), 256, st, join));
                 basp_count_launch(1);
             }
         }
         // (3)
         if (a.dw) {
             prm.dz = dz_mn;
-            prm.tiles_n = z.tiles_h; prm.splits = 1; prm.wide = a.hidden % 16 == 0 && (uintptr_t)a.dw % 32 == 0;
+            prm.tiles_n = z.tiles_h; prm.splits = 1;
             prm.k_blocks = cdiv((long long)prm.rows.slots << z.slot_log2, kBK);
             prm.acc_in = piece > 0 ? (const float *)(a.ws + w.acc) : nullptr;
             prm.acc_out = piece + 1 < z.pieces ? (float *)(a.ws + w.acc) : nullptr;

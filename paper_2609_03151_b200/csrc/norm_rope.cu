@@ -9,10 +9,10 @@
 // What the kernels wait for is memory latency, so they are laid out by the bytes in flight per SM that the registers allow:
 //   forward   a lane holds eight features, D/8 lanes a vector, a warp 32 / (D/8) neighbouring heads of one token (of 512 bytes at
 //             D = 128); the rotation's partner comes by shuffle.  80 registers, three blocks of 256 threads per SM.
-//             2 x 8K tokens, 64 heads of 128: 93 us (5.8 TB/s); with the backward's layout 104 us.
+//             2 x 8K tokens, 64 heads of 128: 95 us (5.7 TB/s); with the backward's layout 104 us.
 //   backward  a lane holds eight features and their eight partners, so D/16 lanes (rounded up to a power of two) a vector, no
 //             shuffle but the sums; the groups of lanes hold neighbouring tokens.  126 registers, two blocks per SM.
-//             128K tokens, 40 heads of 128: 700 us (5.8 TB/s); with the forward's layout 727 us.
+//             128K tokens, 40 heads of 128: 707 us (5.8 TB/s); with the forward's layout 727 us.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -218,6 +218,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) norm_rope_bwd_kernel(con
     const Share share = share_of(p);
     const HeadSet &t = p.t[share.which];
     const bool mine = lane * 16 < p.D;
+    allow_next_kernel();
     const uint64_t minus = pack_f2(-1.f, -1.f);
     F8 wl{}, wh{}, gl{}, gh{};
     if (mine) { wl = widen(ld16(t.w + 8 * lane)); wh = widen(ld16(t.w + half + 8 * lane)); }
@@ -307,6 +308,7 @@ __global__ void __launch_bounds__(256) dw_kernel(const float *partial, int D, in
     const int f = threadIdx.x % 8, i = threadIdx.x / 8, col = blockIdx.x * 8 + f;
     const int b0 = blockIdx.y ? q_blocks : 0, b1 = blockIdx.y ? blocks : q_blocks;
     float s = 0.f;
+    wait_previous_kernel();
 #pragma unroll 8
     for (int b = b0 + i; b < b1; b += 32) s += partial[(size_t)b * D + col];
     part[i][f] = s;
@@ -443,8 +445,8 @@ extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_se
     return dispatch<1, 2, 4, 8>(bwd_lanes(p->D), [&](auto lanes) -> int {
         norm_rope_bwd_kernel<decltype(lanes)::value><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(prm);
         BASP_CUDA_TRY(cudaGetLastError());
-        dw_kernel<<<dim3(p->D / 8, 2), 256, 0, (cudaStream_t)stream>>>(prm.partial, p->D, prm.q_blocks, blocks, dw_q, dw_k);
-        BASP_CUDA_TRY(cudaGetLastError());
+        BASP_CUDA_TRY(launch_early(dw_kernel, dim3(p->D / 8, 2), 256, (cudaStream_t)stream, (const float *)prm.partial, p->D, prm.q_blocks,
+                                   blocks, dw_q, dw_k));
         basp_count_launch(2);
         return BASP_OK;
     });

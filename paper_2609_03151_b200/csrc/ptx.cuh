@@ -205,6 +205,11 @@ __device__ __forceinline__ void mma_ss_pair(uint32_t d_tmem, uint64_t a_desc, ui
         : "memory");
 }
 
+// Programmatic dependent launch: the next kernel of the stream may start (its blocks as soon as they find room); a kernel that was
+// started so waits here until the previous one has finished and its writes can be read.
+__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Instruction descriptor of kind::f16 with bf16 A and B, fp32 D.
 //   bits 4-5 D format (1 = f32) | 7-9 A format (1 = bf16) | 10-12 B format (1 = bf16)
 //   bit 15 A is MN-major | bit 16 B is MN-major | 17-22 N/8 | 24-28 M/16
