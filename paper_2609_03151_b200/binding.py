@@ -16,6 +16,7 @@ if not os.path.exists(_LIB_PATH):
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2609_03151_b200.build` "
                       "(there is no fallback path)")
 lib = ctypes.CDLL(_LIB_PATH)
+from ._marshal import addresses as _fast_addresses  # noqa: E402  (built beside the library, from csrc/marshal.cpp)
 
 BASP_OK = 0
 BASP_ERR_INVALID, BASP_ERR_UNSUPPORTED, BASP_ERR_NULL, BASP_ERR_ALIGN = -1, -2, -3, -4
@@ -422,24 +423,21 @@ def basp_out_proj(plan, hidden, o_seq, w_o, y_seq, stream=None):
                              _stream(stream)), "basp_out_proj")
 
 
-_T = torch.Tensor
-_numel, _contiguous, _device, _data_ptr, _dtype = _T.numel, _T.is_contiguous, _T.get_device, _T.data_ptr, _T.dtype.__get__
+_BF16, _F32, _I64, _U8 = torch.bfloat16, torch.float32, torch.int64, torch.uint8
 
 
 class _Marshal:
     """Pointer tables and checks of one call.  The library sees addresses only, so tensors that it would misread are refused
     here: wrong type or size, gaps between the elements, not in the current device's memory.  Raw addresses and objects with a
-    data_ptr (as_shards) pass as they are.  Short calls take less time on the GPU than here, so all shards of a type are checked
-    together, by functions that loop outside the interpreter."""
+    data_ptr (as_shards) pass as they are."""
 
     __slots__ = ("device", "kept")
 
     def __init__(self):
         self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
-        self.kept = []                 # the tables, while the call reads them
 
-    def address(self, t, dtype, numel, what):
-        if isinstance(t, _T):
+    def _address(self, t, dtype, numel, what):
+        if isinstance(t, torch.Tensor):
             if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
                 raise ValueError(f"{what}: expected {numel} contiguous elements of {dtype}, got {tuple(t.shape)} of {t.dtype}"
                                  + ("" if t.is_contiguous() else ", not contiguous"))
@@ -450,31 +448,26 @@ class _Marshal:
             return t.data_ptr()
         return None if t is None else t.data_ptr() if hasattr(t, "data_ptr") else int(t)
 
-    def tables(self, dtype, *named):
-        """Addresses of pointer tables, one for each (name, shards or None, tuple of their sizes in elements)."""
-        flat, sizes = [], ()
-        for what, shards, want in named:
-            if shards is not None:
-                if len(shards) != len(want):
-                    raise ValueError(f"expected {len(want)} shards, got {len(shards)}: {what}")
-                flat += shards
-                sizes += want
-        try:
-            right = tuple(map(_numel, flat)) == sizes and set(map(_dtype, flat)) == {dtype} and \
-                set(map(_device, flat)) == {self.device} and all(map(_contiguous, flat))
-        except TypeError:              # not all of them tensors
-            right = False
-        if right:
-            table = (c_void_p * len(flat))(*map(_data_ptr, flat))
-        else:
-            names = [f"{what}[{i}]" for what, shards, want in named if shards is not None for i in range(len(want))]
-            table = (c_void_p * len(flat))(*[self.address(t, dtype, n, what) for t, n, what in zip(flat, sizes, names)])
-        self.kept.append(table)
-        at, out = ctypes.addressof(table), []
-        for _, shards, want in named:
-            out.append(None if shards is None else at)
-            if shards is not None:
-                at += 8 * len(want)
+    def addresses(self, *named):
+        """One address for each (name, dtype, shards, sizes): of the table of a list's addresses (sizes: a tuple), of one tensor
+        (sizes: its elements), None for None."""
+        right = _fast_addresses(self.device, named)
+        if right is not None:
+            self.kept, out = right
+            return out
+        self.kept, out = [], []
+        for what, dtype, shards, sizes in named:
+            if shards is None:
+                out.append(None)
+            elif isinstance(sizes, int):
+                out.append(self._address(shards, dtype, sizes, what))
+            else:
+                if len(shards) != len(sizes):
+                    raise ValueError(f"expected {len(sizes)} shards, got {len(shards)}: {what}")
+                table = (c_void_p * len(sizes))(*[self._address(t, dtype, n, f"{what}[{i}]")
+                                                  for i, (t, n) in enumerate(zip(shards, sizes))])
+                self.kept.append(table)
+                out.append(ctypes.addressof(table))
         return out
 
     def space(self, workspace):
@@ -506,11 +499,11 @@ def basp_qk_norm_rope(plan, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, q_out, k
     basp_qkv_proj_rope (same feature-major tables).  q_out[r] may be q_seq[r], k_out[r] may be k_seq[r]."""
     m, D, table = _Marshal(), plan.D, plan.D // 2 * plan.S
     q, k = _qk(plan)
-    x, xk, y, yk = m.tables(torch.bfloat16, ("q_seq", q_seq, q), ("k_seq", k_seq, k), ("q_out", q_out, q), ("k_out", k_out, k))
-    _check(lib.basp_qk_norm_rope(plan.handle, x, xk, m.address(w_q, torch.bfloat16, D, "w_q"),
-                                 m.address(w_k, torch.bfloat16, D, "w_k"), m.address(rope_cos, torch.float32, table, "rope_cos"),
-                                 m.address(rope_sin, torch.float32, table, "rope_sin"), eps, y, yk, m.stream(stream)),
-           "basp_qk_norm_rope")
+    x, xk, wq, wk, cos, sin, y, yk = m.addresses(
+        ("q_seq", _BF16, q_seq, q), ("k_seq", _BF16, k_seq, k), ("w_q", _BF16, w_q, D), ("w_k", _BF16, w_k, D),
+        ("rope_cos", _F32, rope_cos, table), ("rope_sin", _F32, rope_sin, table), ("q_out", _BF16, q_out, q),
+        ("k_out", _BF16, k_out, k))
+    _check(lib.basp_qk_norm_rope(plan.handle, x, xk, wq, wk, cos, sin, eps, y, yk, m.stream(stream)), "basp_qk_norm_rope")
 
 
 def basp_qk_norm_rope_bwd_workspace_bytes(plan) -> int:
@@ -522,14 +515,13 @@ def basp_qk_norm_rope_bwd(plan, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, dq_o
     """Gradients of basp_qk_norm_rope: dq_seq, dk_seq (bf16; may be dq_out, dk_out themselves) and dw_q, dw_k (fp32 [D])."""
     m, D, table = _Marshal(), plan.D, plan.D // 2 * plan.S
     q, k = _qk(plan)
-    x, xk, dy, dyk, dx, dxk = m.tables(torch.bfloat16, ("q_seq", q_seq, q), ("k_seq", k_seq, k), ("dq_out", dq_out, q),
-                                       ("dk_out", dk_out, k), ("dq_seq", dq_seq, q), ("dk_seq", dk_seq, k))
-    _check(lib.basp_qk_norm_rope_bwd(plan.handle, x, xk, m.address(w_q, torch.bfloat16, D, "w_q"),
-                                     m.address(w_k, torch.bfloat16, D, "w_k"),
-                                     m.address(rope_cos, torch.float32, table, "rope_cos"),
-                                     m.address(rope_sin, torch.float32, table, "rope_sin"), eps, dy, dyk, dx, dxk,
-                                     m.address(dw_q, torch.float32, D, "dw_q"), m.address(dw_k, torch.float32, D, "dw_k"),
-                                     *m.space(workspace), m.stream(stream)), "basp_qk_norm_rope_bwd")
+    x, xk, wq, wk, cos, sin, dy, dyk, dx, dxk, gq, gk = m.addresses(
+        ("q_seq", _BF16, q_seq, q), ("k_seq", _BF16, k_seq, k), ("w_q", _BF16, w_q, D), ("w_k", _BF16, w_k, D),
+        ("rope_cos", _F32, rope_cos, table), ("rope_sin", _F32, rope_sin, table), ("dq_out", _BF16, dq_out, q),
+        ("dk_out", _BF16, dk_out, k), ("dq_seq", _BF16, dq_seq, q), ("dk_seq", _BF16, dk_seq, k), ("dw_q", _F32, dw_q, D),
+        ("dw_k", _F32, dw_k, D))
+    _check(lib.basp_qk_norm_rope_bwd(plan.handle, x, xk, wq, wk, cos, sin, eps, dy, dyk, dx, dxk, gq, gk, *m.space(workspace),
+                                     m.stream(stream)), "basp_qk_norm_rope_bwd")
 
 
 def basp_ckpt_bytes(plan, rank) -> int:
@@ -537,37 +529,39 @@ def basp_ckpt_bytes(plan, rank) -> int:
     return int(lib.basp_ckpt_bytes(plan.handle, int(rank)))
 
 
-def _ckpt(plan, m, ckpt):
+def _ckpt_sizes(plan):
     sizes = plan.sizes.get("ckpt")
     if sizes is None:
         sizes = plan.sizes["ckpt"] = tuple(basp_ckpt_bytes(plan, r) for r in range(plan.N))
-    return m.tables(torch.uint8, ("ckpt", ckpt, sizes))[0]
+    return sizes
 
 
 def basp_ckpt_pack(plan, q_seq, k_seq, v_seq, o_seq, ckpt, stream=None):
     """Q, K, V and O to 8 bits with one scale per head vector; ckpt[r]: uint8 tensor of basp_ckpt_bytes(plan, r)."""
     m = _Marshal()
     q, k = _qk(plan)
-    t = m.tables(torch.bfloat16, ("q_seq", q_seq, q), ("k_seq", k_seq, k), ("v_seq", v_seq, k), ("o_seq", o_seq, q))
-    _check(lib.basp_ckpt_pack(plan.handle, *t, _ckpt(plan, m, ckpt), m.stream(stream)), "basp_ckpt_pack")
+    a = m.addresses(("q_seq", _BF16, q_seq, q), ("k_seq", _BF16, k_seq, k), ("v_seq", _BF16, v_seq, k), ("o_seq", _BF16, o_seq, q),
+                    ("ckpt", _U8, ckpt, _ckpt_sizes(plan)))
+    _check(lib.basp_ckpt_pack(plan.handle, *a, m.stream(stream)), "basp_ckpt_pack")
 
 
 def basp_ckpt_reshard_s2h(plan, ckpt, q_head, k_head, v_head, o_head, stream=None):
     """Checkpoints to head-sharded bf16 Q, K, V and O: the reading back and the all-to-all in one launch."""
     m, vec = _Marshal(), plan.Bl * plan.S * plan.D
     q, k = (vec * plan.Hq_l,) * plan.N, (vec * plan.Hkv_l,) * plan.N
-    t = m.tables(torch.bfloat16, ("q_head", q_head, q), ("k_head", k_head, k), ("v_head", v_head, k), ("o_head", o_head, q))
-    _check(lib.basp_ckpt_reshard_s2h(plan.handle, _ckpt(plan, m, ckpt), *t, m.stream(stream)), "basp_ckpt_reshard_s2h")
+    a = m.addresses(("ckpt", _U8, ckpt, _ckpt_sizes(plan)), ("q_head", _BF16, q_head, q), ("k_head", _BF16, k_head, k),
+                    ("v_head", _BF16, v_head, k), ("o_head", _BF16, o_head, q))
+    _check(lib.basp_ckpt_reshard_s2h(plan.handle, *a, m.stream(stream)), "basp_ckpt_reshard_s2h")
 
 
 def basp_layer_bwd_ckpt(plan, ckpt, lse_shards, do_seq, dq_seq, dk_seq, dv_seq, workspace, softmax_scale=0.0, stream=None):
     """basp_layer_bwd_seq from the 8-bit checkpoints (workspace: basp_layer_bwd_seq_workspace_bytes)."""
     m = _Marshal()
     q, k = _qk(plan)
-    (lse,) = m.tables(torch.float32, ("lse_shards", lse_shards, (plan.Bl * plan.Hq_l * plan.S,) * plan.N))
-    t = m.tables(torch.bfloat16, ("do_seq", do_seq, q), ("dq_seq", dq_seq, q), ("dk_seq", dk_seq, k), ("dv_seq", dv_seq, k))
-    _check(lib.basp_layer_bwd_ckpt(plan.handle, _ckpt(plan, m, ckpt), lse, *t, *m.space(workspace), softmax_scale,
-                                   m.stream(stream)), "basp_layer_bwd_ckpt")
+    a = m.addresses(("ckpt", _U8, ckpt, _ckpt_sizes(plan)),
+                    ("lse_shards", _F32, lse_shards, (plan.Bl * plan.Hq_l * plan.S,) * plan.N), ("do_seq", _BF16, do_seq, q),
+                    ("dq_seq", _BF16, dq_seq, q), ("dk_seq", _BF16, dk_seq, k), ("dv_seq", _BF16, dv_seq, k))
+    _check(lib.basp_layer_bwd_ckpt(plan.handle, *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_layer_bwd_ckpt")
 
 
 def basp_lm_loss_fwd_workspace_bytes(plan, vocab) -> int:
@@ -582,11 +576,10 @@ def basp_lm_loss_fwd(plan, hidden, vocab, x_seq, w, labels, loss_seq, lse_seq, w
     """Per-token cross entropy of softmax(x W^T) against `labels` (int64; outside [0, vocab): no loss) and the log-sum-exp
     (lse_seq may be None), fp32."""
     m, n = _Marshal(), _per_rank(plan, 1)
-    (x,) = m.tables(torch.bfloat16, ("x_seq", x_seq, _per_rank(plan, hidden)))
-    (y,) = m.tables(torch.int64, ("labels", labels, n))
-    loss, lse = m.tables(torch.float32, ("loss_seq", loss_seq, n), ("lse_seq", lse_seq, n))
-    _check(lib.basp_lm_loss_fwd(plan.handle, int(hidden), int(vocab), x, m.address(w, torch.bfloat16, vocab * hidden, "w"), y,
-                                loss, lse, *m.space(workspace), m.stream(stream)), "basp_lm_loss_fwd")
+    a = m.addresses(("x_seq", _BF16, x_seq, _per_rank(plan, hidden)), ("w", _BF16, w, vocab * hidden), ("labels", _I64, labels, n),
+                    ("loss_seq", _F32, loss_seq, n), ("lse_seq", _F32, lse_seq, n))
+    _check(lib.basp_lm_loss_fwd(plan.handle, int(hidden), int(vocab), *a, *m.space(workspace), m.stream(stream)),
+           "basp_lm_loss_fwd")
 
 
 def basp_lm_loss_grad(plan, hidden, vocab, x_seq, w, labels, token_weights, loss_seq, lse_seq, dx_seq, dw, workspace,
@@ -594,12 +587,11 @@ def basp_lm_loss_grad(plan, hidden, vocab, x_seq, w, labels, token_weights, loss
     """basp_lm_loss_fwd together with the gradients of sum(token_weights * loss): dx_seq and dw, bf16 (token_weights: fp32
     shards, or None for 1 each; dx_seq or dw None: not wanted)."""
     m, n, wide = _Marshal(), _per_rank(plan, 1), _per_rank(plan, hidden)
-    x, dx = m.tables(torch.bfloat16, ("x_seq", x_seq, wide), ("dx_seq", dx_seq, wide))
-    (y,) = m.tables(torch.int64, ("labels", labels, n))
-    g, loss, lse = m.tables(torch.float32, ("token_weights", token_weights, n), ("loss_seq", loss_seq, n), ("lse_seq", lse_seq, n))
-    _check(lib.basp_lm_loss_grad(plan.handle, int(hidden), int(vocab), x, m.address(w, torch.bfloat16, vocab * hidden, "w"), y, g,
-                                 loss, lse, dx, m.address(dw, torch.bfloat16, vocab * hidden, "dw"), int(piece_rows),
-                                 *m.space(workspace), m.stream(stream)), "basp_lm_loss_grad")
+    a = m.addresses(("x_seq", _BF16, x_seq, wide), ("w", _BF16, w, vocab * hidden), ("labels", _I64, labels, n),
+                    ("token_weights", _F32, token_weights, n), ("loss_seq", _F32, loss_seq, n), ("lse_seq", _F32, lse_seq, n),
+                    ("dx_seq", _BF16, dx_seq, wide), ("dw", _BF16, dw, vocab * hidden))
+    _check(lib.basp_lm_loss_grad(plan.handle, int(hidden), int(vocab), *a, int(piece_rows), *m.space(workspace), m.stream(stream)),
+           "basp_lm_loss_grad")
 
 
 def basp_selftest_wait_timeout(limit_us: int, stream=None):

@@ -1,4 +1,4 @@
-"""Build libbasp.so (sm_100a) in-tree with nvcc.  `python -m paper_2609_03151_b200.build`."""
+"""Build libbasp.so (sm_100a) in-tree with nvcc, and the binding's _marshal.so with g++.  `python -m paper_2609_03151_b200.build`."""
 from __future__ import annotations
 
 import os
@@ -9,6 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libbasp.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 SOURCES = ["plan.cpp", "status.cu", "reshard.cu", "attn_fwd.cu", "attn_bwd.cu", "proj_gemm.cu", "layer.cu", "layer_static.cu",
            "norm_rope.cu", "ckpt.cu", "lm_loss.cu"]
 
@@ -24,7 +25,7 @@ def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "basp.h"), __file__]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != "marshal.cpp"] + [os.path.join(ROOT, "include", "basp.h"), __file__]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -41,5 +42,24 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build_marshal(force: bool = False) -> str:
+    """The Python module that looks at a call's tensors (csrc/marshal.cpp)."""
+    src = os.path.join(CSRC, "marshal.cpp")
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(os.path.getmtime(src), os.path.getmtime(__file__)):
+        return MARSHAL
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+                           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(root, "include"),
+                           "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-o", MARSHAL, src,
+                           "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+                           "-Wl,-rpath," + os.path.join(root, "lib")])
+    return MARSHAL
+
+
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_marshal(force="--force" in sys.argv))
