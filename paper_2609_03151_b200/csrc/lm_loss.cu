@@ -731,9 +731,10 @@ struct Sizes {
     size_t pitch;
 };
 
-// Per 128 x 256 x 64 products a single CTA's tile fetches 48 KiB from L2, a pair's 24 KiB; under the power limit that is time.  A
-// pair's tile wants its 512 rows.
-bool use_pair(int rows) { return rows > 2 * kBM; }
+// A pair's tile takes 0.85 of the time of four single CTAs' tiles (1024 rows of 4096 against 128256 words: 855 and 894 us; 512:
+// 406 and 472; under the power limit its fewer bytes from L2, 24 instead of 48 KiB per 128 x 256 x 64 products, count for more),
+// but it is 512 rows high: for 320 rows a single CTA's three tiles are faster (359 and 380 us), for 768 its six (705 and 787).
+bool use_pair(int rows) { return 0.85 * 4 * cdiv(rows, kTileM<true>) < cdiv(rows, kTileM<false>); }
 
 // How often the vocabulary is split in dx = dz W: the time of `waves` rounds of tiles over the SMs, a tile costing its K
 // blocks plus a start and an epilogue (8 blocks), plus writing and reading the partial sums.
@@ -802,9 +803,9 @@ Workspace workspace_of(const Sizes &z, int hidden, int vocab, bool grad) {
     return w;
 }
 
-// 8192 rows of 4096: 6.83 / 6.31 / 6.14 / 5.98 / 6.26 ms with 1 / 2 / 4 / 8 / 16 row tiles (4 MiB each) in a group
+// 8192 rows of 4096 features: 6.83 / 6.31 / 6.14 / 5.98 / 6.26 ms with 1 / 2 / 4 / 8 / 16 row tiles (4 MiB each) in a group
 constexpr long long kGroupBytes = 34 << 20;
-constexpr int kPairBlocks = 8;
+constexpr int kPairBlocks = 8;                     // 128 rows (2 blocks of K): 609 us with single CTAs, 673 with pairs; 512 rows: alike
 
 template <int kKind, int R, bool kPair>
 int launch_as(const LossParams<R> &prm, cudaStream_t st) {

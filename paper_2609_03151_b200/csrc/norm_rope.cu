@@ -10,8 +10,8 @@
 //   forward   a lane holds eight features, D/8 lanes a vector, a warp 32 / (D/8) neighbouring heads of one token (of 512 bytes at
 //             D = 128); the rotation's partner comes by shuffle.  80 registers, three blocks of 256 threads per SM.
 //             2 x 8K tokens, 64 heads of 128: 95 us (5.7 TB/s); with the backward's layout 104 us.
-//   backward  a lane holds eight features and their eight partners, so D/16 lanes (rounded up to a power of two) a vector, no
-//             shuffle but the sums; the groups of lanes hold neighbouring tokens.  126 registers, two blocks per SM.
+//   backward  a lane holds eight features and their eight partners, so D/16 lanes a vector and no shuffle but the sums; the
+//             vectors of a warp are neighbouring tokens.  128 registers, two blocks per SM.
 //             128K tokens, 40 heads of 128: 707 us (5.8 TB/s); with the forward's layout 727 us.
 #include <cuda_bf16.h>
 
@@ -34,7 +34,8 @@ struct HeadSet {               // one of the two tensors (Q or K) of all ranks
     const __nv_bfloat16 *dy[BASP_MAX_RANKS];      // backward only
     __nv_bfloat16 *out[BASP_MAX_RANKS];           // y, or dx
     const __nv_bfloat16 *w;
-    uint32_t heads, chunks;    // heads per token, chunks of heads
+    uint32_t heads, chunks;    // heads per token, work items per token tile
+    uint32_t chunk_heads;      // heads per work item
     uint32_t items;            // token tiles of all ranks x chunks
 };
 
@@ -44,7 +45,7 @@ struct NormRopeParams {
     float *partial;            // backward: [blocks][D] sums of dw
     float eps, inv_D;
     int D, S, T, T_last, K, Bl;
-    uint32_t tiles, tile_tokens, chunk_heads;      // token tiles per rank and their tokens; heads per work item
+    uint32_t tiles, tile_tokens;   // token tiles per rank and their tokens
     int q_blocks;              // blocks that work on the first tensor (the others on the second)
 };
 
@@ -80,7 +81,7 @@ __device__ __forceinline__ float sum2(uint64_t v) {
     unpack_f2(v, lo, hi);
     return lo + hi;
 }
-// Sum over the N lanes that hold a vector; `lane`: this one's place among them.  N up to 16, not only powers of two.
+// Sum over the N lanes that hold a vector, in all of them; `lane`: this one's place among them.  N up to 16, not only powers of two.
 template <int N>
 __device__ __forceinline__ float group_sum(float v, int lane) {
     if constexpr ((N & (N - 1)) == 0) {
@@ -89,7 +90,7 @@ __device__ __forceinline__ float group_sum(float v, int lane) {
         return v;
     } else {
 #pragma unroll
-        for (int o = N > 8 ? 8 : 4; o > 0; o >>= 1) {
+        for (int o = N > 8 ? 8 : N > 4 ? 4 : 2; o > 0; o >>= 1) {
             const float far = __shfl_down_sync(0xffffffffu, v, o);
             if (lane + o < N) v += far;
         }
@@ -97,7 +98,7 @@ __device__ __forceinline__ float group_sum(float v, int lane) {
     }
 }
 
-// A work item: up to chunk_heads heads of a tile of neighbouring tokens of one rank.  The blocks of a tensor take its items in turn,
+// A work item: some heads of a tile of neighbouring tokens of one rank.  The blocks of a tensor take its items in turn,
 // so that at any time they read and write neighbouring memory.
 struct Share {
     int which;
@@ -121,8 +122,8 @@ struct Place {
 };
 __device__ __forceinline__ Place place_of(const NormRopeParams &p, const HeadSet &t, uint32_t item, uint32_t token) {
     Place o;
-    const uint32_t tile = item / t.chunks, head = (item - tile * t.chunks) * p.chunk_heads;
-    o.count = (int)min(p.chunk_heads, t.heads - head);
+    const uint32_t tile = item / t.chunks, head = (item - tile * t.chunks) * t.chunk_heads;
+    o.count = (int)min(t.chunk_heads, t.heads - head);
     o.rank = tile / p.tiles;
     const uint32_t row = (tile - o.rank * p.tiles) * p.tile_tokens + token, l = o.rank % p.K;
     const uint32_t Tr = (int)l == p.K - 1 ? p.T_last : p.T;
@@ -208,22 +209,24 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) norm_rope_kernel(const _
     }
 }
 
-// Backward: L lanes hold a vector (those past D/16 idle).  A block keeps the dw sums of its features in registers, at the end adds
-// its groups together in shared memory and writes one partial row, in a fixed order (the result does not depend on timing).
-template <int L>
+// Backward: N = D / 16 lanes hold a vector, the vectors of a warp are one head of 32 / N neighbouring tokens.  A block keeps the dw sums
+// of its features in registers, at the end adds its vectors together in shared memory and writes one partial row, in a fixed order
+// (the result does not depend on timing).
+template <int N>
 __global__ void __launch_bounds__(kThreads, kBwdBlocks) norm_rope_bwd_kernel(const __grid_constant__ NormRopeParams p) {
-    constexpr int kUnroll = kBwdUnroll;
-    __shared__ float part[kWarps][128];
-    const int lane = threadIdx.x % L, half = p.D / 2;
+    constexpr int kUnroll = kBwdUnroll, kVectors = 32 / N, half = 8 * N;
+    __shared__ float part[kWarps * kVectors][16 * N];
+    const int warp_lane = threadIdx.x & 31, vec = warp_lane / N, lane = warp_lane - vec * N;
     const Share share = share_of(p);
     const HeadSet &t = p.t[share.which];
-    const bool mine = lane * 16 < p.D;
+    const bool mine = vec < kVectors;
+    const uint32_t token = threadIdx.x / 32 * kVectors + vec;
     allow_next_kernel();
     const uint64_t minus = pack_f2(-1.f, -1.f);
     F8 wl{}, wh{}, gl{}, gh{};
     if (mine) { wl = widen(ld16(t.w + 8 * lane)); wh = widen(ld16(t.w + half + 8 * lane)); }
     for (uint32_t item = share.item; item < share.end; item += share.step) {
-        const Place at = place_of(p, t, item, threadIdx.x / L);
+        const Place at = place_of(p, t, item, token);
         const bool active = at.valid && mine;
         const __nv_bfloat16 *x = t.x[at.rank] + at.off + 8 * lane, *dy = t.dy[at.rank] + at.off + 8 * lane;
         __nv_bfloat16 *dx = t.out[at.rank] + at.off + 8 * lane;
@@ -256,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) norm_rope_bwd_kernel(con
                     sq = fma2(xl.p[e], xl.p[e], fma2(xh.p[e], xh.p[e], sq));
                     dot = fma2(xl.p[e], mul2(l, wl.p[e]), fma2(xh.p[e], mul2(g, wh.p[e]), dot));
                 }
-                const float s1 = group_sum<L>(sum2(sq), lane), s2 = group_sum<L>(sum2(dot), lane);
+                const float s1 = group_sum<N>(sum2(sq), lane), s2 = group_sum<N>(sum2(dot), lane);
                 const float r = rsqrtf(fmaf(s1, p.inv_D, p.eps));
                 if (!active || h + u >= at.count) continue;
                 const float k = -r * r * r * s2 * p.inv_D;
@@ -275,29 +278,19 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) norm_rope_bwd_kernel(con
             }
         }
     }
-    float sums[2][8];
+    if (mine) {
+        float *dst = part[token] + 8 * lane;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { unpack_f2(gl.p[e], sums[0][2 * e], sums[0][2 * e + 1]); unpack_f2(gh.p[e], sums[1][2 * e], sums[1][2 * e + 1]); }
-    // groups of a warp, then the warps
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int o = 16; o >= L; o >>= 1) {
-            sums[0][e] += __shfl_xor_sync(0xffffffffu, sums[0][e], o);
-            sums[1][e] += __shfl_xor_sync(0xffffffffu, sums[1][e], o);
-        }
-    if (threadIdx.x % 32 < L && mine) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            part[threadIdx.x / 32][8 * lane + e] = sums[0][e];
-            part[threadIdx.x / 32][half + 8 * lane + e] = sums[1][e];
+        for (int e = 0; e < 4; ++e) {
+            unpack_f2(gl.p[e], dst[2 * e], dst[2 * e + 1]);
+            unpack_f2(gh.p[e], dst[half + 2 * e], dst[half + 2 * e + 1]);
         }
     }
     __syncthreads();
-    if ((int)threadIdx.x < p.D) {
+    if (threadIdx.x < 16 * N) {
         float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) s += part[w][threadIdx.x];
+#pragma unroll 16
+        for (int k = 0; k < kWarps * kVectors; ++k) s += part[k][threadIdx.x];
         p.partial[(size_t)blockIdx.x * p.D + threadIdx.x] = s;
     }
 }
@@ -319,10 +312,10 @@ __global__ void __launch_bounds__(256) dw_kernel(const float *partial, int D, in
     }
 }
 
-// What both directions share: supported sizes, the geometry and the split of the work into items of tile_tokens tokens and
-// chunk_heads heads (a multiple of `batch`, the heads that a warp has in flight).
+// What both directions share: the geometry and the split of the work over one wave of blocks, in items of tile_tokens tokens and some
+// of their heads (`batch`: the heads of a token that are in flight).
 int fill(const basp_plan *p, const void *w_q, const void *w_k, const float *cos, const float *sin, float eps, int tile_tokens,
-         int batch, int items_per_block, int wave, NormRopeParams *prm, int *blocks) {
+         int batch, int wave, NormRopeParams *prm, int *blocks) {
     const long long rows = (long long)p->Bl * p->T, tiles = (rows + tile_tokens - 1) / tile_tokens;
     if (tiles * tile_tokens >= (1ll << 31) || tiles * p->N * p->Hq >= (1ll << 31)) return BASP_ERR_UNSUPPORTED;     // 31-bit rows, items
     prm->cos = cos; prm->sin = sin; prm->eps = eps; prm->inv_D = 1.0f / (float)p->D;
@@ -330,23 +323,27 @@ int fill(const basp_plan *p, const void *w_q, const void *w_k, const float *cos,
     prm->tiles = (uint32_t)tiles; prm->tile_tokens = (uint32_t)tile_tokens;
     prm->t[0].w = (const __nv_bfloat16 *)w_q; prm->t[0].heads = p->Hq;
     prm->t[1].w = (const __nv_bfloat16 *)w_k; prm->t[1].heads = p->Hkv;
-    // A token's heads together where there are many tokens; with fewer the heads are spread over more items, so that a block has
-    // several and the last round of them is short
-    const long long per = tiles * p->N * (p->Hq + p->Hkv) / ((long long)items_per_block * wave);
-    prm->chunk_heads = (uint32_t)(per < batch ? batch : per / batch * batch);
-    if (prm->chunk_heads > (uint32_t)p->Hq) prm->chunk_heads = p->Hq;
+    // blocks in proportion to the heads, at least one per tensor
+    const long long units = tiles * p->N;
+    int q = (wave * p->Hq + (p->Hq + p->Hkv) / 2) / (p->Hq + p->Hkv);
+    q = q < 1 ? 1 : (q > wave - 1 ? wave - 1 : q);
     for (HeadSet &t : prm->t) {
-        t.chunks = (t.heads + prm->chunk_heads - 1) / prm->chunk_heads;
-        t.items = (uint32_t)(tiles * p->N * t.chunks);
+        // A tile's heads in n items: few, and a token's cos and sin are fetched for more of them; many, and the last round of items
+        // over the blocks is short.  An item costs its batches of heads and a start of three quarters of a batch
+        const int blocks_of = &t == &prm->t[0] ? q : wave - q;
+        double best = 1e30;
+        for (uint32_t n = 1; n <= t.heads && n <= 32; ++n) {
+            const uint32_t heads = (t.heads + n - 1) / n;
+            const double cost = (double)((units * n + blocks_of - 1) / blocks_of) * ((heads + batch - 1) / batch + 0.75);
+            if (cost < best) { best = cost; t.chunk_heads = heads; }
+        }
+        t.chunks = (t.heads + t.chunk_heads - 1) / t.chunk_heads;
+        t.items = (uint32_t)(units * t.chunks);
     }
-    // blocks in proportion to the heads, at least one per tensor, none without an item
-    const long long all = (long long)prm->t[0].items + prm->t[1].items, total = all < wave ? all : wave;
-    long long q = (total * p->Hq + (p->Hq + p->Hkv) / 2) / (p->Hq + p->Hkv);
-    if (total - q > prm->t[1].items) q = total - prm->t[1].items;
-    if (q > prm->t[0].items) q = prm->t[0].items;
-    q = q < 1 ? 1 : (q > total - 1 ? total - 1 : q);
-    prm->q_blocks = (int)q;
-    *blocks = (int)total;
+    if (q > (int)prm->t[0].items) q = (int)prm->t[0].items;                      // no block without an item
+    const int k = wave - q < (int)prm->t[1].items ? wave - q : (int)prm->t[1].items;
+    prm->q_blocks = q;
+    *blocks = q + k;
     return BASP_OK;
 }
 
@@ -383,12 +380,6 @@ int dispatch(int n, F &&f) {
     return rc;
 }
 
-int bwd_lanes(int D) {
-    int l = 1;
-    while (l * 16 < D) l *= 2;
-    return l;
-}
-
 }  // namespace
 
 extern "C" int basp_qk_norm_rope(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *w_q,
@@ -398,7 +389,7 @@ extern "C" int basp_qk_norm_rope(const basp_plan *p, const void *const *q_seq, c
     NormRopeParams prm;
     int blocks = 0;
     BASP_TRY(supported(p, eps));
-    BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kWarps, kFwdUnroll * (32 / (p->D / 8)), 8, 148 * kFwdBlocks, &prm, &blocks));
+    BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kWarps, kFwdUnroll * (32 / (p->D / 8)), 148 * kFwdBlocks, &prm, &blocks));
     SpanSet spans;
     BASP_TRY(add_tables(p, &spans, w_q, w_k, rope_cos, rope_sin));
     BASP_TRY(add_shards(p, &spans, p->Hq, q_seq, false, 0, prm.t[0].x));
@@ -427,7 +418,7 @@ extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_se
     NormRopeParams prm;
     int blocks = 0;
     BASP_TRY(supported(p, eps));
-    BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kThreads / bwd_lanes(p->D), kBwdUnroll, 4, 148 * kBwdBlocks, &prm, &blocks));
+    BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kWarps * (32 / (p->D / 16)), kBwdUnroll, 148 * kBwdBlocks, &prm, &blocks));
     SpanSet spans;
     BASP_TRY(add_tables(p, &spans, w_q, w_k, rope_cos, rope_sin));
     BASP_TRY(add_shards(p, &spans, p->Hq, q_seq, false, -1, prm.t[0].x));
@@ -442,7 +433,7 @@ extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_se
     if (workspace_bytes < basp_qk_norm_rope_bwd_workspace_bytes(p)) return BASP_ERR_WORKSPACE;
     BASP_TRY(spans.overlaps());
     prm.partial = (float *)workspace;
-    return dispatch<1, 2, 4, 8>(bwd_lanes(p->D), [&](auto lanes) -> int {
+    return dispatch<1, 2, 3, 4, 5, 6, 7, 8>(p->D / 16, [&](auto lanes) -> int {
         norm_rope_bwd_kernel<decltype(lanes)::value><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(prm);
         BASP_CUDA_TRY(cudaGetLastError());
         BASP_CUDA_TRY(launch_early(dw_kernel, dim3(p->D / 8, 2), 256, (cudaStream_t)stream, (const float *)prm.partial, p->D, prm.q_blocks,

@@ -120,7 +120,7 @@ def test_loss_and_gradients(basp, w, hidden, vocab):
     assert torch.equal(cat(loss), cat(got[0]))
 
 
-@pytest.mark.parametrize("piece_rows", [1, 256, 384])
+@pytest.mark.parametrize("piece_rows", [1, 256, 384, 512])
 def test_pieces(basp, piece_rows):
     w, hidden, vocab = L("pieces", 4, 2, 500, 320, 1111)
     pl = make_plan(basp, w)
