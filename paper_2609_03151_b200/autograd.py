@@ -21,6 +21,7 @@ The operations run on the current stream with the tensors' device current, and m
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -104,6 +105,7 @@ class _QkNormRope(torch.autograd.Function):
         return tuple(out)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, *d_out):
         plan, n = ctx.plan, ctx.plan.N
         cos, sin, w_q, w_k, *shards = ctx.saved_tensors
@@ -151,6 +153,7 @@ class _LmLoss(torch.autograd.Function):
         return every.sum()
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_loss):
         saved = list(ctx.saved_tensors)
         want_w, want_x = ctx.want

@@ -575,10 +575,10 @@ def basp_lm_loss_grad_workspace_bytes(plan, hidden, vocab, piece_rows=0) -> int:
 def basp_lm_loss_fwd(plan, hidden, vocab, x_seq, w, labels, loss_seq, lse_seq, workspace, stream=None):
     """Per-token cross entropy of softmax(x W^T) against `labels` (int64; outside [0, vocab): no loss) and the log-sum-exp
     (lse_seq may be None), fp32."""
-    m, n = _Marshal(), _per_rank(plan, 1)
+    m, n, hidden, vocab = _Marshal(), _per_rank(plan, 1), int(hidden), int(vocab)
     a = m.addresses(("x_seq", _BF16, x_seq, _per_rank(plan, hidden)), ("w", _BF16, w, vocab * hidden), ("labels", _I64, labels, n),
                     ("loss_seq", _F32, loss_seq, n), ("lse_seq", _F32, lse_seq, n))
-    _check(lib.basp_lm_loss_fwd(plan.handle, int(hidden), int(vocab), *a, *m.space(workspace), m.stream(stream)),
+    _check(lib.basp_lm_loss_fwd(plan.handle, hidden, vocab, *a, *m.space(workspace), m.stream(stream)),
            "basp_lm_loss_fwd")
 
 
@@ -586,11 +586,12 @@ def basp_lm_loss_grad(plan, hidden, vocab, x_seq, w, labels, token_weights, loss
                       piece_rows=0, stream=None):
     """basp_lm_loss_fwd together with the gradients of sum(token_weights * loss): dx_seq and dw, bf16 (token_weights: fp32
     shards, or None for 1 each; dx_seq or dw None: not wanted)."""
-    m, n, wide = _Marshal(), _per_rank(plan, 1), _per_rank(plan, hidden)
+    m, n, hidden, vocab = _Marshal(), _per_rank(plan, 1), int(hidden), int(vocab)
+    wide = _per_rank(plan, hidden)
     a = m.addresses(("x_seq", _BF16, x_seq, wide), ("w", _BF16, w, vocab * hidden), ("labels", _I64, labels, n),
                     ("token_weights", _F32, token_weights, n), ("loss_seq", _F32, loss_seq, n), ("lse_seq", _F32, lse_seq, n),
                     ("dx_seq", _BF16, dx_seq, wide), ("dw", _BF16, dw, vocab * hidden))
-    _check(lib.basp_lm_loss_grad(plan.handle, int(hidden), int(vocab), *a, int(piece_rows), *m.space(workspace), m.stream(stream)),
+    _check(lib.basp_lm_loss_grad(plan.handle, hidden, vocab, *a, int(piece_rows), *m.space(workspace), m.stream(stream)),
            "basp_lm_loss_grad")
 
 
