@@ -61,9 +61,11 @@ struct CkptTensor {
     FastDiv div_row, div_run;
 };
 
+// R: room for ranks (8 or BASP_MAX_RANKS; a launch takes longer the larger its parameters)
+template <int R>
 struct CkptParams {
-    char *ckpt[BASP_MAX_RANKS];
-    const char *wide[kTensors][BASP_MAX_RANKS];   // bf16 shards: sequence side (pack), head side (way back)
+    char *ckpt[R];
+    const char *wide[kTensors][R];            // bf16 shards: sequence side (pack), head side (way back)
     CkptTensor t[kTensors];
     uint32_t K, T, T_last, S, Bl, D, vec_u;       // vec_u: units per head vector = D / 16
     FastDiv div_T, div_T_last, div_vec;
@@ -74,7 +76,8 @@ struct Where {
     uint32_t rank, chunk, local;
     bool last;
 };
-__device__ __forceinline__ Where where(const CkptParams &p) {
+template <int R>
+__device__ __forceinline__ Where where(const CkptParams<R> &p) {
     Where w;
     uint32_t c = blockIdx.x;
     w.tensor = 0;
@@ -89,8 +92,8 @@ __device__ __forceinline__ Where where(const CkptParams &p) {
 }
 
 // kL lanes hold one head vector, 16 elements each (lanes past D/16 idle).
-template <int kL, bool kWide>
-__global__ void __launch_bounds__(kThreads) ckpt_pack_kernel(const __grid_constant__ CkptParams p) {
+template <int kL, bool kWide, int R>
+__global__ void __launch_bounds__(kThreads) ckpt_pack_kernel(const __grid_constant__ CkptParams<R> p) {
     constexpr uint32_t kGroups = kThreads / kL;
     const Where at = where(p);
     const CkptTensor &t = p.t[at.tensor];
@@ -144,8 +147,8 @@ __global__ void __launch_bounds__(kThreads) ckpt_pack_kernel(const __grid_consta
 }
 
 // The way back: walk the codes in memory order, write every run of a token's heads to the rank that owns them.
-template <bool kWide>
-__global__ void __launch_bounds__(kThreads) ckpt_to_heads_kernel(const __grid_constant__ CkptParams p) {
+template <bool kWide, int R>
+__global__ void __launch_bounds__(kThreads) ckpt_to_heads_kernel(const __grid_constant__ CkptParams<R> p) {
     const Where at = where(p);
     const CkptTensor &t = p.t[at.tensor];
     const uint32_t Tr = at.last ? p.T_last : p.T;
@@ -211,7 +214,8 @@ size_t layout(const basp_plan *p, int tokens, uint64_t (&codes)[kTensors], uint6
 }
 
 // Geometry, chunks and spans of either direction; `units_per_chunk` in head vectors (pack) or units (way back).
-int fill(const basp_plan *p, const void *const *ckpt, const void *const *const (&wide)[kTensors], bool pack, CkptParams *prm,
+template <int R>
+int fill(const basp_plan *p, const void *const *ckpt, const void *const *const (&wide)[kTensors], bool pack, CkptParams<R> *prm,
          SpanSet *spans, uint32_t *blocks) {
     if (p->D % 16 != 0 || p->D > 128) return BASP_ERR_UNSUPPORTED;
     if (!ckpt) return BASP_ERR_NULL;
@@ -260,17 +264,47 @@ int fill(const basp_plan *p, const void *const *ckpt, const void *const *const (
 }
 
 // 256-bit accesses fault below 32-byte alignment; the interface promises 16.
-bool all_on_32(const basp_plan *p, const CkptParams &prm) {
+template <int R>
+bool all_on_32(const basp_plan *p, const CkptParams<R> &prm) {
     uintptr_t bits = 0;
     for (int i = 0; i < kTensors; ++i)
         for (int r = 0; r < p->N; ++r) bits |= (uintptr_t)prm.wide[i][r];
     return (bits & 31) == 0;
 }
 
-template <int kL>
-void launch_pack(const CkptParams &prm, uint32_t blocks, bool wide, cudaStream_t st) {
-    if (wide) ckpt_pack_kernel<kL, true><<<blocks, kThreads, 0, st>>>(prm);
-    else ckpt_pack_kernel<kL, false><<<blocks, kThreads, 0, st>>>(prm);
+template <int kL, int R>
+void launch_pack(const CkptParams<R> &prm, uint32_t blocks, bool wide, cudaStream_t st) {
+    if (wide) ckpt_pack_kernel<kL, true, R><<<blocks, kThreads, 0, st>>>(prm);
+    else ckpt_pack_kernel<kL, false, R><<<blocks, kThreads, 0, st>>>(prm);
+}
+
+template <int R>
+int run_pack(const basp_plan *p, const void *const *const (&shards)[kTensors], void *const *ckpt_shards, cudaStream_t st) {
+    CkptParams<R> prm;
+    SpanSet spans;
+    uint32_t blocks = 0;
+    BASP_TRY(fill(p, (const void *const *)ckpt_shards, shards, true, &prm, &spans, &blocks));
+    const bool wide = all_on_32(p, prm);
+    if (p->D > 64) launch_pack<8>(prm, blocks, wide, st);
+    else if (p->D > 32) launch_pack<4>(prm, blocks, wide, st);
+    else if (p->D > 16) launch_pack<2>(prm, blocks, wide, st);
+    else launch_pack<1>(prm, blocks, wide, st);
+    BASP_CUDA_TRY(cudaGetLastError());
+    basp_count_launch(1);
+    return BASP_OK;
+}
+
+template <int R>
+int run_to_heads(const basp_plan *p, const void *const *ckpt_shards, const void *const *const (&heads)[kTensors], cudaStream_t st) {
+    CkptParams<R> prm;
+    SpanSet spans;
+    uint32_t blocks = 0;
+    BASP_TRY(fill(p, ckpt_shards, heads, false, &prm, &spans, &blocks));
+    if (all_on_32(p, prm)) ckpt_to_heads_kernel<true, R><<<blocks, kThreads, 0, st>>>(prm);
+    else ckpt_to_heads_kernel<false, R><<<blocks, kThreads, 0, st>>>(prm);
+    BASP_CUDA_TRY(cudaGetLastError());
+    basp_count_launch(1);
+    return BASP_OK;
 }
 
 }  // namespace
@@ -284,33 +318,16 @@ extern "C" size_t basp_ckpt_bytes(const basp_plan *p, int rank) {
 extern "C" int basp_ckpt_pack(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *const *v_seq,
                               const void *const *o_seq, void *const *ckpt_shards, void *stream) {
     if (!p) return BASP_ERR_NULL;
-    CkptParams prm;
-    SpanSet spans;
-    uint32_t blocks = 0;
-    BASP_TRY(fill(p, (const void *const *)ckpt_shards, {q_seq, k_seq, v_seq, o_seq}, true, &prm, &spans, &blocks));
-    const bool wide = all_on_32(p, prm);
-    cudaStream_t st = (cudaStream_t)stream;
-    if (p->D > 64) launch_pack<8>(prm, blocks, wide, st);
-    else if (p->D > 32) launch_pack<4>(prm, blocks, wide, st);
-    else if (p->D > 16) launch_pack<2>(prm, blocks, wide, st);
-    else launch_pack<1>(prm, blocks, wide, st);
-    BASP_CUDA_TRY(cudaGetLastError());
-    basp_count_launch(1);
-    return BASP_OK;
+    const void *const *const shards[kTensors] = {q_seq, k_seq, v_seq, o_seq};
+    return p->N <= 8 ? run_pack<8>(p, shards, ckpt_shards, (cudaStream_t)stream)
+                     : run_pack<BASP_MAX_RANKS>(p, shards, ckpt_shards, (cudaStream_t)stream);
 }
 
 extern "C" int basp_ckpt_reshard_s2h(const basp_plan *p, const void *const *ckpt_shards, void *const *q_head, void *const *k_head,
                                      void *const *v_head, void *const *o_head, void *stream) {
     if (!p) return BASP_ERR_NULL;
-    CkptParams prm;
-    SpanSet spans;
-    uint32_t blocks = 0;
     typedef const void *const *In;
-    BASP_TRY(fill(p, ckpt_shards, {(In)q_head, (In)k_head, (In)v_head, (In)o_head}, false, &prm, &spans, &blocks));
-    cudaStream_t st = (cudaStream_t)stream;
-    if (all_on_32(p, prm)) ckpt_to_heads_kernel<true><<<blocks, kThreads, 0, st>>>(prm);
-    else ckpt_to_heads_kernel<false><<<blocks, kThreads, 0, st>>>(prm);
-    BASP_CUDA_TRY(cudaGetLastError());
-    basp_count_launch(1);
-    return BASP_OK;
+    const In heads[kTensors] = {(In)q_head, (In)k_head, (In)v_head, (In)o_head};
+    return p->N <= 8 ? run_to_heads<8>(p, ckpt_shards, heads, (cudaStream_t)stream)
+                     : run_to_heads<BASP_MAX_RANKS>(p, ckpt_shards, heads, (cudaStream_t)stream);
 }

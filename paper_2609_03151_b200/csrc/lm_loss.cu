@@ -35,6 +35,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "common.cuh"
 #include "ptx.cuh"
 #include "spans.h"
@@ -719,7 +721,7 @@ __global__ void __launch_bounds__(256) lm_dx_join_kernel(const __grid_constant__
 }
 
 // ------------------------------------------------------------------------------------------------ host side
-constexpr int kDefaultPiece = 8192, kMaxPiece = 32768;
+constexpr int kDefaultPiece = 8192, kMaxPiece = 32768, kMaxDevices = 64;
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
 
@@ -809,12 +811,17 @@ constexpr int kPairBlocks = 8;                     // 128 rows (2 blocks of K): 
 
 template <int kKind, int R, bool kPair>
 int launch_as(const LossParams<R> &prm, cudaStream_t st) {
-    int dev = 0, sms = 0;
-    BASP_CUDA_TRY(cudaGetDevice(&dev));
-    BASP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    const long long items = (long long)prm.tiles_m * prm.tiles_n * prm.splits, slots = kPair ? sms / 2 : sms;
     const int smem = kStages * kStageBytes + (kKind == kDw ? 8 * kStagingBytes : 0) + 1024;
-    BASP_CUDA_TRY(cudaFuncSetAttribute(lm_gemm_kernel<kKind, R, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    int dev = 0;
+    BASP_CUDA_TRY(cudaGetDevice(&dev));
+    static std::atomic<int> sm_count[kMaxDevices];         // 0: this kernel has not been set up on the device
+    int sms = dev < kMaxDevices ? sm_count[dev].load(std::memory_order_acquire) : 0;
+    if (sms == 0) {
+        BASP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        BASP_CUDA_TRY(cudaFuncSetAttribute(lm_gemm_kernel<kKind, R, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        if (dev < kMaxDevices) sm_count[dev].store(sms, std::memory_order_release);
+    }
+    const long long items = (long long)prm.tiles_m * prm.tiles_n * prm.splits, slots = kPair ? sms / 2 : sms;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(items < slots ? items : slots) * (kPair ? 2 : 1));
     cfg.blockDim = dim3(kThreads);

@@ -29,18 +29,21 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kFwdBlocks = 3, kBwdBlocks = 2;      // per SM
 constexpr int kFwdUnroll = 4, kBwdUnroll = 2;      // vectors in flight per lane: 64 and 128 bytes
 
+// R: room for ranks (8 or BASP_MAX_RANKS; a launch takes longer the larger its parameters)
+template <int R>
 struct HeadSet {               // one of the two tensors (Q or K) of all ranks
-    const __nv_bfloat16 *x[BASP_MAX_RANKS];
-    const __nv_bfloat16 *dy[BASP_MAX_RANKS];      // backward only
-    __nv_bfloat16 *out[BASP_MAX_RANKS];           // y, or dx
+    const __nv_bfloat16 *x[R];
+    const __nv_bfloat16 *dy[R];                   // backward only
+    __nv_bfloat16 *out[R];                        // y, or dx
     const __nv_bfloat16 *w;
     uint32_t heads, chunks;    // heads per token, work items per token tile
     uint32_t chunk_heads;      // heads per work item
     uint32_t items;            // token tiles of all ranks x chunks
 };
 
+template <int R>
 struct NormRopeParams {
-    HeadSet t[2];
+    HeadSet<R> t[2];
     const float *cos, *sin;    // [D/2][S]
     float *partial;            // backward: [blocks][D] sums of dw
     float eps, inv_D;
@@ -104,7 +107,8 @@ struct Share {
     int which;
     uint32_t item, end, step;
 };
-__device__ __forceinline__ Share share_of(const NormRopeParams &p) {
+template <int R>
+__device__ __forceinline__ Share share_of(const NormRopeParams<R> &p) {
     Share o;
     o.which = (int)blockIdx.x >= p.q_blocks;
     o.item = o.which ? blockIdx.x - p.q_blocks : blockIdx.x;
@@ -120,7 +124,8 @@ struct Place {
     size_t off;                // the token's first element of the first of the heads in the rank's shard
     bool valid;                // the rank has such a token
 };
-__device__ __forceinline__ Place place_of(const NormRopeParams &p, const HeadSet &t, uint32_t item, uint32_t token) {
+template <int R>
+__device__ __forceinline__ Place place_of(const NormRopeParams<R> &p, const HeadSet<R> &t, uint32_t item, uint32_t token) {
     Place o;
     const uint32_t tile = item / t.chunks, head = (item - tile * t.chunks) * t.chunk_heads;
     o.count = (int)min(t.chunk_heads, t.heads - head);
@@ -155,14 +160,14 @@ __device__ __forceinline__ uint4 partner(const uint4 &v, int src) {
 }
 
 // N = D / 8 lanes hold a vector, a warp 32 / N neighbouring heads of its token.
-template <int N>
-__global__ void __launch_bounds__(kThreads, kFwdBlocks) norm_rope_kernel(const __grid_constant__ NormRopeParams p) {
+template <int N, int R>
+__global__ void __launch_bounds__(kThreads, kFwdBlocks) norm_rope_kernel(const __grid_constant__ NormRopeParams<R> p) {
     constexpr int kUnroll = kFwdUnroll, kVectors = 32 / N;
     const int warp_lane = threadIdx.x & 31, vec = warp_lane / N, lane = warp_lane - vec * N;
     const bool low = lane < N / 2, mine = vec < kVectors;
     const int other = low ? lane + N / 2 : lane - N / 2, src = vec * N + other;
     const Share share = share_of(p);
-    const HeadSet &t = p.t[share.which];
+    const HeadSet<R> &t = p.t[share.which];
     for (uint32_t item = share.item; item < share.end; item += share.step) {
         const Place at = place_of(p, t, item, threadIdx.x / 32);
         if (!at.valid) continue;
@@ -212,13 +217,13 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) norm_rope_kernel(const _
 // Backward: N = D / 16 lanes hold a vector, the vectors of a warp are one head of 32 / N neighbouring tokens.  A block keeps the dw sums
 // of its features in registers, at the end adds its vectors together in shared memory and writes one partial row, in a fixed order
 // (the result does not depend on timing).
-template <int N>
-__global__ void __launch_bounds__(kThreads, kBwdBlocks) norm_rope_bwd_kernel(const __grid_constant__ NormRopeParams p) {
+template <int N, int R>
+__global__ void __launch_bounds__(kThreads, kBwdBlocks) norm_rope_bwd_kernel(const __grid_constant__ NormRopeParams<R> p) {
     constexpr int kUnroll = kBwdUnroll, kVectors = 32 / N, half = 8 * N;
     __shared__ float part[kWarps * kVectors][16 * N];
     const int warp_lane = threadIdx.x & 31, vec = warp_lane / N, lane = warp_lane - vec * N;
     const Share share = share_of(p);
-    const HeadSet &t = p.t[share.which];
+    const HeadSet<R> &t = p.t[share.which];
     const bool mine = vec < kVectors;
     const uint32_t token = threadIdx.x / 32 * kVectors + vec;
     allow_next_kernel();
@@ -314,8 +319,9 @@ __global__ void __launch_bounds__(256) dw_kernel(const float *partial, int D, in
 
 // What both directions share: the geometry and the split of the work over one wave of blocks, in items of tile_tokens tokens and some
 // of their heads (`batch`: the heads of a token that are in flight).
+template <int R>
 int fill(const basp_plan *p, const void *w_q, const void *w_k, const float *cos, const float *sin, float eps, int tile_tokens,
-         int batch, int wave, NormRopeParams *prm, int *blocks) {
+         int batch, int wave, NormRopeParams<R> *prm, int *blocks) {
     const long long rows = (long long)p->Bl * p->T, tiles = (rows + tile_tokens - 1) / tile_tokens;
     if (tiles * tile_tokens >= (1ll << 31) || tiles * p->N * p->Hq >= (1ll << 31)) return BASP_ERR_UNSUPPORTED;     // 31-bit rows, items
     prm->cos = cos; prm->sin = sin; prm->eps = eps; prm->inv_D = 1.0f / (float)p->D;
@@ -327,7 +333,7 @@ int fill(const basp_plan *p, const void *w_q, const void *w_k, const float *cos,
     const long long units = tiles * p->N;
     int q = (wave * p->Hq + (p->Hq + p->Hkv) / 2) / (p->Hq + p->Hkv);
     q = q < 1 ? 1 : (q > wave - 1 ? wave - 1 : q);
-    for (HeadSet &t : prm->t) {
+    for (HeadSet<R> &t : prm->t) {
         // A tile's heads in n items: few, and a token's cos and sin are fetched for more of them; many, and the last round of items
         // over the blocks is short.  An item costs its batches of heads and a start of three quarters of a batch
         const int blocks_of = &t == &prm->t[0] ? q : wave - q;
@@ -380,15 +386,11 @@ int dispatch(int n, F &&f) {
     return rc;
 }
 
-}  // namespace
-
-extern "C" int basp_qk_norm_rope(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *w_q,
-                                 const void *w_k, const float *rope_cos, const float *rope_sin, float eps, void *const *q_out,
-                                 void *const *k_out, void *stream) {
-    if (!p) return BASP_ERR_NULL;
-    NormRopeParams prm;
+template <int R>
+int run_fwd(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *w_q, const void *w_k,
+            const float *rope_cos, const float *rope_sin, float eps, void *const *q_out, void *const *k_out, void *stream) {
+    NormRopeParams<R> prm;
     int blocks = 0;
-    BASP_TRY(supported(p, eps));
     BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kWarps, kFwdUnroll * (32 / (p->D / 8)), 148 * kFwdBlocks, &prm, &blocks));
     SpanSet spans;
     BASP_TRY(add_tables(p, &spans, w_q, w_k, rope_cos, rope_sin));
@@ -398,26 +400,22 @@ extern "C" int basp_qk_norm_rope(const basp_plan *p, const void *const *q_seq, c
     BASP_TRY(add_shards(p, &spans, p->Hkv, k_out, true, 1, const_cast<const __nv_bfloat16 **>(prm.t[1].out)));
     BASP_TRY(spans.overlaps());
     return dispatch<2, 4, 6, 8, 10, 12, 14, 16>(p->D / 8, [&](auto lanes) -> int {
-        norm_rope_kernel<decltype(lanes)::value><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(prm);
+        norm_rope_kernel<decltype(lanes)::value, R><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(prm);
         BASP_CUDA_TRY(cudaGetLastError());
         basp_count_launch(1);
         return BASP_OK;
     });
 }
 
-extern "C" size_t basp_qk_norm_rope_bwd_workspace_bytes(const basp_plan *p) {
-    return p ? (size_t)148 * kBwdBlocks * p->D * 4 : 0;
-}
+size_t bwd_workspace_bytes(const basp_plan *p) { return (size_t)148 * kBwdBlocks * p->D * 4; }
 
-extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *w_q,
-                                     const void *w_k, const float *rope_cos, const float *rope_sin, float eps,
-                                     const void *const *dq_out, const void *const *dk_out, void *const *dq_seq,
-                                     void *const *dk_seq, float *dw_q, float *dw_k, void *workspace, size_t workspace_bytes,
-                                     void *stream) {
-    if (!p) return BASP_ERR_NULL;
-    NormRopeParams prm;
+template <int R>
+int run_bwd(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *w_q, const void *w_k,
+            const float *rope_cos, const float *rope_sin, float eps, const void *const *dq_out, const void *const *dk_out,
+            void *const *dq_seq, void *const *dk_seq, float *dw_q, float *dw_k, void *workspace, size_t workspace_bytes,
+            void *stream) {
+    NormRopeParams<R> prm;
     int blocks = 0;
-    BASP_TRY(supported(p, eps));
     BASP_TRY(fill(p, w_q, w_k, rope_cos, rope_sin, eps, kWarps * (32 / (p->D / 16)), kBwdUnroll, 148 * kBwdBlocks, &prm, &blocks));
     SpanSet spans;
     BASP_TRY(add_tables(p, &spans, w_q, w_k, rope_cos, rope_sin));
@@ -429,16 +427,42 @@ extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_se
     BASP_TRY(add_shards(p, &spans, p->Hkv, dk_seq, true, 1, const_cast<const __nv_bfloat16 **>(prm.t[1].out)));
     BASP_TRY(spans.add_out(dw_q, (size_t)p->D * 4, 4));
     BASP_TRY(spans.add_out(dw_k, (size_t)p->D * 4, 4));
-    BASP_TRY(spans.add_out(workspace, basp_qk_norm_rope_bwd_workspace_bytes(p)));
-    if (workspace_bytes < basp_qk_norm_rope_bwd_workspace_bytes(p)) return BASP_ERR_WORKSPACE;
+    BASP_TRY(spans.add_out(workspace, bwd_workspace_bytes(p)));
+    if (workspace_bytes < bwd_workspace_bytes(p)) return BASP_ERR_WORKSPACE;
     BASP_TRY(spans.overlaps());
     prm.partial = (float *)workspace;
     return dispatch<1, 2, 3, 4, 5, 6, 7, 8>(p->D / 16, [&](auto lanes) -> int {
-        norm_rope_bwd_kernel<decltype(lanes)::value><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(prm);
+        norm_rope_bwd_kernel<decltype(lanes)::value, R><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(prm);
         BASP_CUDA_TRY(cudaGetLastError());
         BASP_CUDA_TRY(launch_early(dw_kernel, dim3(p->D / 8, 2), 256, (cudaStream_t)stream, (const float *)prm.partial, p->D, prm.q_blocks,
                                    blocks, dw_q, dw_k));
         basp_count_launch(2);
         return BASP_OK;
     });
+}
+
+}  // namespace
+
+extern "C" int basp_qk_norm_rope(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *w_q,
+                                 const void *w_k, const float *rope_cos, const float *rope_sin, float eps, void *const *q_out,
+                                 void *const *k_out, void *stream) {
+    if (!p) return BASP_ERR_NULL;
+    BASP_TRY(supported(p, eps));
+    return p->N <= 8 ? run_fwd<8>(p, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, eps, q_out, k_out, stream)
+                     : run_fwd<BASP_MAX_RANKS>(p, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, eps, q_out, k_out, stream);
+}
+
+extern "C" size_t basp_qk_norm_rope_bwd_workspace_bytes(const basp_plan *p) { return p ? bwd_workspace_bytes(p) : 0; }
+
+extern "C" int basp_qk_norm_rope_bwd(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *w_q,
+                                     const void *w_k, const float *rope_cos, const float *rope_sin, float eps,
+                                     const void *const *dq_out, const void *const *dk_out, void *const *dq_seq,
+                                     void *const *dk_seq, float *dw_q, float *dw_k, void *workspace, size_t workspace_bytes,
+                                     void *stream) {
+    if (!p) return BASP_ERR_NULL;
+    BASP_TRY(supported(p, eps));
+    return p->N <= 8 ? run_bwd<8>(p, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, eps, dq_out, dk_out, dq_seq,
+                                  dk_seq, dw_q, dw_k, workspace, workspace_bytes, stream)
+                     : run_bwd<BASP_MAX_RANKS>(p, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, eps, dq_out, dk_out, dq_seq,
+                                                  dk_seq, dw_q, dw_k, workspace, workspace_bytes, stream);
 }
