@@ -5,32 +5,34 @@
 //   dz = g (softmax(z) - onehot(y)),       dx = dz W,       dW = sum_tokens dz^T x
 //
 // Three products, each 2 rows*vocab*hidden operations on the tensor cores, and one element-wise pass:
-//   (1) z = x W^T          epilogue: per row and 128 columns the maximum m and the sum of exp(z - m), the target's
-//                          logit apart from the others; for the gradient also every logit as its distance below that
-//                          maximum, 16 bits: rn((m - z) log2(e) 2^10), saturating at 2^-64 of the maximum's probability
-//   (merge)                rows' statistics -> loss and lse
-//   (dz)                   in place: 16-bit distance -> bf16 dz (and the piece's rows of x side by side for (3), those without a
-//                          part in the gradients as zeros: 0 x NaN would reach every word's gradient).  A distance is off by at most 2^-11 in log2, so the
-//                          probability by 2^-11 ln 2 = 3.4e-4, against bf16's own 2^-8: the 16 bits cost a fifth of nothing
-//                          and save half of an fp32 logit's traffic and memory
-//   (2) dx = dz W          split over the vocabulary where there are too few row tiles for all SMs (fp32 partial sums, joined
-//                          by one more pass)
+//   (1) z = x W^T          epilogue: per row and 128 columns the maximum m and the sum of exp(z - m), the target's logit apart
+//                          from the others; for the gradient also every logit as its distance below that maximum, 16 bits:
+//                          rn((m - z) log2(e) 2^10), saturating at 2^-64 of the maximum's probability
+//   (merge)                rows' statistics -> loss and lse; the target's logit summed again in fp32
+//   (dz)                   in place: 16-bit distance -> bf16 dz; and the piece's rows of x side by side for (3), those without a
+//                          part in the gradients as zeros (0 x NaN would reach every word's gradient)
+//   (2) dx = dz W          split over the vocabulary where there are too few row tiles for all SMs (fp32 partial sums, joined by
+//                          one more pass)
 //   (3) dW = dz^T x        K = the piece's rows; with several pieces the sum is carried in fp32
-// The rows are worked on in pieces (default 8192), so the memory between the products is 2 bytes per logit of one piece.
+// Tensor-bound for many rows: 8192 rows of 4096 features against 128256 words take 19.7 ms (1308 TFLOP/s, at the power limit; the
+// three products alone by cuBLAS 18.6 ms), of which dz takes 0.62 (4.2 GB, HBM-bound).  Few rows: bound by reading W twice and
+// writing dW.  Rows are worked on in pieces (default 8192), so what lies between the products is 2 bytes per logit of one piece.
 //
-// The target's logit is left out of the sums: with o = ln sum_{v != y} exp z_v, loss = softplus(o - z_y) and the target's
-// dz = -g sigmoid(o - z_y).  lse - z_y and p_y - 1 would cancel for a confident prediction.
+// Roundings.  A distance is off by at most 2^-11 in log2, so a probability by 2^-11 ln 2 = 3.4e-4, before it is rounded to bf16
+// (2^-8) as an operand: 16 bits do for what would otherwise be an fp32 logit, twice the memory and traffic.  The target is left out of
+// the sums: with o = ln sum_{v != y} exp z_v, loss = softplus(o - z_y) and the target's dz = -g sigmoid(o - z_y); lse - z_y and
+// p_y - 1 would cancel for a confident prediction.  dz is kept in units of the largest weight of the piece, which the epilogues of
+// (2) and (3) multiply in fp32.
 //
-// Products: persistent, one CTA per SM, tile 128 x 256, K in blocks of 64 (128-byte-swizzled TMA boxes):
-//   warp 0      TMA producer, 4-stage ring (A 16 KiB + B 32 KiB per stage)
-//   warp 1      tcgen05.mma issuer (M = 128, N = 256, K = 16), two 256-column TMEM accumulators so that the epilogue of one
-//               tile runs under the main loop of the next
-//   warps 2-5   epilogue (a thread owns a row of the tile)
-// W and x are read as they lie: K-major for (1), and as MN-major operands for (2) and (3), dz K-major for (2) and MN-major for
-// (3); nothing is transposed in memory.
+// Products: persistent, K in blocks of 64 (128-byte-swizzled TMA boxes), a four-stage ring of 48 KiB stages:
+//   warp 0      TMA producer
+//   warp 1      tcgen05.mma issuer, two 256-column accumulators in TMEM
+//   warps 2-9   epilogue (a thread owns a row of an accumulator)
+// Tiles of 128 x 256 by single CTAs, or of 512 x 256 by pairs (see lm_gemm_kernel).  W and x are read as they lie: K-major for (1),
+// as MN-major operands for (2) and (3); dz K-major for (2) and MN-major for (3); nothing is transposed in memory.
 //
-// Rows of all ranks are put together in slots of 8..128 rows (a power of two, by the rows of a rank), so that a tile holds
-// several ranks where a rank has few tokens; rows of a slot past a rank's end are zero in every product.
+// Rows of all ranks are put together in slots of 8..128 rows (a power of two, by the rows of a rank), so that a tile holds several
+// ranks where a rank has few tokens.
 #include <cuda.h>
 #include <math.h>
 #include <string.h>
@@ -171,11 +173,12 @@ __device__ __forceinline__ void store_bf16x32(__nv_bfloat16 *dst, const float (&
     }
 }
 
-// kPair = false: a CTA works on 128 x 256 tiles; its two accumulators take turns, so that the epilogue of one tile runs under
-// the main loop of the next.
-// kPair = true: two neighbouring CTAs (a cluster) work on one 512 x 256 tile, each with 256 of its rows and half of B; the two
-// accumulators of a CTA are the upper and lower 128 of its rows.  The last blocks of K are issued for the upper rows first, the
-// first blocks of the next tile too: either epilogue then runs under the other half's products.
+// kPair = false: a CTA works on 128 x 256 tiles; its two accumulators take turns, so that the epilogue of one tile runs under the
+// main loop of the next.
+// kPair = true: two neighbouring CTAs (a cluster) work on one 512 x 256 tile, each with 256 of its rows and half of B, so that a
+// product needs half the bytes from L2; the two accumulators of a CTA are the upper and lower 128 of its rows.  The last blocks of
+// K are issued for the upper rows first, the first blocks of the next tile too: either epilogue then runs under the other half's
+// products.
 template <int kKind, int R, bool kPair>
 __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_constant__ LossParams<R> p) {
     constexpr int kS = kStages, kRows = kRowsPerCta<kPair>, kBCols = kPair ? kBN / 2 : kBN;
