@@ -13,7 +13,7 @@
 // 32 bytes of bf16, 16 bytes of codes.
 #include <cuda_bf16.h>
 
-#include <type_traits>
+#include <utility>
 
 #include "common.cuh"
 #include "spans.h"
@@ -91,13 +91,31 @@ __device__ __forceinline__ Where where(const CkptParams<R> &p) {
     return w;
 }
 
-// kL lanes hold one head vector, 16 elements each (lanes past D/16 idle).
-template <int kL, bool kWide, int R>
+// The largest of the N lanes that hold a vector, in all of them; `lane`: this one's place among them.
+template <int N>
+__device__ __forceinline__ uint32_t group_max(uint32_t v, int lane) {
+    if constexpr ((N & (N - 1)) == 0) {
+#pragma unroll
+        for (int o = N / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+        return v;
+    } else {
+#pragma unroll
+        for (int o = N > 4 ? 4 : 2; o > 0; o >>= 1) {
+            const uint32_t far = __shfl_down_sync(0xffffffffu, v, o);
+            if (lane + o < N) v = max(v, far);
+        }
+        return __shfl_sync(0xffffffffu, v, (threadIdx.x & 31) - lane);
+    }
+}
+
+// N = D / 16 lanes hold a head vector, 16 elements each; a warp holds 32 / N vectors.
+template <int N, bool kWide, int R>
 __global__ void __launch_bounds__(kThreads) ckpt_pack_kernel(const __grid_constant__ CkptParams<R> p) {
-    constexpr uint32_t kGroups = kThreads / kL;
+    constexpr uint32_t kPerWarp = 32 / N, kGroups = kThreads / 32 * kPerWarp;
     const Where at = where(p);
     const CkptTensor &t = p.t[at.tensor];
-    const uint32_t group = threadIdx.x / kL, lane = threadIdx.x % kL;
+    const uint32_t warp_lane = threadIdx.x & 31, vec = warp_lane / N, lane = warp_lane - vec * N, group = threadIdx.x / 32 * kPerWarp + vec;
+    const bool mine = vec < kPerWarp;
     const uint32_t vectors = p.Bl * (at.last ? p.T_last : p.T) * t.heads;
     const uint32_t v0 = at.chunk * kGroups * kUnroll + group;
     const char *src = p.wide[at.tensor][at.rank];
@@ -107,7 +125,7 @@ __global__ void __launch_bounds__(kThreads) ckpt_pack_kernel(const __grid_consta
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
         const uint32_t v = v0 + i * kGroups;
-        if (v < vectors && lane < p.vec_u) x[i] = load_unit<kWide>(src + ((uint64_t)v * p.vec_u + lane) * 32);
+        if (v < vectors && mine) x[i] = load_unit<kWide>(src + ((uint64_t)v * N + lane) * 32);
         else
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[i].w[e] = 0;
@@ -120,8 +138,7 @@ __global__ void __launch_bounds__(kThreads) ckpt_pack_kernel(const __grid_consta
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = __vmaxu2(top, x[i].w[e] & 0x7fff7fffu);
         top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-        for (int o = kL / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o, kL));
+        top = group_max<N>(top, (int)lane);
         const float amax = __uint_as_float(top << 16);
         const bool zero = amax < 7.888609052210118e-31f;             // 2^-100
         const float inv = zero ? 0.f : __fdiv_rn(127.f, amax);
@@ -139,8 +156,8 @@ __global__ void __launch_bounds__(kThreads) ckpt_pack_kernel(const __grid_consta
             }
             out[q] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
         }
-        if (v < vectors && lane < p.vec_u) {
-            *reinterpret_cast<uint4 *>(codes + ((uint64_t)v * p.vec_u + lane) * 16) = make_uint4(out[0], out[1], out[2], out[3]);
+        if (v < vectors && mine) {
+            *reinterpret_cast<uint4 *>(codes + ((uint64_t)v * N + lane) * 16) = make_uint4(out[0], out[1], out[2], out[3]);
             if (lane == 0) scales[v] = scale;
         }
     }
@@ -230,8 +247,6 @@ int fill(const basp_plan *p, const void *const *ckpt, const void *const *const (
         BASP_TRY(pack ? spans->add_out(ckpt[r], n) : spans->add_in(ckpt[r], n));
         prm->ckpt[r] = (char *)ckpt[r];
     }
-    int lanes = 1;
-    while (lanes * 16 < p->D) lanes *= 2;
     uint64_t cursor = 0;
     for (int i = 0; i < kTensors; ++i) {
         CkptTensor &t = prm->t[i];
@@ -246,7 +261,7 @@ int fill(const basp_plan *p, const void *const *ckpt, const void *const *const (
         const uint64_t vectors = (uint64_t)p->Bl * p->T * heads, units = vectors * prm->vec_u;
         const uint64_t head_units = (uint64_t)p->Bl * p->S * t.run_u;
         if (units + kThreads * kUnroll >= (1ull << 31) || head_units >= (1ull << 32)) return BASP_ERR_UNSUPPORTED;
-        const uint64_t per_chunk = pack ? (uint64_t)(kThreads / lanes) * kUnroll : (uint64_t)kThreads * kUnroll;
+        const uint64_t per_chunk = pack ? (uint64_t)(kThreads / 32 * (32 / prm->vec_u)) * kUnroll : (uint64_t)kThreads * kUnroll;
         const uint64_t chunks = ((pack ? vectors : units) + per_chunk - 1) / per_chunk;
         t.chunk_begin = (uint32_t)cursor;
         t.chunks_per_shard = (uint32_t)chunks;
@@ -272,10 +287,11 @@ bool all_on_32(const basp_plan *p, const CkptParams<R> &prm) {
     return (bits & 31) == 0;
 }
 
-template <int kL, int R>
-void launch_pack(const CkptParams<R> &prm, uint32_t blocks, bool wide, cudaStream_t st) {
-    if (wide) ckpt_pack_kernel<kL, true, R><<<blocks, kThreads, 0, st>>>(prm);
-    else ckpt_pack_kernel<kL, false, R><<<blocks, kThreads, 0, st>>>(prm);
+template <int R, int... kN>
+void launch_pack(const CkptParams<R> &prm, uint32_t blocks, bool wide, cudaStream_t st, std::integer_sequence<int, kN...>) {
+    ((prm.vec_u != kN + 1 ? (void)0
+                          : wide ? ckpt_pack_kernel<kN + 1, true, R><<<blocks, kThreads, 0, st>>>(prm)
+                                 : ckpt_pack_kernel<kN + 1, false, R><<<blocks, kThreads, 0, st>>>(prm)), ...);
 }
 
 template <int R>
@@ -285,10 +301,7 @@ int run_pack(const basp_plan *p, const void *const *const (&shards)[kTensors], v
     uint32_t blocks = 0;
     BASP_TRY(fill(p, (const void *const *)ckpt_shards, shards, true, &prm, &spans, &blocks));
     const bool wide = all_on_32(p, prm);
-    if (p->D > 64) launch_pack<8>(prm, blocks, wide, st);
-    else if (p->D > 32) launch_pack<4>(prm, blocks, wide, st);
-    else if (p->D > 16) launch_pack<2>(prm, blocks, wide, st);
-    else launch_pack<1>(prm, blocks, wide, st);
+    launch_pack(prm, blocks, wide, st, std::make_integer_sequence<int, 8>{});
     BASP_CUDA_TRY(cudaGetLastError());
     basp_count_launch(1);
     return BASP_OK;
