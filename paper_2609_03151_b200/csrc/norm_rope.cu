@@ -12,7 +12,7 @@
 //             2 x 8K tokens, 64 heads of 128: 95 us (5.7 TB/s); with the backward's layout 104 us.
 //   backward  a lane holds eight features and their eight partners, so D/16 lanes a vector and no shuffle but the sums; the
 //             vectors of a warp are neighbouring tokens.  128 registers, two blocks per SM.
-//             128K tokens, 40 heads of 128: 707 us (5.8 TB/s); with the forward's layout 727 us.
+//             128K tokens, 40 heads of 128: 715 us (5.7 TB/s); with the forward's layout 727 us.
 #include <cuda_bf16.h>
 
 #include <type_traits>
