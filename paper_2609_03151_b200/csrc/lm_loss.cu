@@ -796,10 +796,10 @@ Workspace workspace_of(const Sizes &z, int hidden, int vocab, bool grad) {
         w.info = take(rows * sizeof(RowInfo));
         w.kept = take(rows * hidden * 2);
         const int last = z.tiles_m - (z.pieces - 1) * z.piece_tiles, kb = cdiv(vocab, kBK);
-        size_t partial = 0;
+        size_t partial = 0;                        // both sizes of piece; the sums of a split lie a whole piece apart
         for (int tiles : {z.piece_tiles, last}) {
             const int s = dx_splits(tiles, z.tiles_h, kb, hidden);
-            if (s > 1 && (size_t)s * tiles * kBM * hidden * 4 > partial) partial = (size_t)s * tiles * kBM * hidden * 4;
+            if (s > 1 && (size_t)s * rows * hidden * 4 > partial) partial = (size_t)s * rows * hidden * 4;
         }
         w.partial = take(partial);
         w.acc = take(z.pieces > 1 ? (size_t)vocab * hidden * 4 : 0);

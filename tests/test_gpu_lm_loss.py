@@ -133,6 +133,17 @@ def test_pieces(basp, piece_rows):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("rows,piece_rows", [(300, 256), (1100, 512), (700, 640)])
+def test_short_last_piece_with_a_split_vocabulary(basp, rows, piece_rows):
+    """The last piece has fewer row tiles than the others, so its dx splits the vocabulary more often: its partial sums stay clear of
+    the running sum of dw."""
+    w, hidden, vocab = L("short_last", 1, 1, rows, 64, 20000)
+    pl = make_plan(basp, w)
+    W, x, labels, weights = inputs(pl, hidden, vocab, 6)
+    ref = oracle.lm_loss(f64(cat(x)), f64(W), cat(labels).numpy(), cat(weights).numpy().astype(np.float64))
+    check(run(basp, pl, hidden, vocab, W, x, labels, weights, piece_rows=piece_rows), ref, x, W, hidden, vocab, (rows, piece_rows))
+
+
 def test_weights_of_one_and_confident_predictions(basp):
     """No weight table; the target 60 above the others: a loss far below fp32's spacing at the logit's size."""
     w, hidden, vocab = L("sure", 2, 1, 64, 256, 700)
