@@ -16,7 +16,10 @@ if not os.path.exists(_LIB_PATH):
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2609_03151_b200.build` "
                       "(there is no fallback path)")
 lib = ctypes.CDLL(_LIB_PATH)
-from ._marshal import addresses as _fast_addresses  # noqa: E402  (built beside the library, from csrc/marshal.cpp)
+try:
+    from ._marshal import addresses as _fast_addresses  # built beside the library, from csrc/marshal.cpp
+except ImportError as e:
+    raise ImportError(f"the binding's _marshal.so does not load ({e}): build it with `python -m paper_2609_03151_b200.build`") from e
 
 BASP_OK = 0
 BASP_ERR_INVALID, BASP_ERR_UNSUPPORTED, BASP_ERR_NULL, BASP_ERR_ALIGN = -1, -2, -3, -4

@@ -164,3 +164,21 @@ def test_binding_refuses_tensors_it_would_misread(basp, plan):
         basp.basp_ckpt_pack(plan, q, q, q, q, q)
     with pytest.raises(ValueError, match="expected 4 shards"):
         basp.basp_ckpt_pack(plan, q[:0], q, q, q, q)
+
+
+def test_marshalling_passes_on_what_it_cannot_vouch_for(basp):
+    """The quick look at a call's tensors answers with addresses or not at all; what it does not know (raw addresses, wrong
+    tensors, wrong arguments) is left to the binding's own checks."""
+    from paper_2609_03151_b200._marshal import addresses
+    t = torch.zeros(8, dtype=torch.bfloat16)
+    assert addresses(0, (("a", torch.bfloat16, [t], (8,)),)) is None                 # not in device memory
+    assert addresses(0, (("a", torch.bfloat16, [123], (8,)),)) is None
+    assert addresses(0, (("a", torch.bfloat16, [t, t], (8,)),)) is None
+    assert addresses(0, (("a", torch.bfloat16, t, "8"),)) is None
+    assert addresses(0, (("a", torch.bfloat16, None, (8,)), ("b", torch.float32, None, 3)))[1] == [None, None]
+    assert addresses(0, ())[1] == []
+    with pytest.raises(TypeError):
+        addresses(0)
+    m = basp._Marshal()
+    table, one, none = m.addresses(("a", torch.bfloat16, [16, None, 48], (8, 8, 8)), ("b", torch.float32, 4096, 3), ("c", torch.int64, None, 1))
+    assert list((ctypes.c_void_p * 3).from_address(table)) == [16, None, 48] and one == 4096 and none is None
