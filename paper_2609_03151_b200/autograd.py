@@ -16,7 +16,8 @@ fused=True and checkpoint8=True what is kept of Q, K, V and O are 8-bit checkpoi
 the backward reads them back with the exchanges (basp_layer_bwd_ckpt).  That pays off where nothing else keeps the bf16
 tensors alive.
 
-The operations run on the current stream with the tensors' device current, and may be captured into a CUDA graph.
+The operations run on the current stream with the tensors' device current, and may be captured into a CUDA graph, forward and
+backward, as torch prescribes: warmed up on a side stream, and with no eager graph of the same leaves alive during the capture.
 """
 from __future__ import annotations
 

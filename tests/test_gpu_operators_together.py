@@ -87,6 +87,54 @@ def test_two_graphs_and_eager(basp, op):
                 assert torch.equal(a, b), i
 
 
+def test_captured_training_step(basp):
+    """Head norms, attention with checkpoints and the loss, forward and backward by torch's autograd, captured as one graph and
+    replayed on new inputs: the gradients of an eager step on them."""
+    from paper_2609_03151_b200.autograd import basp_attention, basp_lm_loss, basp_qk_norm_rope
+    pl = basp.basp_plan_create(4, 2, 256, 4, 2, 128)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    tables = [t.t().contiguous().cuda() for t in synth.rope_tables(256, 128)]
+    labels = [torch.randint(0, 500, (128,), generator=g, device="cuda") for _ in range(4)]
+    weight = [torch.full((128,), 1.0 / 512, device="cuda") for _ in range(4)]
+    make = lambda: [normal(g, 128, h, 128) for h in (4,) * 4 + (2,) * 8] + [normal(g, 128) * 0.1 + 1, normal(g, 128) * 0.1 + 1,
+                                                                             normal(g, 500, 512) * 0.05]
+    leaves = [t.to(torch.bfloat16).requires_grad_() for t in make()]
+
+    def step():
+        q, k = basp_qk_norm_rope(pl, leaves[:4], leaves[4:8], leaves[12], leaves[13], *tables)
+        o = basp_attention(pl, q, k, leaves[8:12], fused=True, checkpoint8=True)
+        loss = basp_lm_loss(pl, [t.reshape(128, 512) for t in o], leaves[14], labels, weight)
+        loss.backward()
+        return loss.detach()
+
+    basp.basp_clear_status()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    for t in leaves:
+        t.grad = None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        loss = step()
+    fresh = make()
+    with torch.no_grad():
+        for t, f in zip(leaves, fresh):
+            t.copy_(f)
+    graph.replay()
+    torch.cuda.synchronize()
+    got, got_loss = [t.grad.clone() for t in leaves], loss.clone()
+    for t in leaves:
+        t.grad = None
+    eager_loss = step()
+    basp.basp_get_status()
+    assert torch.equal(got_loss, eager_loss)
+    for i, (a, t) in enumerate(zip(got, leaves)):
+        off = (a.float() - t.grad.float()).norm() / t.grad.float().norm()
+        assert off <= 2.0 ** -8, (i, off.item())          # dQ comes from a reduction in whatever order its blocks finish
+
+
 def test_two_streams_at_once(basp):
     """Two losses of different sizes on two streams, a dozen times over, against each alone."""
     g = torch.Generator(device="cuda").manual_seed(2)
