@@ -396,12 +396,15 @@ int basp_layer_bwd_ckpt(const basp_plan *plan, const void *const *ckpt_shards, c
  * shards, without keeping the logits.  For a token with hidden state x (a row of x_seq[r], bf16 [Bl*T][hidden]) and label y:
  *   z = x W^T  (w: bf16 [vocab][hidden], shared by all ranks),   lse = ln sum_v exp(z_v),   loss = lse - z_y
  * labels[r]: int64 [Bl*T]; a label outside [0, vocab) (such as -100) marks a token without a loss: its loss is 0 and it has
- * no part in the gradients.  loss_seq[r], lse_seq[r]: fp32 [Bl*T] (lse_seq may be NULL).  bf16 products with fp32 sums; the logits are not rounded.
+ * no part in the gradients.  loss_seq[r], lse_seq[r]: fp32 [Bl*T] (lse_seq may be NULL).  bf16 products with fp32 sums; in the
+ * loss the logits are not rounded.
  *
  * basp_lm_loss_grad also writes the gradients of sum_tokens g loss with g = token_weights[r][token] (fp32 [Bl*T]; NULL table:
- * 1 each):  dz = g (softmax(z) - onehot(y)),  dx_seq[r] = dz W (bf16),  dw = sum dz^T x (bf16 [vocab][hidden]; summed in fp32, rounded
- * once).  dz is rounded to bf16 as an operand.  A NULL dx_seq or dw (not both) leaves that gradient and its product out.  A token of weight 0 has no part in the gradients whatever its values.  Both
- * gradients are written, not added to; the same inputs and piece_rows give the same bits.
+ * 1 each):  dz = g (softmax(z) - onehot(y)),  dx_seq[r] = dz W (bf16),  dw = sum dz^T x (bf16 [vocab][hidden]; summed in
+ * fp32, rounded once).  Between the products a probability is held to 3.4e-4 of itself (zero below 2^-64 of the largest of
+ * its 128 words), and dz is rounded to bf16 as an operand.  A NULL dx_seq or dw (not both) leaves that gradient and its
+ * product out.  A token of weight 0 has no part in the gradients, NaN among its values or not.  Both gradients are written,
+ * not added to; the same inputs and piece_rows give the same bits.
  * The rows are worked on in pieces of piece_rows (rounded up to 128; 0: 8192; at most 32768), 2 bytes per logit of one piece
  * in the workspace, plus 4 vocab hidden bytes for the running sum of dw where there are several pieces.
  * Requires hidden a multiple of 8 up to 65536 and vocab up to 2^24 (BASP_ERR_UNSUPPORTED; neither positive:
