@@ -26,6 +26,7 @@
  *   - returns 0 (BASP_OK) or a negative BASP_ERR_* code; nothing throws across the ABI;
  *   - "*_shards" arguments are HOST arrays of n_ranks DEVICE pointers; the array is read
  *     during the call and not retained; every device pointer must be 16-byte aligned;
+ *   - a workspace belongs to one call at a time: calls, or replays of captured calls, that can overlap on the GPU need one each;
  *   - the caller owns every device buffer (workspace included); the library allocates no
  *     device memory and keeps no pointer after return; the plan is the only library object
  *     (one exception, stated there: basp_layer_fwd_static keeps its scratch in a fixed array
