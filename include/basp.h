@@ -404,8 +404,9 @@ int basp_layer_bwd_ckpt(const basp_plan *plan, const void *const *ckpt_shards, c
  * 1 each):  dz = g (softmax(z) - onehot(y)),  dx_seq[r] = dz W (bf16),  dw = sum dz^T x (bf16 [vocab][hidden]; summed in
  * fp32, rounded once).  Between the products a probability is held to 3.4e-4 of itself (zero below 2^-64 of the largest of
  * its 128 words), and dz is rounded to bf16 as an operand.  A NULL dx_seq or dw (not both) leaves that gradient and its
- * product out.  A token of weight 0 has no part in the gradients, NaN among its values or not.  Both gradients are written,
- * not added to; the same inputs and piece_rows give the same bits.
+ * product out.  A token of weight 0 has no part in the gradients, NaN among its values or not; a weight that is no finite
+ * number reaches its own dx and dw only.  Both gradients are written, not added to; the same inputs and piece_rows give the
+ * same bits.
  * The rows are worked on in pieces of piece_rows (rounded up to 128; 0: 8192; at most 32768), 2 bytes per logit of one piece
  * in the workspace, plus 4 vocab hidden bytes for the running sum of dw where there are several pieces.
  * Requires hidden a multiple of 8 up to 65536 and vocab up to 2^24 (BASP_ERR_UNSUPPORTED; neither positive:

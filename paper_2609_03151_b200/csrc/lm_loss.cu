@@ -21,8 +21,8 @@
 // Roundings.  A distance is off by at most 2^-11 in log2, so a probability by 2^-11 ln 2 = 3.4e-4, before it is rounded to bf16
 // (2^-8) as an operand: 16 bits do for what would otherwise be an fp32 logit, twice the memory and traffic.  The target is left out of
 // the sums: with o = ln sum_{v != y} exp z_v, loss = softplus(o - z_y) and the target's dz = -g sigmoid(o - z_y); lse - z_y and
-// p_y - 1 would cancel for a confident prediction.  dz is kept in units of the largest weight of the piece, which the epilogues of
-// (2) and (3) multiply in fp32.
+// p_y - 1 would cancel for a confident prediction.  dz is kept in units of the largest finite weight of the piece, which the
+// epilogues of (2) and (3) multiply in fp32.
 //
 // Products: persistent, K in blocks of 64 (128-byte-swizzled TMA boxes), a four-stage ring of 48 KiB stages:
 //   warp 0      TMA producer
@@ -103,7 +103,7 @@ struct LossParams {
     size_t pitch;              // columns of a row of 16-bit logits
     int piece_rows;
     float2 *stats;             // [groups of kStatCols columns][piece_rows]: maximum, sum
-    unsigned *scale;           // bits of the largest |weight| of the piece: dz is in its units, so that equal weights leave
+    unsigned *scale;           // bits of the largest finite |weight| of the piece: dz is in its units, so that equal weights leave
                                // p - 1 as it is (rounding -1 g would be one relative error common to all tokens)
     uint16_t *codes;           // [piece_rows][pitch]
     float *partial;            // (2) with splits > 1: [splits][piece_rows][hidden]
@@ -617,7 +617,9 @@ __global__ void __launch_bounds__(1024) lm_merge_kernel(const __grid_constant__ 
         }
         if (p.info) {
             p.info[row] = info;
-            atomicMax(&scale, __float_as_uint(fabsf(info.weight)));
+            // a weight that is no finite number is not a unit: it reaches its own dx and dw, not other tokens' dx
+            const float size = fabsf(info.weight);
+            atomicMax(&scale, size < INFINITY ? __float_as_uint(size) : 0u);
         }
     }
     if (!p.info) return;

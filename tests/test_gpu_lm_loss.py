@@ -207,6 +207,32 @@ def test_special_rows_and_words(basp):
     assert (f64(dw)[100:] == 0).all() and np.linalg.norm(f64(dw)[:100] - ref2["dw"]) <= 2.0 ** -8 * np.linalg.norm(ref2["dw"])
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("N,S", [(2, 40), (1, 700)])
+def test_a_weight_that_is_no_number_stays_with_its_token(basp, value, N, S):
+    """A NaN or infinite token weight makes its own row of dx and dw no numbers (dz = g (p - onehot)); the losses and the
+    other tokens' dx are those of the call without it."""
+    w, hidden, vocab = L("odd_weight", N, 1, S, 64, 600)
+    pl = make_plan(basp, w)
+    W, x, labels, weights = inputs(pl, hidden, vocab, 6)
+    labels = [torch.where((y < 0) | (y >= vocab), 5, y) for y in labels]
+    weights[0][5] = 0.5                                     # not the largest: the others' unit does not change
+    weights[0][6] = 1.25
+    loss, lse, dx, _ = run(basp, pl, hidden, vocab, W, x, labels, weights)
+    weights[0][5] = value
+    loss2, lse2, dx2, dw2 = run(basp, pl, hidden, vocab, W, x, labels, weights)
+    assert torch.equal(cat(loss), cat(loss2)) and torch.equal(cat(lse), cat(lse2))
+    keep = torch.ones(S, dtype=torch.bool, device="cuda")
+    keep[5] = False
+    assert torch.equal(cat(dx)[keep], cat(dx2)[keep]) and torch.isfinite(cat(dx2)[keep]).all().item()
+    assert not torch.isfinite(cat(dx2)[5]).any().item() and not torch.isfinite(dw2).any().item()
+    # no finite weight at all
+    none = [torch.full_like(t, value) for t in weights]
+    loss3, _, dx3, dw3 = run(basp, pl, hidden, vocab, W, x, labels, none)
+    assert torch.equal(cat(loss), cat(loss3))
+    assert not torch.isfinite(cat(dx3)).any().item() and not torch.isfinite(dw3).any().item()
+
+
 def test_rows_and_words_behind_the_ends_are_left(basp):
     w, hidden, vocab = L("ends", 2, 1, 20, 72, 300)
     pl = make_plan(basp, w)
