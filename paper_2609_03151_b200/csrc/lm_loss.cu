@@ -238,12 +238,13 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                         else tma_load_3d(dst, map, &bars.full[s], c, 0, r);
                     };
                     if constexpr (kKind == kStats || kKind == kLogits) {
+                        // W, which comes from HBM, is asked for before x (1 token: 30.9 us per call, x first; 29.8 so)
+                        load(b, &p.w, kb * kBK, n0);
                         // slots past the piece's end are left as they are: a row of A reaches its own row of the product only
                         for (int j = 0; j < mine; ++j) {
                             const int at = p.rows.slot_begin + (m0 >> p.rows.slot_log2) + j, r = at / p.rows.per_rank;
                             load(a + (j << p.rows.slot_log2) * kBK * 2, &p.x[r], kb * kBK, (at - r * p.rows.per_rank) << p.rows.slot_log2);
                         }
-                        load(b, &p.w, kb * kBK, n0);
                     } else if constexpr (kKind == kDx) {
 #pragma unroll
                         for (int j = 0; j < kRows; j += kBM) load(a + j * kBK * 2, &p.dz, kb * kBK, m0 + j);
