@@ -166,6 +166,24 @@ def test_weights_of_one_and_confident_predictions(basp):
     assert (np.abs(f64(cat(got[0])) - exact) <= (4 * tz + 2.0 ** -18) * exact).all()
 
 
+@pytest.mark.parametrize("rows", [100, 520])           # single CTAs, pairs
+@pytest.mark.parametrize("hidden", [2048, 8192])
+def test_lse_is_not_short_of_what_the_products_cut_off(basp, rows, hidden):
+    """The tensor cores cut a running sum off towards zero, up to 2^-23 of it in each of hidden / 16 steps; on such values
+    that is 2^-30 hidden of a logit in the mean (2^-3 of the bound), by which lse = ln sum exp z is short by as much of
+    sum p z.  The kernel makes up for it: at least half has to be gone from the mean over the tokens, besides 2^-21 for the
+    statistics (fp32 of about 9: half a step of 2^-21)."""
+    w, hidden, vocab = L("short", 1, 1, rows, hidden, 4096)
+    pl = make_plan(basp, w)
+    W, x, labels, weights = inputs(pl, hidden, vocab, 7, sure=0.0)
+    z = x[0].cuda().double() @ W.cuda().double().T
+    exact = torch.logsumexp(z, -1)
+    spread = (torch.softmax(z, -1) * z).sum(-1)
+    _, lse, _, _ = run(basp, pl, hidden, vocab, W, x, labels, weights, dw=False)
+    short = (exact - lse[0].double()).mean().abs().item()
+    assert short <= 2.0 ** -31 * hidden * spread.mean().item() + 2.0 ** -21, short
+
+
 def test_special_rows_and_words(basp):
     """Infinities and NaN: a row that has them is NaN and no other row is; a row without a label or a weight leaves the
     gradients alone; a word whose weights make its logit -inf has probability zero."""
