@@ -122,7 +122,9 @@ class _QkNormRope(torch.autograd.Function):
 
 def basp_qk_norm_rope(plan, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, eps: float = 1e-6):
     """Root-mean-square norm of every query and key head (weights w_q, w_k [D], bf16) with the rotary embedding, on
-    sequence-sharded Q and K; differentiable in the shards and the weights.  Returns (q shards, k shards)."""
+    sequence-sharded Q and K; differentiable in the shards and the weights, not in the tables.  Returns (q shards, k shards)."""
+    if rope_cos.requires_grad or rope_sin.requires_grad:
+        raise ValueError("rope_cos and rope_sin are not differentiable")
     out = _QkNormRope.apply(plan, float(eps), rope_cos, rope_sin, w_q, w_k, *q_seq, *k_seq)
     return list(out[:plan.N]), list(out[plan.N:])
 
@@ -150,7 +152,9 @@ class _LmLoss(torch.autograd.Function):
         every = torch.cat([t.reshape(-1) for t in loss])
         if token_weights is not None:
             weight = torch.cat([t.reshape(-1) for t in token_weights])
-            every = torch.where(weight != 0, every * weight, 0.0)        # a token of weight 0 has no part, whatever its loss
+            label = torch.cat([t.reshape(-1) for t in labels])
+            # a token of weight 0 has no part, whatever its loss, and one without a label none, whatever its weight
+            every = torch.where((weight != 0) & (label >= 0) & (label < vocab), every * weight, 0.0)
         return every.sum()
 
     @staticmethod

@@ -312,3 +312,22 @@ def test_autograd_pieces_of_it_and_graph(basp):
     call(eager, torch.empty_like(space))
     basp.basp_get_status()
     assert all(torch.equal(a, b) for a, b in zip(out[0] + out[1] + [out[2]], eager[0] + eager[1] + [eager[2]]))
+
+
+def test_the_weight_of_a_token_without_a_label_has_no_part(basp):
+    """1 / (number of labels) is infinite where a shard's tokens have none: the summed loss and its gradients leave them out."""
+    from paper_2609_03151_b200.autograd import basp_lm_loss
+    w, hidden, vocab = L("no_label", 2, 1, 40, 64, 600)
+    pl = make_plan(basp, w)
+    W, x, labels, weights = inputs(pl, hidden, vocab, 8)
+    labels[0][3], labels[0][4], labels[1][:] = -100, vocab, -100
+    c = lambda ts: [t.cuda() for t in ts]
+    grads = []
+    for odd in (1.0, float("inf"), float("nan")):
+        weights[0][3] = weights[0][4] = odd
+        weights[1][:] = odd
+        xl, wl = [t.requires_grad_() for t in c(x)], W.cuda().requires_grad_()
+        loss = basp_lm_loss(pl, xl, wl, c(labels), c(weights))
+        grads.append((loss.detach(), *torch.autograd.grad(loss, [*xl, wl])))
+    assert all(torch.isfinite(t).all().item() for t in grads[0])
+    assert all(torch.equal(a, b) for other in grads[1:] for a, b in zip(grads[0], other))

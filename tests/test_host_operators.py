@@ -182,3 +182,11 @@ def test_marshalling_passes_on_what_it_cannot_vouch_for(basp):
     m = basp._Marshal()
     table, one, none = m.addresses(("a", torch.bfloat16, [16, None, 48], (8, 8, 8)), ("b", torch.float32, 4096, 3), ("c", torch.int64, None, 1))
     assert list((ctypes.c_void_p * 3).from_address(table)) == [16, None, 48] and one == 4096 and none is None
+
+
+def test_the_rotation_tables_are_not_differentiable():
+    from paper_2609_03151_b200.autograd import basp_qk_norm_rope
+    t = torch.zeros(4, 8)
+    for cos, sin in ((t.clone().requires_grad_(), t), (t, t.clone().requires_grad_())):
+        with pytest.raises(ValueError, match="not differentiable"):
+            basp_qk_norm_rope(None, [], [], t, t, cos, sin)
