@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) norm_rope_bwd_kernel(con
                 const float s1 = group_sum<N>(sum2(sq), lane), s2 = group_sum<N>(sum2(dot), lane);
                 const float r = rsqrtf(fmaf(s1, p.inv_D, p.eps));
                 if (!active || h + u >= at.count) continue;
-                const float k = -r * r * r * s2 * p.inv_D;
+                const float k = -(r * s2 * p.inv_D) * r * r;     // in this order: r^3 alone leaves fp32 for zeros and an eps below 1e-25
                 const uint64_t r2 = pack_f2(r, r), k2 = pack_f2(k, k);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {

@@ -140,6 +140,30 @@ def test_zero_and_special_vectors(basp):
     assert (np.abs(y[:2] - ref) <= 2.0 ** -8 * np.abs(ref) + 1e-5).all()
 
 
+def test_backward_of_zeros_and_small_vectors_with_a_small_eps(basp):
+    """eps = 1e-30: r = 10^15 of a zero vector leaves fp32 in its third power, but x r^3 (x . w u) / D is zero there; a vector
+    of 2^-40 is far above eps.  The bounds are those of the other tests, in the vector's own units."""
+    w, eps = synth.Workload("small_eps", N=1, B=1, S=4, Hq=4, Hkv=2, D=64), 1e-30
+    pl, mk, ws, cos, sin, pos = setup(basp, w, 3)
+    x, dy = [mk(4), mk(2)], [mk(4), mk(2)]
+    x[0][0][1, 2], x[1][0][:] = 0.0, 0.0
+    x[0][0][2] *= 2.0 ** -40                              # exact
+    table = [t.t().contiguous().cuda() for t in (cos, sin)]
+    dx = [blank(cuda(t)) for t in x]
+    dw = [torch.full((w.D,), float("nan"), device="cuda") for _ in range(2)]
+    space = torch.full((basp.basp_qk_norm_rope_bwd_workspace_bytes(pl) // 4,), float("nan"), device="cuda")
+    basp.basp_qk_norm_rope_bwd(pl, cuda(x[0]), cuda(x[1]), ws[0].cuda(), ws[1].cuda(), *table, cuda(dy[0]), cuda(dy[1]), *dx,
+                               *dw, space, eps=eps)
+    for i in range(2):
+        X, W, DY = f64(x[i][0]), f64(ws[i]), f64(dy[i][0])
+        want, want_w = oracle.qk_norm_rope_bwd(X, W, cos.numpy(), sin.numpy(), pos[0], eps, DY)
+        s, u = (X * X).mean(-1, keepdims=True) + eps, halves(DY)
+        terms = np.abs(W) * u / np.sqrt(s) + np.abs(X) * s ** -1.5 * (np.abs(X * W) * u).sum(-1, keepdims=True) / w.D
+        assert (np.abs(f64(dx[i][0]) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -18 * terms).all(), i
+        size = (np.abs(X) / np.sqrt(s) * u).sum((0, 1))
+        assert (np.abs(f64(dw[i]) - want_w) <= (2.0 ** -14 + 2.0 ** -19) * size).all(), i
+
+
 def test_rows_behind_the_shard_are_left(basp):
     """A buffer longer than the shard keeps what lies behind it (tiles of 32 tokens, shards of 5)."""
     w = synth.Workload("tail", N=2, B=2, S=5, Hq=2, Hkv=2, D=128)
