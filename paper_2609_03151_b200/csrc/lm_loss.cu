@@ -401,22 +401,28 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                     for (int c = 0; c < kStatCols / 32; ++c)
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) m = max3(m, __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
-                    // nothing but the target: distances are infinite.  The rounding of top (2^-24 of some 20) shifts all
-                    // terms alike, by 1e-6 of the sum
-                    const float top = (m == -INFINITY ? 0.f : m) * -p.z_log2;
+                    // Distances are differences first and scaled after: zero for the largest itself and below zero for all others,
+                    // however far from zero the logits lie (v log2e - m log2e in one operation would be off by the rounding of
+                    // m log2e, to either side).  Nothing but the target: distances are infinite
+                    const float base = m == -INFINITY ? 0.f : -m;
+                    const uint64_t base2 = pack_f2(base, base), unit2 = pack_f2(p.z_log2, p.z_log2);
                     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int c = 0; c < kStatCols / 32; ++c) {
                         uint32_t out[16];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float d = fmaf(__uint_as_float(v[c][e]), p.z_log2, top);    // log2 of the term, <= 0
-                            sum[e & 3] += exp2_approx(d);
+                        for (int e = 0; e < 32; e += 2) {
+                            float d[2];            // log2 of the terms, <= 0
+                            unpack_f2(mul2(add2(pack_f2(__uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1])), base2), unit2), d[0], d[1]);
+                            sum[e & 3] += exp2_approx(d[0]);
+                            sum[(e & 3) + 1] += exp2_approx(d[1]);
                             if constexpr (kKind == kLogits) {
                                 // + 2^23: the nearest whole number in the low bits
-                                const uint32_t code = __float_as_uint(fminf(fmaf(d, -kCodeStep, 8388608.f), 8388608.f + kCodeMax));
-                                if (e & 1) out[e / 2] = __byte_perm(out[e / 2], code, 0x5410);
-                                else out[e / 2] = code;
+                                uint32_t code[2];
+#pragma unroll
+                                for (int h = 0; h < 2; ++h)
+                                    code[h] = __float_as_uint(fminf(fmaf(d[h], -kCodeStep, 8388608.f), 8388608.f + kCodeMax));
+                                out[e / 2] = __byte_perm(code[0], code[1], 0x5410);
                             }
                         }
                         if constexpr (kKind == kLogits) {

@@ -166,6 +166,45 @@ def test_weights_of_one_and_confident_predictions(basp):
     assert (np.abs(f64(cat(got[0])) - exact) <= (4 * tz + 2.0 ** -18) * exact).all()
 
 
+def far_from_zero(rows, vocab, seed):
+    """Logits that are exact in fp32 and up to 6e4 off zero, all words of a row alike: x = (+-2^k, 1, 0, ...), a word's first weight is
+    1.171875 for all, its second a multiple of 1/8.  Four words stand above the others, within 2 of one another; labels are elsewhere."""
+    hidden = 64
+    g = torch.Generator().manual_seed(seed)
+    W = torch.zeros((vocab, hidden))
+    W[:, 0] = 1.171875
+    W[:, 1] = torch.randint(-32, 33, (vocab,), generator=g) / 8
+    for i, word in enumerate((7, vocab // 2, vocab // 2 + 1, vocab - 3)):
+        W[word, 1] = 10 + i / 2
+    x = torch.zeros((rows, hidden))
+    x[:, 0] = 2.0 ** (10 + torch.arange(rows) % 6) * (1 - 2 * (torch.arange(rows) // 6 % 2))
+    x[:, 1] = 1 + torch.randint(0, 3, (rows,), generator=g) / 4
+    y = 8 + torch.randint(0, vocab // 2 - 8, (rows,), generator=g)
+    return hidden, W.to(torch.bfloat16), x.to(torch.bfloat16), y, torch.rand(rows, generator=g) + 0.5
+
+
+@pytest.mark.parametrize("rows", [100, 520])           # single CTAs, pairs
+def test_top_words_of_logits_far_from_zero(basp, rows):
+    """A logit's distance below its group's largest is zero for the largest whatever the rounding of large numbers.  Here the
+    logits are exact, so what is left of the tolerances above is dz's 2^-8 + 2^-11 and the log-sum-exp, which is rounded twice
+    at its size: 2 x 2^-24 |lse| of every probability."""
+    vocab = 700
+    hidden, W, x, y, weights = far_from_zero(rows, vocab, 11)
+    pl = make_plan(basp, L("far", 1, 1, rows, hidden, vocab)[0])
+    ref = oracle.lm_loss(f64(x), f64(W), y.numpy(), weights.numpy().astype(np.float64))
+    size = np.abs(ref["lse"]).max()
+    assert size > 3e4 and np.sort(np.abs(ref["dz"]), 1)[:, -3].min() > 0.02
+    loss, lse, dx, dw = run(basp, pl, hidden, vocab, W, [x], [y], [weights])
+    off = 2.0 ** -23 * size
+    assert (np.abs(f64(loss[0]) - ref["loss"]) <= off + 2.0 ** -20 * (1 + ref["loss"])).all()
+    assert (np.abs(f64(lse[0]) - ref["lse"]) <= off + 2.0 ** -20).all()
+    adz, X8, W8 = np.abs(ref["dz"]), f64(x), f64(W)
+    for name, got, want, terms, k in (("dx", dx[0], ref["dx"], adz @ np.abs(W8), vocab), ("dw", dw, ref["dw"], adz.T @ np.abs(X8), rows)):
+        err = np.abs(f64(got) - want)
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -11 + off + (k / 16 + 16) * 2.0 ** -23) * terms + 1e-37
+        assert (err <= tol).all(), (name, float(err.max()), float((err / tol).max()))
+
+
 @pytest.mark.parametrize("rows", [100, 520])           # single CTAs, pairs
 @pytest.mark.parametrize("hidden", [2048, 8192])
 def test_lse_is_not_short_of_what_the_products_cut_off(basp, rows, hidden):
