@@ -527,7 +527,9 @@ gemm_done:
 
 // ------------------------------------------------------------------------------------------------ statistics of the rows
 struct RowInfo {               // what the element-wise pass needs of a row
-    float lse, weight, target_dz;                  // target_dz: without the weight
+    float top, rest;           // lse in two parts, the largest logit besides the target's and the rest: one number would be
+                               // off by its rounding, which is an error of every probability where logits are large
+    float weight, target_dz;   // target_dz: without the weight
     int label;                 // -1: none
 };
 
@@ -610,23 +612,24 @@ __global__ void __launch_bounds__(1024) lm_merge_kernel(const __grid_constant__ 
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) {
-        RowInfo info{0.f, 0.f, 0.f, -1};
+        RowInfo info{0.f, 0.f, 0.f, 0.f, -1};
         if (tok.valid) {
-            const float others = m + logf(s);      // -inf where the target is the only word
-            float loss = 0.f, lse = others;
+            info.top = m == -INFINITY ? 0.f : m;
+            info.rest = logf(s);                   // -inf where the target is the only word
+            float loss = 0.f;
             if (counts) {
-                const float away = others - z, tail = log1pf(expf(-fabsf(away)));
+                // differences of logits first: they stay small where the logits are large
+                const float away = (info.top - z) + info.rest, tail = log1pf(expf(-fabsf(away)));
                 loss = (away > 0.f ? away : 0.f) + tail;
-                lse = (away > 0.f ? others : z) + tail;
+                info.rest = (away > 0.f ? info.rest : z - info.top) + tail;
                 if (p.info) {
                     info.weight = p.weight[tok.rank] ? p.weight[tok.rank][tok.row] : 1.f;
                     info.target_dz = -1.f / (1.f + expf(-away));
                     info.label = (int)label;
                 }
             }
-            info.lse = lse;
             p.loss[tok.rank][tok.row] = loss;
-            if (p.lse[tok.rank]) p.lse[tok.rank][tok.row] = lse;
+            if (p.lse[tok.rank]) p.lse[tok.rank][tok.row] = info.top + info.rest;
         }
         if (p.info) {
             p.info[row] = info;
@@ -689,7 +692,7 @@ __global__ void __launch_bounds__(256) lm_dz_kernel(const __grid_constant__ DzPa
         if (n0 + u >= tiles_n) break;
         uint4 o = make_uint4(0, 0, 0, 0);
         if (info.weight != 0.f) {
-            const float c = (m[u] - info.lse) * kLog2e;
+            const float c = ((m[u] - info.top) - info.rest) * kLog2e;
             const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
             const int target = info.label - ((n0 + u) * 256 + lane * 8);
             uint32_t r[4];

@@ -205,6 +205,29 @@ def test_top_words_of_logits_far_from_zero(basp, rows):
         assert (err <= tol).all(), (name, float(err.max()), float((err / tol).max()))
 
 
+@pytest.mark.parametrize("target", ["elsewhere", "top", "only"])
+@pytest.mark.parametrize("rows", [100, 520])           # single CTAs, pairs
+def test_losses_and_probabilities_do_not_depend_on_the_offset(basp, rows, target):
+    """softmax(z + c) = softmax(z): nothing of the loss or the gradients is rounded at the size of the logits, only lse itself is
+    (half a step, 2^-24 of it).  The label is a word far below the top, one of the top, or the one word far above all others."""
+    vocab = 700
+    hidden, W, x, y, weights = far_from_zero(rows, vocab, 12)
+    if target != "elsewhere":
+        y[:] = vocab // 2
+    if target == "only":
+        W[vocab // 2, 1] = 24
+    pl = make_plan(basp, L("far", 1, 1, rows, hidden, vocab)[0])
+    ref = oracle.lm_loss(f64(x), f64(W), y.numpy(), weights.numpy().astype(np.float64))
+    loss, lse, dx, dw = run(basp, pl, hidden, vocab, W, [x], [y], [weights])
+    assert (np.abs(f64(loss[0]) - ref["loss"]) <= 2.0 ** -20 * (1 + ref["loss"])).all()
+    assert (np.abs(f64(lse[0]) - ref["lse"]) <= 2.0 ** -24 * np.abs(ref["lse"]) + 2.0 ** -19).all()
+    adz, X8, W8 = np.abs(ref["dz"]), f64(x), f64(W)
+    for name, got, want, terms, k in (("dx", dx[0], ref["dx"], adz @ np.abs(W8), vocab), ("dw", dw, ref["dw"], adz.T @ np.abs(X8), rows)):
+        err = np.abs(f64(got) - want)
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -11 + (k / 16 + 16) * 2.0 ** -23) * terms + 1e-37
+        assert (err <= tol).all(), (name, float(err.max()), float((err / tol).max()))
+
+
 @pytest.mark.parametrize("rows", [100, 520])           # single CTAs, pairs
 @pytest.mark.parametrize("hidden", [2048, 8192])
 def test_lse_is_not_short_of_what_the_products_cut_off(basp, rows, hidden):
