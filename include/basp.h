@@ -398,7 +398,10 @@ int basp_layer_bwd_ckpt(const basp_plan *plan, const void *const *ckpt_shards, c
  *   z = x W^T  (w: bf16 [vocab][hidden], shared by all ranks),   lse = ln sum_v exp(z_v),   loss = lse - z_y
  * labels[r]: int64 [Bl*T]; a label outside [0, vocab) (such as -100) marks a token without a loss: its loss is 0 and it has
  * no part in the gradients.  loss_seq[r], lse_seq[r]: fp32 [Bl*T] (lse_seq may be NULL).  bf16 products with fp32 sums; in the
- * loss the logits are not rounded.
+ * loss the logits are not rounded.  The tensor cores cut their sums off towards zero, by some 2^-30 of the sum per product; in lse and
+ * among the words that are not the target the logits of a row are scaled up by 1 + 2^-30 n to make up for it, n: the nonzero
+ * features of x where there are more than 64.  A row that lost nothing (small whole numbers) is off by that: 3.8e-6 of a logit at
+ * 4096 features.  The target's own logit is summed apart, rounded to nearest.
  *
  * basp_lm_loss_grad also writes the gradients of sum_tokens g loss with g = token_weights[r][token] (fp32 [Bl*T]; NULL table:
  * 1 each):  dz = g (softmax(z) - onehot(y)),  dx_seq[r] = dz W (bf16),  dw = sum dz^T x (bf16 [vocab][hidden]; summed in

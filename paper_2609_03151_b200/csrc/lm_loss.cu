@@ -5,6 +5,7 @@
 //   dz = g (softmax(z) - onehot(y)),       dx = dz W,       dW = sum_tokens dz^T x
 //
 // Three products, each 2 rows*vocab*hidden operations on the tensor cores, and one element-wise pass:
+//   (rows)                 every row's nonzero features, see "cut off" below
 //   (1) z = x W^T          epilogue: per row and 128 columns the maximum m and the sum of exp(z - m), the target's logit apart
 //                          from the others; for the gradient also every logit as its distance below that maximum, 16 bits:
 //                          rn((m - z) log2(e) 2^10), saturating at 2^-64 of the maximum's probability
@@ -24,10 +25,14 @@
 // p_y - 1 would cancel for a confident prediction.  dz is kept in units of the largest finite weight of the piece, which the
 // epilogues of (2) and (3) multiply in fp32.
 //
-// The tensor cores cut off what does not fit into their running sum, so a sum of K products comes out short by about 2^-30 K of
-// itself (normal values: 0.96 to 1.04 times that for K of 2048 to 8192; with a drift, outliers or a confident prediction 0.96 to
-// 1.4, products of one sign more).  The logits are scaled up by it, which halves their error (4096 normal values: 4.4e-6 -> 2.2e-6
-// of the logits' size) and takes most of lse's, where nearly equal shares add up (3.9e-6 -> 5e-7).  dx and dw round to bf16.
+// The tensor cores cut off what does not fit into their running sum, towards zero, so a sum of many products comes out short.  By
+// how much depends on the values; measured, in units of 2^-30 of the sum per nonzero feature of x: normal values 0.83 to 1.07
+// (256 to 65536 features), one product in two to ten of them zero 1.5, in ten of 65536 3.2, products of one sign 4 to 6, features a
+// hundred times the others 2 where they come first and 0.04 where they come last, one to four features and small whole numbers none.
+// The logits of a row are therefore scaled up by 1 + 2^-30 n with n its nonzero features (lm_rows_kernel).  For 4096 normal
+// values that halves a logit's error (4.4e-6 -> 2.2e-6 of the logits' size) and takes most of lse's, where nearly equal shares add
+// up (3.9e-6 -> 5e-7); a row of up to 64 features is left as it is, and a dense row that lost nothing is off by 2^-30 n of its
+// logits.  dx and dw round to bf16.
 //
 // Products: persistent, K in blocks of 64 (128-byte-swizzled TMA boxes), a four-stage ring of 48 KiB stages:
 //   warp 0      TMA producer
@@ -104,11 +109,11 @@ struct LossParams {
     Rows rows;
     int tiles_m, tiles_n, k_blocks, splits, group;
     int vocab, hidden;
-    float z_scale, z_log2;     // (1): makes up for what the products cut off; the same times log2(e)
+    const float *cut;          // (1): what the products of each row cut off, as a share of the sum
     bool wide;                 // (2): every row of the result starts on a multiple of 32 bytes
     size_t pitch;              // columns of a row of 16-bit logits
     int piece_rows;
-    float2 *stats;             // [groups of kStatCols columns][piece_rows]: maximum, sum
+    float2 *stats;             // [groups of kStatCols columns][piece_rows]: maximum as the products left it, sum
     unsigned *scale;           // bits of the largest finite |weight| of the piece: dz is in its units, so that equal weights leave
                                // p - 1 as it is (rounding -1 g would be one relative error common to all tokens)
     uint16_t *codes;           // [piece_rows][pitch]
@@ -350,6 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
         const int quarter = warp & 3;                       // the TMEM lanes this warp can reach
         const int row = quarter * 32 + lane;
         const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
+        if constexpr (kKind == kStats || kKind == kLogits) wait_previous_kernel();         // what `cut` comes from; the operands do not
         uint8_t *staging = smem + kStages * kStageBytes + (warp - 2) * kStagingBytes;       // (3)
         uint32_t cnt = 0;
         float scale = 1.f;
@@ -377,6 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                 // the target's column in this tile, or -1
                 const int hit = label >= col0 && label < p.vocab && label < col0 + kCols ? (int)(label - col0) : -1;
                 const bool stored = prow < p.piece_rows;            // not the second half of an odd last tile
+                const float unit = fmaf(kLog2e, stored ? p.cut[prow] : 0.f, kLog2e);       // of a distance
                 LOSS_WAIT(&bars.acc_full[acc], parity, 3, i);
                 tc_fence_after();
                 uint16_t *dst = p.codes + (size_t)prow * p.pitch + col0;
@@ -405,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                     // however far from zero the logits lie (v log2e - m log2e in one operation would be off by the rounding of
                     // m log2e, to either side).  Nothing but the target: distances are infinite
                     const float base = m == -INFINITY ? 0.f : -m;
-                    const uint64_t base2 = pack_f2(base, base), unit2 = pack_f2(p.z_log2, p.z_log2);
+                    const uint64_t base2 = pack_f2(base, base), unit2 = pack_f2(unit, unit);
                     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int c = 0; c < kStatCols / 32; ++c) {
@@ -436,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                     }
                     if (stored)
                         p.stats[(size_t)(col0 / kStatCols + g) * p.piece_rows + prow] =
-                            make_float2(m * p.z_scale, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+                            make_float2(m, (sum[0] + sum[1]) + (sum[2] + sum[3]));
                 }
             } else {
                 const int width = min(kCols, p.hidden - col0);      // a multiple of 8
@@ -527,8 +534,9 @@ gemm_done:
 
 // ------------------------------------------------------------------------------------------------ statistics of the rows
 struct RowInfo {               // what the element-wise pass needs of a row
-    float top, rest;           // lse in two parts, the largest logit besides the target's and the rest: one number would be
-                               // off by its rounding, which is an error of every probability where logits are large
+    float top, rest;           // lse = top (1 + cut) + rest, top: the largest logit besides the target's, as the products left it.  One
+                               // number would be off by its rounding, an error of every probability where logits are large
+    float unit;                // of a distance of two logits in log2, with what the products cut off
     float weight, target_dz;   // target_dz: without the weight
     int label;                 // -1: none
 };
@@ -542,14 +550,45 @@ struct MergeParams {
     Rows rows;
     int groups, piece_rows, vocab, hidden;
     const float2 *stats;
+    const float *cut;
     unsigned *scale;
     RowInfo *info;             // NULL: not wanted
 };
 
-__device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
+// `unit`: of a distance in log2
+__device__ __forceinline__ void join(float &m, float &s, float m2, float s2, float unit) {
     const float top = fmaxf(m, m2), use = top == -INFINITY ? 0.f : top;
-    s = s * exp2f((m - use) * kLog2e) + s2 * exp2f((m2 - use) * kLog2e);
+    s = s * exp2f((m - use) * unit) + s2 * exp2f((m2 - use) * unit);
     m = top;
+}
+
+// What the products with a row cut off, as a share of the sums.  A warp takes a row.
+template <int R>
+struct CutParams {
+    const __nv_bfloat16 *x[R];
+    Rows rows;
+    int hidden;
+    float *cut;
+};
+template <int R>
+__global__ void __launch_bounds__(256) lm_rows_kernel(const __grid_constant__ CutParams<R> p) {
+    const int lane = threadIdx.x & 31, row = blockIdx.x * 8 + (threadIdx.x >> 5);
+    allow_next_kernel();
+    const Token tok = token_of(p.rows, row);
+    int n = 0;
+    if (tok.valid) {
+        const uint4 *x = reinterpret_cast<const uint4 *>(p.x[tok.rank] + (size_t)tok.row * p.hidden);
+#pragma unroll 8
+        for (int c = lane; c < p.hidden / 8; c += 32) {
+            const uint4 u = __ldg(x + c);
+            const uint32_t us[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) n += ((us[q] & 0x7fffu) != 0) + ((us[q] & 0x7fff0000u) != 0);
+        }
+    }
+    n = __reduce_add_sync(0xffffffffu, n);
+    // 64 features: 2^-24, which a sum loses in its own rounding
+    if (lane == 0) p.cut[row] = n > 64 ? (float)n * 0x1p-30f : 0.f;
 }
 
 // A block takes 32 rows.  Its 32 warps share the column groups (neighbouring lanes read neighbouring rows), then each takes one
@@ -587,6 +626,7 @@ __global__ void __launch_bounds__(1024) lm_merge_kernel(const __grid_constant__ 
     {
         const int i = blockIdx.x * 32 + lane;
         float m = -INFINITY, s = 0.f;
+        const float unit = fmaf(kLog2e, p.cut[i], kLog2e);
         constexpr int kBatch = 8;                  // loads in flight
         for (int n0 = warp; n0 < p.groups; n0 += 32 * kBatch) {
             float2 v[kBatch];
@@ -596,7 +636,7 @@ __global__ void __launch_bounds__(1024) lm_merge_kernel(const __grid_constant__ 
                 v[u] = n < p.groups ? p.stats[(size_t)n * p.piece_rows + i] : make_float2(-INFINITY, 0.f);
             }
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) join(m, s, v[u].x, v[u].y);
+            for (int u = 0; u < kBatch; ++u) join(m, s, v[u].x, v[u].y, unit);
         }
         part[warp][lane] = make_float2(m, s);
     }
@@ -608,28 +648,31 @@ __global__ void __launch_bounds__(1024) lm_merge_kernel(const __grid_constant__ 
         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         z += __shfl_xor_sync(0xffffffffu, z, o);
     }
-    s = mine.y * exp2f((mine.x - (m == -INFINITY ? 0.f : m)) * kLog2e);
+    const float cut = p.cut[row], unit = fmaf(kLog2e, cut, kLog2e);
+    s = mine.y * exp2f((mine.x - (m == -INFINITY ? 0.f : m)) * unit);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) {
-        RowInfo info{0.f, 0.f, 0.f, 0.f, -1};
+        RowInfo info{0.f, 0.f, unit, 0.f, 0.f, -1};
         if (tok.valid) {
             info.top = m == -INFINITY ? 0.f : m;
-            info.rest = logf(s);                   // -inf where the target is the only word
-            float loss = 0.f;
+            // lse - top; `back`: of that, what the products cut off top itself
+            const float back = info.top * cut;
+            float loss = 0.f, rest = logf(s) + back;       // -inf where the target is the only word
             if (counts) {
                 // differences of logits first: they stay small where the logits are large
-                const float away = (info.top - z) + info.rest, tail = log1pf(expf(-fabsf(away)));
+                const float away = (info.top - z) + rest, tail = log1pf(expf(-fabsf(away)));
                 loss = (away > 0.f ? away : 0.f) + tail;
-                info.rest = (away > 0.f ? info.rest : z - info.top) + tail;
+                rest = (away > 0.f ? rest : z - info.top) + tail;
                 if (p.info) {
                     info.weight = p.weight[tok.rank] ? p.weight[tok.rank][tok.row] : 1.f;
                     info.target_dz = -1.f / (1.f + expf(-away));
                     info.label = (int)label;
                 }
             }
+            info.rest = rest - back;
             p.loss[tok.rank][tok.row] = loss;
-            if (p.lse[tok.rank]) p.lse[tok.rank][tok.row] = info.top + info.rest;
+            if (p.lse[tok.rank]) p.lse[tok.rank][tok.row] = info.top + rest;
         }
         if (p.info) {
             p.info[row] = info;
@@ -692,7 +735,7 @@ __global__ void __launch_bounds__(256) lm_dz_kernel(const __grid_constant__ DzPa
         if (n0 + u >= tiles_n) break;
         uint4 o = make_uint4(0, 0, 0, 0);
         if (info.weight != 0.f) {
-            const float c = ((m[u] - info.top) - info.rest) * kLog2e;
+            const float c = (m[u] - info.top) * info.unit - info.rest * kLog2e;
             const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
             const int target = info.label - ((n0 + u) * 256 + lane * 8);
             uint32_t r[4];
@@ -800,13 +843,14 @@ int sizes_of(const basp_plan *p, int hidden, int vocab, int piece_rows, Sizes *z
 }
 
 struct Workspace {
-    size_t stats, scale, codes, info, kept, partial, acc, bytes;
+    size_t cut, stats, scale, codes, info, kept, partial, acc, bytes;
 };
 Workspace workspace_of(const Sizes &z, int hidden, int vocab, bool grad) {
     Workspace w{};
     const size_t rows = (size_t)z.piece_tiles * kBM;
     size_t at = 0;
     auto take = [&](size_t n) { const size_t o = at; at += up256(n); return o; };
+    w.cut = take(rows * sizeof(float));
     w.stats = take(rows * z.tiles_v * (kBN / kStatCols) * sizeof(float2));
     if (grad) {
         w.scale = take(sizeof(unsigned));
@@ -848,11 +892,13 @@ int launch_as(const LossParams<R> &prm, cudaStream_t st) {
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = kPair ? 2 : 1; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = kPair ? 2 : 1; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;         // (1) starts under lm_rows_kernel
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = kKind == kStats || kKind == kLogits ? 2 : 1;
     BASP_CUDA_TRY(cudaLaunchKernelEx(&cfg, lm_gemm_kernel<kKind, R, kPair>, prm));
     basp_count_launch(1);
     return BASP_OK;
@@ -894,10 +940,8 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
     prm.status = basp_status_device_ptr();
     if (!prm.status) return BASP_ERR_CUDA;
     prm.rows.slot_log2 = z.slot_log2; prm.rows.per_rank = z.per_rank; prm.rows.K = p->K; prm.rows.M = M; prm.rows.M_last = M_last;
-    prm.z_scale = (float)(1.0 + a.hidden * 0x1p-30);
-    prm.z_log2 = (float)(1.4426950408889634 * (1.0 + a.hidden * 0x1p-30));
     prm.vocab = a.vocab; prm.hidden = a.hidden; prm.pitch = z.pitch; prm.piece_rows = rows;
-    prm.stats = (float2 *)(a.ws + w.stats); prm.scale = (unsigned *)(a.ws + w.scale);
+    prm.cut = (const float *)(a.ws + w.cut); prm.stats = (float2 *)(a.ws + w.stats); prm.scale = (unsigned *)(a.ws + w.scale);
     prm.codes = (uint16_t *)(a.ws + w.codes); prm.partial = (float *)(a.ws + w.partial);
     for (int r = 0; r < p->N; ++r) {
         prm.label[r] = a.labels[r];
@@ -909,7 +953,7 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
         merge.lse[r] = a.lse ? a.lse[r] : nullptr;
     }
     merge.groups = z.tiles_v * (kBN / kStatCols); merge.piece_rows = rows; merge.vocab = a.vocab;
-    merge.stats = prm.stats; merge.scale = prm.scale; merge.hidden = a.hidden; merge.w = (const __nv_bfloat16 *)a.w;
+    merge.stats = prm.stats; merge.cut = prm.cut; merge.scale = prm.scale; merge.hidden = a.hidden; merge.w = (const __nv_bfloat16 *)a.w;
     merge.info = grad ? (RowInfo *)(a.ws + w.info) : nullptr;
     CUtensorMap w_k[2], w_mn, dz_k, dz_mn;     // w_k: of a single CTA, of a pair's
     for (int r = 0; r < p->N; ++r) {
@@ -924,6 +968,10 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
         if (a.dw) BASP_TRY(tmap::encode_rows_heads_d(&prm.dw, a.dw, a.vocab, 1, a.hidden, 32));
         BASP_TRY(tmap::encode_rows_heads_d(&prm.kept, a.ws + w.kept, rows, 1, a.hidden, kBK));
     }
+    CutParams<R> cut;
+    memset(&cut, 0, sizeof(cut));
+    for (int r = 0; r < p->N; ++r) cut.x[r] = (const __nv_bfloat16 *)a.x[r];
+    cut.hidden = a.hidden; cut.cut = (float *)(a.ws + w.cut);
     bool wide_dx = a.hidden % 16 == 0;
     for (int r = 0; a.dx && r < p->N; ++r) wide_dx = wide_dx && (uintptr_t)a.dx[r] % 32 == 0;
     DzParams<R> dz;
@@ -936,7 +984,10 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
         const int per_tile = kBM >> z.slot_log2;
         prm.rows.slot_begin = tile0 * per_tile;
         prm.rows.slots = z.slots - prm.rows.slot_begin < tiles * per_tile ? z.slots - prm.rows.slot_begin : tiles * per_tile;
-        merge.rows = prm.rows;
+        merge.rows = prm.rows; cut.rows = prm.rows;
+        lm_rows_kernel<R><<<tiles * kBM / 8, 256, 0, st>>>(cut);
+        BASP_CUDA_TRY(cudaGetLastError());
+        basp_count_launch(1);
         // (1)
         prm.tiles_n = z.tiles_v; prm.splits = 1; prm.k_blocks = cdiv(a.hidden, kBK);
         prm.w = w_k[use_pair(tiles * kBM)];

@@ -246,6 +246,46 @@ def test_lse_is_not_short_of_what_the_products_cut_off(basp, rows, hidden):
     assert short <= 2.0 ** -31 * hidden * spread.mean().item() + 2.0 ** -21, short
 
 
+@pytest.mark.parametrize("rows", [100, 520])           # single CTAs, pairs
+@pytest.mark.parametrize("hidden,features", [(4096, 1), (4096, 16), (65536, 2), (65536, 16)])
+def test_rows_of_few_features_are_exact(basp, hidden, features, rows):
+    """Rows of x with few features other than zero lose nothing in the products: logits (up to 60) exact in fp32, so the loss and
+    lse have the statistics' errors alone."""
+    w, hidden, vocab = L("few", 1, 1, rows, hidden, 500)
+    pl = make_plan(basp, w)
+    g = torch.Generator().manual_seed(hidden + features)
+    at = torch.rand((rows, hidden), generator=g).topk(features, 1).indices
+    x = torch.zeros((rows, hidden)).scatter_(1, at, 2.0 ** torch.randint(-1, 2, (rows, features), generator=g).float())
+    W = torch.randint(-32, 33, (vocab, hidden), generator=g) / 8 * (4.0 if features == 1 else 1.0)
+    x, W = x.to(torch.bfloat16), W.to(torch.bfloat16)
+    y = torch.randint(0, vocab, (rows,), generator=g)
+    y[::7] = -100
+    ref = oracle.lm_loss(f64(x), f64(W), y.numpy(), np.ones(rows))
+    assert ref["lse"].max() > 8
+    loss, lse, _, _ = run(basp, pl, hidden, vocab, W, [x], [y], None, dw=False)
+    for got, want in ((loss, ref["loss"]), (lse, ref["lse"])):
+        err = np.abs(f64(got[0]) - want)
+        assert (err <= 2.0 ** -20 * (1 + np.abs(ref["lse"]))).all(), float(err.max())
+
+
+@pytest.mark.parametrize("features", [512, 2048])
+def test_what_is_made_up_for_goes_by_the_features_of_the_row(basp, features):
+    """As test_lse_is_not_short_of_what_the_products_cut_off, on rows whose features behind the first ones are zero: the shortfall is
+    that of the shorter sum, in every rank's rows."""
+    w, hidden, vocab = L("padded", 2, 1, 200, 8192, 4096)
+    pl = make_plan(basp, w)
+    W, x, labels, weights = inputs(pl, hidden, vocab, 9, sure=0.0)
+    for t in x:
+        t[:, features:] = 0.0
+        t.mul_(2.0 if features == 2048 else 4.0)            # logits of about unit size again, an exact factor
+    z = cat(x).cuda().double() @ W.cuda().double().T
+    exact = torch.logsumexp(z, -1)
+    spread = (torch.softmax(z, -1) * z).sum(-1)
+    _, lse, _, _ = run(basp, pl, hidden, vocab, W, x, labels, weights, dw=False)
+    short = (exact - cat(lse).double()).mean().abs().item()
+    assert short <= 2.0 ** -31 * features * spread.mean().item() + 2.0 ** -21, short
+
+
 def test_special_rows_and_words(basp):
     """Infinities and NaN: a row that has them is NaN and no other row is; a row without a label or a weight leaves the
     gradients alone; a word whose weights make its logit -inf has probability zero."""
