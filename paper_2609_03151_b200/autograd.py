@@ -131,10 +131,11 @@ def basp_qk_norm_rope(plan, q_seq, k_seq, w_q, w_k, rope_cos, rope_sin, eps: flo
 
 class _LmLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, plan, labels, token_weights, piece_rows, w, *x_seq):
+    def forward(ctx, plan, labels, token_weights, piece_rows, grads, w, *x_seq):
         vocab, hidden = w.shape
         dev = w.device
-        want_w, want_x = ctx.needs_input_grad[4], any(ctx.needs_input_grad[5:])
+        # needs_input_grad goes by requires_grad alone; `grads`: whether there will be a backward at all
+        want_w, want_x = grads and ctx.needs_input_grad[5], grads and any(ctx.needs_input_grad[6:])
         loss = [torch.empty(t.shape[:-1], dtype=torch.float32, device=dev) for t in x_seq]
         dx = [torch.empty_like(t) for t in x_seq] if want_x else None
         dw = torch.empty_like(w) if want_w else None
@@ -163,7 +164,7 @@ class _LmLoss(torch.autograd.Function):
         saved = list(ctx.saved_tensors)
         want_w, want_x = ctx.want
         dw = saved.pop(0) * d_loss if want_w else None
-        return (None, None, None, None, dw, *((t * d_loss for t in saved) if want_x else [None] * ctx.n))
+        return (None, None, None, None, None, dw, *((t * d_loss for t in saved) if want_x else [None] * ctx.n))
 
 
 def basp_lm_loss(plan, x_seq, w, labels, token_weights=None, piece_rows: int = 0):
@@ -172,7 +173,8 @@ def basp_lm_loss(plan, x_seq, w, labels, token_weights=None, piece_rows: int = 0
     differentiable in x_seq and w.  labels: int64 shards, a value outside [0, vocab) marks a token without a loss;
     token_weights: fp32 shards or None (1 each), for a mean 1 / (number of tokens with a label); not differentiable.
     The gradients are formed together with the loss (they need the same products) and kept for the backward, which
-    scales them by the incoming gradient."""
+    scales them by the incoming gradient; under torch.no_grad() or inference_mode() the loss alone is computed."""
     if token_weights is not None and any(t.requires_grad for t in token_weights):
         raise ValueError("token_weights are not differentiable")
-    return _LmLoss.apply(plan, list(labels), None if token_weights is None else list(token_weights), int(piece_rows), w, *x_seq)
+    return _LmLoss.apply(plan, list(labels), None if token_weights is None else list(token_weights), int(piece_rows),
+                         torch.is_grad_enabled(), w, *x_seq)

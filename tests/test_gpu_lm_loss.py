@@ -433,3 +433,30 @@ def test_the_weight_of_a_token_without_a_label_has_no_part(basp):
         grads.append((loss.detach(), *torch.autograd.grad(loss, [*xl, wl])))
     assert all(torch.isfinite(t).all().item() for t in grads[0])
     assert all(torch.equal(a, b) for other in grads[1:] for a, b in zip(grads[0], other))
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_an_evaluation_computes_the_loss_alone(basp, mode):
+    """Without a backward to come there are no gradients, whatever the head's requires_grad: the launches are those of
+    basp_lm_loss_fwd, and nothing of the gradients' size is allocated."""
+    from paper_2609_03151_b200.autograd import basp_lm_loss
+    w, hidden, vocab = L("eval", 2, 1, 300, 256, 20000)
+    pl = make_plan(basp, w)
+    W, x, labels, weights = inputs(pl, hidden, vocab, 10)
+    c = lambda ts: [t.cuda() for t in ts]
+    xl, wl, yl, gl = [t.requires_grad_() for t in c(x)], W.cuda().requires_grad_(), c(labels), c(weights)
+    loss = basp_lm_loss(pl, xl, wl, yl, gl)
+    out = [torch.empty(t.shape[0], device="cuda") for t in x]
+    ws = torch.empty(basp.basp_lm_loss_fwd_workspace_bytes(pl, vocab), dtype=torch.uint8, device="cuda")
+    before = basp.basp_launch_count()
+    basp.basp_lm_loss_fwd(pl, hidden, vocab, [t.detach() for t in xl], wl.detach(), yl, out, None, ws)
+    alone = basp.basp_launch_count() - before
+    del ws
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    held, before = torch.cuda.memory_allocated(), basp.basp_launch_count()
+    with mode():
+        value = basp_lm_loss(pl, xl, wl, yl, gl)
+    assert basp.basp_launch_count() - before == alone
+    assert torch.cuda.max_memory_allocated() - held < wl.numel() * 2
+    assert torch.equal(value, loss) and not value.requires_grad
