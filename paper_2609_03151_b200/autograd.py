@@ -29,7 +29,7 @@ from . import binding
 
 class _BaspAttention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, plan, softmax_scale, fused, checkpoint8, *shards):
+    def forward(ctx, plan, softmax_scale, fused, checkpoint8, grads, *shards):
         n = plan.N
         if checkpoint8 and not fused:
             raise ValueError("checkpoint8 goes with fused=True (the other form keeps its head-sharded copies)")
@@ -46,10 +46,10 @@ class _BaspAttention(torch.autograd.Function):
             binding.basp_layer_fwd_fused(plan, list(q_seq), list(k_seq), list(v_seq), o_seq, lse, softmax_scale=softmax_scale)
             ws = None
             ctx.ckpt = None
-            if checkpoint8:
+            if checkpoint8 and grads and any(ctx.needs_input_grad):
                 ctx.ckpt = [torch.empty(binding.basp_ckpt_bytes(plan, r), dtype=torch.uint8, device=dev) for r in range(n)]
                 binding.basp_ckpt_pack(plan, q_seq, k_seq, v_seq, o_seq, ctx.ckpt)
-            else:
+            elif not checkpoint8:
                 ctx.save_for_backward(*shards, *o_seq)
         else:
             ws = torch.empty(binding.basp_workspace_bytes(plan), dtype=torch.uint8, device=dev)
@@ -70,26 +70,27 @@ class _BaspAttention(torch.autograd.Function):
             ws2 = torch.empty(binding.basp_layer_bwd_seq_workspace_bytes(plan), dtype=torch.uint8, device=dev)
             binding.basp_layer_bwd_ckpt(plan, ctx.ckpt, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:], ws2,
                                         softmax_scale=ctx.softmax_scale)
-            return (None, None, None, None, *grads)
+            return (None, None, None, None, None, *grads)
         if ctx.fused:
             saved = ctx.saved_tensors
             q_seq, k_seq, v_seq, o_seq = (list(saved[i * n:(i + 1) * n]) for i in range(4))
             ws2 = torch.empty(binding.basp_layer_bwd_seq_workspace_bytes(plan), dtype=torch.uint8, device=dev)
             binding.basp_layer_bwd_seq(plan, q_seq, k_seq, v_seq, o_seq, ctx.lse, do_seq, grads[:n], grads[n:2 * n],
                                        grads[2 * n:], ws2, softmax_scale=ctx.softmax_scale)
-            return (None, None, None, None, *grads)
+            return (None, None, None, None, None, *grads)
         qh, kh, vh, oh = (binding.as_shards(a) for a in binding.basp_layer_workspace_shards(plan, ctx.ws))
         ws2 = torch.empty(binding.basp_layer_bwd_workspace_bytes(plan), dtype=torch.uint8, device=dev)
         binding.basp_layer_bwd(plan, qh, kh, vh, oh, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:], ws2,
                                softmax_scale=ctx.softmax_scale)
-        return (None, None, None, None, *grads)
+        return (None, None, None, None, None, *grads)
 
 
 def basp_attention(plan, q_seq, k_seq, v_seq, softmax_scale: float = 0.0, fused: bool = False, checkpoint8: bool = False):
     """Causal (or, per the plan, unmasked) attention over the group-sharded sequences of `plan`: the two group-local
     all-to-alls and the attention of Section IV-C, differentiable.  Returns the list of n_ranks output shards in the
     layout of q_seq.  checkpoint8 (with fused): keep Q, K, V and O in 8 bits for the backward."""
-    return list(_BaspAttention.apply(plan, float(softmax_scale), bool(fused), bool(checkpoint8), *q_seq, *k_seq, *v_seq))
+    return list(_BaspAttention.apply(plan, float(softmax_scale), bool(fused), bool(checkpoint8), torch.is_grad_enabled(), *q_seq,
+                                     *k_seq, *v_seq))
 
 
 class _QkNormRope(torch.autograd.Function):

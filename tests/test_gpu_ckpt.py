@@ -190,3 +190,28 @@ def test_layer_backward_from_checkpoints(basp, w, autograd):
         for a, b, c in zip(got, ref, several):
             err = np.abs(f64(a).reshape(b.shape) - b)
             assert (err <= 2e-2 + 2.0 ** -8 * (np.abs(b) + c)).all(), (w.name, name, float(err.max()))
+
+
+@pytest.mark.parametrize("mode", ["no_grad", "inference_mode", "no leaf"])
+def test_an_evaluation_packs_no_checkpoints(basp, mode):
+    """Where no backward will come, the layer with checkpoint8 is the fused forward alone."""
+    from contextlib import nullcontext
+
+    from paper_2609_03151_b200.autograd import basp_attention
+    w = synth.Workload("eval", N=4, B=2, S=512, Hq=4, Hkv=2, D=64)
+    pl = make_plan(basp, w)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v = ([torch.randn((pl.Bl, pl.T, h, w.D), generator=g, device="cuda").to(torch.bfloat16) for _ in range(4)]
+               for h in (w.Hq, w.Hkv, w.Hkv))
+    basp.basp_clear_status()
+    before = basp.basp_launch_count()
+    plain = basp_attention(pl, q, k, v, fused=True)
+    alone = basp.basp_launch_count() - before
+    if mode != "no leaf":
+        q, k, v = ([t.clone().requires_grad_() for t in ts] for ts in (q, k, v))
+    with nullcontext() if mode == "no leaf" else getattr(torch, mode)():
+        before = basp.basp_launch_count()
+        out = basp_attention(pl, q, k, v, fused=True, checkpoint8=True)
+    basp.basp_get_status()
+    assert basp.basp_launch_count() - before == alone
+    assert all(torch.equal(a, b) for a, b in zip(plain, out))
