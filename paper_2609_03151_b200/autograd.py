@@ -60,6 +60,7 @@ class _BaspAttention(torch.autograd.Function):
         return tuple(o_seq)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, *do_seq):
         plan, n = ctx.plan, ctx.plan.N
         dev = ctx.lse[0].device

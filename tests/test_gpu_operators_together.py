@@ -230,3 +230,25 @@ def test_second_derivatives_are_refused(basp):
     (dx,) = torch.autograd.grad(loss, x, create_graph=True)
     with pytest.raises(RuntimeError):
         dx.float().sum().backward()
+
+
+@pytest.mark.parametrize("op", ["attention", "attention fused", "attention checkpoint8", "head norms"])
+def test_no_second_derivative_is_lost(basp, op):
+    """The gradients carry no graph of their own: asking for one through them is refused, and not answered with the other paths'
+    terms alone (here a penalty on the gradient beside the loss itself)."""
+    from paper_2609_03151_b200.autograd import basp_attention, basp_qk_norm_rope
+    pl = basp.basp_plan_create(2, 1, 256, 2, 2, 64)           # 128 tokens per rank: the fused form's unit
+    g = torch.Generator(device="cuda").manual_seed(6)
+    leaves = [normal(g, 128, 2, 64).requires_grad_() for _ in range(6)]
+    one = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    tables = [t.t().contiguous().cuda() for t in synth.rope_tables(256, 64)]
+
+    def call(x):
+        if op == "head norms":
+            return sum(basp_qk_norm_rope(pl, x[:2], x[2:4], one, one, *tables), [])
+        return basp_attention(pl, x[:2], x[2:4], x[4:], fused=op != "attention", checkpoint8="8" in op)
+    x = [t * 1.5 for t in leaves]                          # a graph of its own in front of the operation
+    loss = sum(t.float().square().sum() for t in call(x))
+    (dx,) = torch.autograd.grad(loss, leaves[0], create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (dx.float().square().sum() + loss).backward()
