@@ -45,17 +45,17 @@ class _BaspAttention(torch.autograd.Function):
         if fused:
             binding.basp_layer_fwd_fused(plan, list(q_seq), list(k_seq), list(v_seq), o_seq, lse, softmax_scale=softmax_scale)
             ws = None
-            ctx.ckpt = None
             if checkpoint8 and grads and any(ctx.needs_input_grad):
-                ctx.ckpt = [torch.empty(binding.basp_ckpt_bytes(plan, r), dtype=torch.uint8, device=dev) for r in range(n)]
-                binding.basp_ckpt_pack(plan, q_seq, k_seq, v_seq, o_seq, ctx.ckpt)
+                ckpt = [torch.empty(binding.basp_ckpt_bytes(plan, r), dtype=torch.uint8, device=dev) for r in range(n)]
+                binding.basp_ckpt_pack(plan, q_seq, k_seq, v_seq, o_seq, ckpt)
+                ctx.save_for_backward(*ckpt)
             elif not checkpoint8:
                 ctx.save_for_backward(*shards, *o_seq)
         else:
             ws = torch.empty(binding.basp_workspace_bytes(plan), dtype=torch.uint8, device=dev)
             binding.basp_layer_fwd(plan, list(q_seq), list(k_seq), list(v_seq), o_seq, ws, lse_shards=lse,
                                    softmax_scale=softmax_scale)
-        ctx.plan, ctx.softmax_scale, ctx.ws, ctx.lse, ctx.fused = plan, softmax_scale, ws, lse, fused
+        ctx.plan, ctx.softmax_scale, ctx.ws, ctx.lse, ctx.fused, ctx.checkpoint8 = plan, softmax_scale, ws, lse, fused, checkpoint8
         ctx.shapes = [t.shape for t in shards]
         return tuple(o_seq)
 
@@ -67,9 +67,9 @@ class _BaspAttention(torch.autograd.Function):
         do_seq = [torch.zeros(s, dtype=torch.bfloat16, device=dev) if g is None else g.contiguous()
                   for g, s in zip(do_seq, ctx.shapes)]
         grads = [torch.empty(s, dtype=torch.bfloat16, device=dev) for s in ctx.shapes]
-        if ctx.fused and ctx.ckpt is not None:
+        if ctx.checkpoint8:
             ws2 = torch.empty(binding.basp_layer_bwd_seq_workspace_bytes(plan), dtype=torch.uint8, device=dev)
-            binding.basp_layer_bwd_ckpt(plan, ctx.ckpt, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:], ws2,
+            binding.basp_layer_bwd_ckpt(plan, ctx.saved_tensors, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:], ws2,
                                         softmax_scale=ctx.softmax_scale)
             return (None, None, None, None, None, *grads)
         if ctx.fused:

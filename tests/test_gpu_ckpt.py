@@ -215,3 +215,36 @@ def test_an_evaluation_packs_no_checkpoints(basp, mode):
     basp.basp_get_status()
     assert basp.basp_launch_count() - before == alone
     assert all(torch.equal(a, b) for a, b in zip(plain, out))
+
+
+def test_checkpoints_are_saved_tensors(basp):
+    """Saved-tensor hooks (offloading between the passes) see the checkpoints and nothing of the shards in bf16; a backward from
+    what they give back has the gradients of one without them.  dK and dV bit for bit, dQ comes from a reduction in whatever order its blocks
+    finish (fp32, rounded to bf16: neighbours at most)."""
+    from paper_2609_03151_b200.autograd import basp_attention
+    w = synth.Workload("hooks", N=4, B=2, S=512, Hq=4, Hkv=2, D=64)
+    pl = make_plan(basp, w)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v, do = ([torch.randn((pl.Bl, pl.T, h, w.D), generator=g, device="cuda").to(torch.bfloat16) for _ in range(4)]
+                   for h in (w.Hq, w.Hkv, w.Hkv, w.Hq))
+    seen, grads = [], []
+
+    def away(t):
+        seen.append((t.dtype, t.numel()))
+        return t.cpu()
+    for hooks in (False, True):
+        leaves = [[t.clone().requires_grad_() for t in ts] for ts in (q, k, v)]
+        basp.basp_clear_status()
+        if hooks:
+            with torch.autograd.graph.saved_tensors_hooks(away, lambda t: t.cuda()):
+                out = basp_attention(pl, *leaves, fused=True, checkpoint8=True)
+        else:
+            out = basp_attention(pl, *leaves, fused=True, checkpoint8=True)
+        torch.autograd.backward(out, do)
+        basp.basp_get_status()
+        grads.append([[t.grad for t in ts] for ts in leaves])
+    assert seen == [(torch.uint8, basp.basp_ckpt_bytes(pl, r)) for r in range(4)]
+    for a, b in zip(*(x[0] for x in grads)):
+        assert ((a.float() - b.float()).abs() <= 2.0 ** -7 * b.float().abs() + 1e-6).all()
+    for i in (1, 2):
+        assert all(torch.equal(a, b) for a, b in zip(grads[0][i], grads[1][i]))
