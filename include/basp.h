@@ -410,8 +410,9 @@ int basp_layer_bwd_ckpt(const basp_plan *plan, const void *const *ckpt_shards, c
  * product out.  A token of weight 0 has no part in the gradients, NaN among its values or not; a weight that is no finite
  * number reaches its own dx and dw only.  Both gradients are written, not added to; the same inputs and piece_rows give the
  * same bits.
- * The rows are worked on in pieces of piece_rows (rounded up to 128; 0: 8192; at most 32768), 2 bytes per logit of one piece
- * in the workspace, plus 4 vocab hidden bytes for the running sum of dw where there are several pieces.
+ * The rows are worked on in pieces of piece_rows (rounded up to 128; 0: 8192; at most 32768).  The workspace holds of one piece
+ * 2 bytes per logit and 8 per 128 logits, its rows of x, and where its rows are too few to fill the GPU up to 768 MB of partial
+ * sums of dx; where there are several pieces, 4 vocab hidden bytes for the running sum of dw besides.
  * Requires hidden a multiple of 8 up to 65536 and vocab up to 2^24 (BASP_ERR_UNSUPPORTED; neither positive:
  * BASP_ERR_INVALID); labels 8-byte aligned, the fp32 arrays 4-byte.  The size queries return 0 for what the call refuses. */
 int basp_lm_loss_fwd(const basp_plan *plan, int hidden, int vocab, const void *const *x_seq, const void *w,

@@ -117,7 +117,8 @@ struct LossParams {
     unsigned *scale;           // bits of the largest finite |weight| of the piece: dz is in its units, so that equal weights leave
                                // p - 1 as it is (rounding -1 g would be one relative error common to all tokens)
     uint16_t *codes;           // [piece_rows][pitch]
-    float *partial;            // (2) with splits > 1: [splits][piece_rows][hidden]
+    float *partial;            // (2) with splits > 1: [splits][partial_rows][hidden]
+    int partial_rows;          // the rows of this piece, which may be fewer than piece_rows
     const float *acc_in;       // (3) sum of the earlier pieces, or NULL
     float *acc_out;            // (3) sum so far, or NULL: the result
     int *status;
@@ -466,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                         if (p.splits == 1) {
                             store_bf16x32(p.dx[tok.rank] + (size_t)tok.row * p.hidden + col0 + c * 32, v, cols, p.wide);
                         } else {
-                            float *dst = p.partial + ((size_t)t.split * p.piece_rows + prow) * p.hidden + col0 + c * 32;
+                            float *dst = p.partial + ((size_t)t.split * p.partial_rows + prow) * p.hidden + col0 + c * 32;
 #pragma unroll
                             for (int q = 0; q < 8; ++q)
                                 if (4 * q < cols) *reinterpret_cast<float4 *>(dst + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
@@ -762,7 +763,7 @@ struct JoinParams {
     __nv_bfloat16 *dx[R];
     Rows rows;
     const float *partial;
-    int splits, piece_rows, hidden;
+    int splits, partial_rows, hidden;
 };
 template <int R>
 __global__ void __launch_bounds__(256) lm_dx_join_kernel(const __grid_constant__ JoinParams<R> p) {
@@ -770,12 +771,12 @@ __global__ void __launch_bounds__(256) lm_dx_join_kernel(const __grid_constant__
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     const int row = (int)(i / per_row), c = (int)(i - (long long)row * per_row) * 8;
     wait_previous_kernel();
-    if (row >= p.piece_rows) return;
+    if (row >= p.partial_rows) return;
     const Token tok = token_of(p.rows, row);
     if (!tok.valid) return;
     float s[8] = {};
     for (int k = 0; k < p.splits; ++k) {
-        const float4 *src = reinterpret_cast<const float4 *>(p.partial + ((size_t)k * p.piece_rows + row) * p.hidden + c);
+        const float4 *src = reinterpret_cast<const float4 *>(p.partial + ((size_t)k * p.partial_rows + row) * p.hidden + c);
         const float4 a = src[0], b = src[1];
         s[0] += a.x; s[1] += a.y; s[2] += a.z; s[3] += a.w; s[4] += b.x; s[5] += b.y; s[6] += b.z; s[7] += b.w;
     }
@@ -858,10 +859,11 @@ Workspace workspace_of(const Sizes &z, int hidden, int vocab, bool grad) {
         w.info = take(rows * sizeof(RowInfo));
         w.kept = take(rows * hidden * 2);
         const int last = z.tiles_m - (z.pieces - 1) * z.piece_tiles, kb = cdiv(vocab, kBK);
-        size_t partial = 0;                        // both sizes of piece; the sums of a split lie a whole piece apart
+        size_t partial = 0;                        // both sizes of piece, each with its own rows and splits
         for (int tiles : {z.piece_tiles, last}) {
             const int s = dx_splits(tiles, z.tiles_h, kb, hidden);
-            if (s > 1 && (size_t)s * rows * hidden * 4 > partial) partial = (size_t)s * rows * hidden * 4;
+            const size_t bytes = s > 1 ? (size_t)s * tiles * kBM * hidden * 4 : 0;
+            if (bytes > partial) partial = bytes;
         }
         w.partial = take(partial);
         w.acc = take(z.pieces > 1 ? (size_t)vocab * hidden * 4 : 0);
@@ -1006,11 +1008,12 @@ int run(const basp_plan *p, const Args &a, const Sizes &z, const Workspace &w, b
             prm.dz = dz_k;
             prm.tiles_n = z.tiles_h; prm.k_blocks = cdiv(a.vocab, kBK); prm.wide = wide_dx;
             prm.splits = dx_splits(tiles, z.tiles_h, prm.k_blocks, a.hidden);
+            prm.partial_rows = tiles * kBM;
             BASP_TRY((launch_gemm<kDx, R>(prm, tiles * kBM, st)));
             if (prm.splits > 1) {
                 JoinParams<R> join;
                 memcpy(join.dx, prm.dx, sizeof(join.dx));
-                join.rows = prm.rows; join.partial = prm.partial; join.splits = prm.splits; join.piece_rows = rows; join.hidden = a.hidden;
+                join.rows = prm.rows; join.partial = prm.partial; join.splits = prm.splits; join.partial_rows = prm.partial_rows; join.hidden = a.hidden;
                 BASP_CUDA_TRY(launch_early(lm_dx_join_kernel<R>, dim3(cdiv((long long)tiles * kBM * (a.hidden / 8), 256)), 256, st, join));
                 basp_count_launch(1);
             }

@@ -152,6 +152,21 @@ def test_loss_workspace_sizes(basp, plan):
     assert basp.basp_lm_loss_fwd_workspace_bytes(big, 128256) < 64 << 20
 
 
+@pytest.mark.parametrize("rows,hidden,vocab", [(524416, 8192, 128256), (516224, 1024, 32000), (8193, 4096, 128256), (2043, 2560, 50257)])
+def test_loss_workspace_is_what_the_header_says(basp, rows, hidden, vocab):
+    """A short last piece splits its vocabulary often; its partial sums have its own rows, not a whole piece's."""
+    pl = basp.basp_plan_create(1, 1, rows, 8, 8, 64)
+    up = lambda n, m: (n + m - 1) // m * m
+    piece = min(up(rows, 128), 8192)
+    logits = piece * up(vocab, 256)
+    several = rows > 8192
+    least = logits * 2 + logits // 16 + piece * hidden * 2 + several * vocab * hidden * 4
+    got = basp.basp_lm_loss_grad_workspace_bytes(pl, hidden, vocab)
+    # 36 bytes a row for statistics of rows, sections on multiples of 256 bytes; several pieces share the rows evenly
+    assert got <= least + 768e6 + piece * 36 + 8 * 256
+    assert got >= least * (0.5 if several else 1.0)
+
+
 def test_binding_refuses_tensors_it_would_misread(basp, plan):
     q = [torch.zeros((512, 8, 64), dtype=torch.bfloat16) for _ in range(N)]
     with pytest.raises(ValueError, match="q_seq"):
