@@ -460,3 +460,17 @@ def test_an_evaluation_computes_the_loss_alone(basp, mode):
     assert basp.basp_launch_count() - before == alone
     assert torch.cuda.max_memory_allocated() - held < wl.numel() * 2
     assert torch.equal(value, loss) and not value.requires_grad
+
+
+def test_weights_far_apart(basp):
+    """Weights down to 2^-100 of the largest keep their token's dx to the same share of itself: of dz only what is below 2^-26 of a row's
+    largest passes into numbers of fewer bits."""
+    w, hidden, vocab = L("apart", 1, 1, 96, 128, 900)
+    pl = make_plan(basp, w)
+    W, x, labels, _ = inputs(pl, hidden, vocab, 13)
+    labels = [torch.where((y < 0) | (y >= vocab), 5, y) for y in labels]
+    weights = [2.0 ** -torch.tensor([0.0, 40.0, 80.0, 100.0]).repeat(24)]
+    ref = oracle.lm_loss(f64(x[0]), f64(W), labels[0].numpy(), weights[0].numpy().astype(np.float64))
+    _, _, dx, _ = run(basp, pl, hidden, vocab, W, x, labels, weights)
+    off = np.linalg.norm(f64(dx[0]) - ref["dx"], axis=1)
+    assert (off <= 2.0 ** -7 * np.linalg.norm(ref["dx"], axis=1)).all()       # one row: two roundings at most, 2^-8 each
