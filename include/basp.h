@@ -371,7 +371,7 @@ int basp_qk_norm_rope_bwd(const basp_plan *plan, const void *const *q_seq, const
 size_t basp_qk_norm_rope_bwd_workspace_bytes(const basp_plan *plan);
 
 /* ---- what the layer's backward pass needs (Q, K, V, O, sequence-sharded) kept in 8 bits between the passes: about half
- * the memory of the bf16 shards.  Per head vector x[D]:
+ * the memory of the bf16 shards (O is memory on top where an output projection's backward keeps it in bf16).  Per head vector x[D]:
  *   scale = max|x| / 127,   code = round_half_even(x (127 / max|x|)),   brought back as bf16(code scale)
  * (fp32 arithmetic), so an element is off by at most scale / 2 plus the rounding to bf16.  A vector that holds an infinity or
  * a NaN comes back as NaN in all its elements; one whose max|x| is below 2^-100 as zeros.

@@ -15,9 +15,9 @@
 //   (2) dx = dz W          split over the vocabulary where there are too few row tiles for all SMs (fp32 partial sums, joined by
 //                          one more pass)
 //   (3) dW = dz^T x        K = the piece's rows; with several pieces the sum is carried in fp32
-// Tensor-bound for many rows: 8192 rows of 4096 features against 128256 words take 19.7 ms (1308 TFLOP/s, at the power limit; the
-// three products alone by cuBLAS 18.6 ms), of which dz takes 0.62 (4.2 GB, HBM-bound).  Few rows: bound by reading W twice and
-// writing dW.  Rows are worked on in pieces (default 8192), so what lies between the products is 2 bytes per logit of one piece.
+// Tensor-bound for many rows: 8192 rows of 4096 features against 128256 words take 19.3 to 20.1 ms (1280 to 1337 TFLOP/s, at the power
+// limit; the three products alone by cuBLAS 18.6 ms), of which dz takes 0.62 (4.2 GB, HBM-bound).  Several pieces: 1260 TFLOP/s, for
+// the fp32 sum of dW.  Few rows: bound by reading W twice and writing dW (48 rows against 32000 words: 161 us on the GPU).  Rows are worked on in pieces (default 8192), so what lies between the products is 2 bytes per logit of one piece.
 //
 // Roundings.  A distance is off by at most 2^-11 in log2, so a probability by 2^-11 ln 2 = 3.4e-4, before it is rounded to bf16
 // (2^-8) as an operand: 16 bits do for what would otherwise be an fp32 logit, twice the memory and traffic.  The target is left out of
@@ -27,8 +27,9 @@
 //
 // The tensor cores cut off what does not fit into their running sum, towards zero, so a sum of many products comes out short.  By
 // how much depends on the values; measured, in units of 2^-30 of the sum per nonzero feature of x: normal values 0.83 to 1.07
-// (256 to 65536 features), one product in two to ten of them zero 1.5, in ten of 65536 3.2, products of one sign 4 to 6, features a
-// hundred times the others 2 where they come first and 0.04 where they come last, one to four features and small whole numbers none.
+// (256 to 65536 features), half or nine tenths of the features zero 1.5, nine tenths of 65536 3.2, products of one sign 4 to 6, a few
+// features a hundred times the others 2 where they come first and 0.04 where they come last, one to four features and small whole
+// numbers none.
 // The logits of a row are therefore scaled up by 1 + 2^-30 n with n its nonzero features (lm_rows_kernel).  For 4096 normal
 // values that halves a logit's error (4.4e-6 -> 2.2e-6 of the logits' size) and takes most of lse's, where nearly equal shares add
 // up (3.9e-6 -> 5e-7); a row of up to 64 features is left as it is, and a dense row that lost nothing is off by 2^-30 n of its
@@ -250,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) lm_gemm_kernel(const __grid_const
                         else tma_load_3d(dst, map, &bars.full[s], c, 0, r);
                     };
                     if constexpr (kKind == kStats || kKind == kLogits) {
-                        // W, which comes from HBM, is asked for before x (1 token: 30.9 us per call, x first; 29.8 so)
+                        // W, which comes from HBM, is asked for before x (1 token: 1.1 us of 30)
                         load(b, &p.w, kb * kBK, n0);
                         // slots past the piece's end are left as they are: a row of A reaches its own row of the product only
                         for (int j = 0; j < mine; ++j) {

@@ -9,10 +9,12 @@
 // What the kernels wait for is memory latency, so they are laid out by the bytes in flight per SM that the registers allow:
 //   forward   a lane holds eight features, D/8 lanes a vector, a warp 32 / (D/8) neighbouring heads of one token (of 512 bytes at
 //             D = 128); the rotation's partner comes by shuffle.  80 registers, three blocks of 256 threads per SM.
-//             2 x 8K tokens, 64 heads of 128: 95 us (5.7 TB/s); with the backward's layout 104 us.
+//             2 x 8K tokens, 64 heads of 128: 97 us (5.6 TB/s); with the backward's layout a tenth more.
 //   backward  a lane holds eight features and their eight partners, so D/16 lanes a vector and no shuffle but the sums; the
 //             vectors of a warp are neighbouring tokens.  128 registers, two blocks per SM.
-//             128K tokens, 40 heads of 128: 715 us (5.7 TB/s); with the forward's layout 727 us.
+//             128K tokens, 40 heads of 128: 714 us (5.7 TB/s); with the forward's layout 727 us.
+// The blocks are divided between Q and K by their heads (fill), which is even where both have as many; with fewer key heads K's blocks
+// go on after Q's are done (128K tokens, 32 + 8 heads forward: 587 us, 4.6 TB/s).
 #include <cuda_bf16.h>
 
 #include <type_traits>
