@@ -248,3 +248,26 @@ def test_checkpoints_are_saved_tensors(basp):
         assert ((a.float() - b.float()).abs() <= 2.0 ** -7 * b.float().abs() + 1e-6).all()
     for i in (1, 2):
         assert all(torch.equal(a, b) for a, b in zip(grads[0][i], grads[1][i]))
+
+
+def test_what_is_held_between_the_passes(basp):
+    """With checkpoints the layer holds them and the log-sum-exp, without them Q, K, V, O and the log-sum-exp in place of them (to the
+    allocator's 512 bytes a tensor)."""
+    from paper_2609_03151_b200.autograd import basp_attention
+    w = synth.Workload("held", N=4, B=2, S=2048, Hq=8, Hkv=4, D=128)
+    pl = make_plan(basp, w)
+    ones = lambda h: [torch.ones((pl.Bl, pl.T, h, w.D), dtype=torch.bfloat16, device="cuda").requires_grad_() for _ in range(4)]
+    leaves = [ones(h) for h in (w.Hq, w.Hkv, w.Hkv)]
+    bf16 = 4 * pl.Bl * pl.T * (2 * w.Hq + 2 * w.Hkv) * w.D * 2
+    lse = 4 * pl.Bl * pl.Hq_l * pl.S * 4
+    want = {False: bf16 + lse, True: sum(basp.basp_ckpt_bytes(pl, r) for r in range(4)) + lse}
+    assert want[True] < 0.55 * want[False]
+    for ckpt in (False, True):
+        before = torch.cuda.memory_allocated()
+        x = [[t * 1.0 for t in ts] for ts in leaves]       # activations that nothing else keeps
+        out = basp_attention(pl, *x, fused=True, checkpoint8=ckpt)
+        loss = sum(t.float().sum() for t in out)           # holds the graph, and nothing of the outputs
+        del x, out
+        held = torch.cuda.memory_allocated() - before
+        assert want[ckpt] <= held <= want[ckpt] + 32 * 512, (ckpt, held, want[ckpt])
+        del loss
