@@ -409,8 +409,8 @@ int basp_layer_bwd_ckpt(const basp_plan *plan, const void *const *ckpt_shards, c
  * its 128 words), and dz is rounded to bf16 as an operand.  A NULL dx_seq or dw (not both) leaves that gradient and its
  * product out.  A token of weight 0 has no part in the gradients, NaN among its values or not; a weight that is no finite
  * number reaches its own dx and dw only.  Weights count in units of the largest finite one of their piece of rows: dx of a token
- * whose weight is below 2^-100 of that loses bits, below some 2^-130 it is zero.  Both gradients are written, not added to; the same inputs and piece_rows give the
- * same bits.
+ * whose weight is below 2^-100 of that loses bits, below some 2^-130 it is zero.  Both gradients are written, not added to; the
+ * same inputs and piece_rows give the same bits.
  * The rows are worked on in pieces of piece_rows (rounded up to 128; 0: 8192; at most 32768).  The workspace holds of one piece
  * 2 bytes per logit and 8 per 128 logits, its rows of x, and where its rows are too few to fill the GPU up to 768 MB of partial
  * sums of dx; where there are several pieces, 4 vocab hidden bytes for the running sum of dw besides.

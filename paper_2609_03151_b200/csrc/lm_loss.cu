@@ -17,7 +17,8 @@
 //   (3) dW = dz^T x        K = the piece's rows; with several pieces the sum is carried in fp32
 // Tensor-bound for many rows: 8192 rows of 4096 features against 128256 words take 19.3 to 20.1 ms (1280 to 1337 TFLOP/s, at the power
 // limit; the three products alone by cuBLAS 18.6 ms), of which dz takes 0.62 (4.2 GB, HBM-bound).  Several pieces: 1260 TFLOP/s, for
-// the fp32 sum of dW.  Few rows: bound by reading W twice and writing dW (48 rows against 32000 words: 161 us on the GPU).  Rows are worked on in pieces (default 8192), so what lies between the products is 2 bytes per logit of one piece.
+// the fp32 sum of dW.  Few rows: bound by reading W twice and writing dW (48 rows against 32000 words: 161 us on the GPU).  Rows are
+// worked on in pieces (default 8192), so what lies between the products is 2 bytes per logit of one piece.
 //
 // Roundings.  A distance is off by at most 2^-11 in log2, so a probability by 2^-11 ln 2 = 3.4e-4, before it is rounded to bf16
 // (2^-8) as an operand: 16 bits do for what would otherwise be an fp32 logit, twice the memory and traffic.  The target is left out of
