@@ -426,6 +426,118 @@ int basp_lm_loss_grad(const basp_plan *plan, int hidden, int vocab, const void *
                       size_t workspace_bytes, void *stream);
 size_t basp_lm_loss_grad_workspace_bytes(const basp_plan *plan, int hidden, int vocab, int piece_rows);
 
+/* ---- attention with masked and shaped scores over each rank's head slice (the paper has the causal layer alone; batches of packed
+ * documents and models that cap or bias their scores need these):
+ *   z_ij = c tanh(scale q_i.k_j / c) - slope_h |i - j|     (i, j: places in the sequence),   visible iff begin_i <= j < end_i
+ *   O_i = sum_j softmax_j(z_ij) v_j,   LSE_i = ln sum_j exp(z_ij);   a query that sees no key has O = 0 and LSE = -infinity
+ * basp_score says which of it a call has:
+ *   softcap    c; 0: no cap (negative, infinite, NaN, or a scale / c outside 1e-30..1e30: BASP_ERR_INVALID)
+ *   slopes     device fp32 [Hq], the same for all sequences, of the whole layer's query heads in order; NULL: no bias.  Finite.
+ *   mask       a mask object of this plan; NULL: the plan's own mask (causal or none)
+ *
+ * A mask object is what basp_mask_ranges or basp_mask_packed write into basp_mask_bytes(plan) bytes of device memory (16-byte
+ * aligned): the key range of every query and, from them, which 128 x 128 tiles there is something to do in and in what order.  It is
+ * made once for a batch and read by every layer and both passes; it belongs to plans with the same micro_batch and seq_len.
+ *   basp_mask_ranges   key_begin, key_end: device int32 [B][S]; clamped to [0, S], an empty range sees nothing.  The ranges are the whole
+ *                      mask: the plan's causal flag has no part in it.  Any ranges are right; the work follows the smallest
+ *                      range of tiles that holds them.
+ *   basp_mask_packed   causal attention inside packed documents.  positions: device int32 [B][S], the token's place in its document
+ *                      (negative: padding, sees nothing and is seen by no document's tokens);  prefix: device int32 [B][S], for every
+ *                      token how many of its document's first tokens all of the document sees (at most its length), or NULL;
+ *                      window: how many keys back a token sees, itself included, 0: all:
+ *                        begin_i = max(i - pos_i, i - window + 1),   end_i = max(i + 1, i - pos_i + prefix_i)
+ *                      (where the two meet the window has the last word).  BASP_ERR_INVALID for a plan that is not causal.
+ * Operands, layouts and limits as basp_attn_fwd and basp_attn_bwd; outputs may not overlap inputs (BASP_ERR_ALIAS).  bf16 operands, fp32
+ * scores, softmax and sums, P and dS rounded to bf16 as operands.  K may hold anything where no query sees it; otherwise a hidden
+ * element is multiplied by zero, so Q, K, V, O and dO have to be finite numbers in padding too.
+ * The backward pass takes the forward's O and LSE:
+ *   P = exp(z - LSE),  dV_j = sum_i P_ij dO_i,  dZ_ij = P_ij (dO_i.v_j - dO_i.O_i),  dS = scale (1 - tanh^2) dZ,  dQ = dS K,  dK = dS^T Q
+ * (no gradient for the slopes); keys that nothing sees get zeros.  dQ is summed by floating-point atomics.  workspace:
+ * basp_attn_masked_bwd_workspace_bytes(plan). */
+typedef struct basp_score {
+    float softcap;
+    const float *slopes;
+    const void *mask;
+    size_t mask_bytes;       /* of the buffer, at least basp_mask_bytes(plan) (BASP_ERR_WORKSPACE) */
+} basp_score;
+size_t basp_mask_bytes(const basp_plan *plan);
+int basp_mask_ranges(const basp_plan *plan, const int *key_begin, const int *key_end, void *mask, size_t mask_bytes, void *stream);
+int basp_mask_packed(const basp_plan *plan, const int *positions, const int *prefix, int window, void *mask, size_t mask_bytes,
+                     void *stream);
+int basp_attn_masked_fwd(const basp_plan *plan, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                         const void *const *v_head, void *const *o_head, float *const *lse_shards, float softmax_scale, void *stream);
+int basp_attn_masked_bwd(const basp_plan *plan, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                         const void *const *v_head, const void *const *o_head, const void *const *do_head,
+                         const float *const *lse_shards, void *const *dq_head, void *const *dk_head, void *const *dv_head,
+                         void *workspace, size_t workspace_bytes, float softmax_scale, void *stream);
+size_t basp_attn_masked_bwd_workspace_bytes(const basp_plan *plan);
+/* The whole layer with such scores, on sequence-sharded shards: basp_layer_fwd and basp_layer_bwd with the attention above in
+ * their middle (same workspaces; after the forward basp_layer_workspace_shards has what the backward takes). */
+int basp_layer_masked_fwd(const basp_plan *plan, const basp_score *score, const void *const *q_seq, const void *const *k_seq,
+                          const void *const *v_seq, void *const *o_seq, float *const *lse_shards, void *workspace,
+                          size_t workspace_bytes, float softmax_scale, void *stream);
+int basp_layer_masked_bwd(const basp_plan *plan, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                          const void *const *v_head, const void *const *o_head, const float *const *lse_shards,
+                          const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq, void *workspace,
+                          size_t workspace_bytes, float softmax_scale, void *stream);
+
+/* ---- rotary positions of any token order: Q and K of every rank rotated by the token's own position, which restarts in packed
+ * documents, goes on behind a cache, or is that in the sequence.  With theta_j the frequency of pair j and a = position theta_j:
+ *   (x_u, x_v) -> factor (x_u cos a - x_v sin a,  x_v cos a + x_u sin a)
+ * over the first rotary_dim features of a head, (u, v) = (j, j + rotary_dim / 2) or, interleaved, (2j, 2j + 1); the other features
+ * are copied.  basp_rope_make computes the frequencies on the host, once for a model:
+ *   BASP_ROPE_PLAIN       theta_j = base^(-2j / rotary_dim)
+ *   BASP_ROPE_LINEAR      theta_j / stretch
+ *   BASP_ROPE_BY_PARTS    (YaRN) pairs that turn more than beta_fast times in original_len tokens stay, those that turn less than
+ *                         beta_slow times are divided by stretch, a ramp over j between them;  factor = 0.1 ln(stretch) + 1
+ *   BASP_ROPE_WAVELENGTH  (Llama 3) the same by the turns themselves, above high and below low, a ramp over them in between
+ * and keeps them in turns per token as 64-bit fixed-point numbers: position x frequency wraps round where a whole turn does, so the
+ * angle is exact to 2^-32 turns at any int32 position (negative ones too).  No tables in device memory.
+ * positions: device int32 [B][S] in sequence order, or NULL for the place in the sequence.  inverse: 0 rotates; 1 is the transpose
+ * (turned back, times factor): the gradient of the forward call.  q_out[r] may be q_seq[r] itself, k_out[r] k_seq[r]; no other
+ * overlap.  Requires D a multiple of 16 up to 128, rotary_dim a multiple of 16 up to D.  fp32 arithmetic, one rounding to bf16. */
+#define BASP_ROPE_PLAIN      0
+#define BASP_ROPE_LINEAR     1
+#define BASP_ROPE_BY_PARTS   2
+#define BASP_ROPE_WAVELENGTH 3
+typedef struct basp_rope_config {
+    int rotary_dim, interleaved, scaling;
+    double base, stretch;          /* base > 1; stretch >= 1 (scaled forms) */
+    double original_len;           /* trained length, BY_PARTS and WAVELENGTH */
+    double slow, fast;             /* turns in original_len: beta_slow < beta_fast, low < high; both 0: 1 and 32, 1 and 4 */
+    double factor;                 /* on the rotated features; 0: the default of the form (1, or BY_PARTS' own) */
+} basp_rope_config;
+typedef struct basp_rope_turns {   /* filled by basp_rope_make; a plain value, may be copied */
+    int rotary_dim, interleaved;
+    float factor;
+    unsigned long long turns[64];  /* of pair j per token, in 2^-64 turns */
+} basp_rope_turns;
+int basp_rope_make(const basp_rope_config *cfg, basp_rope_turns *rope);
+int basp_rope(const basp_plan *plan, const basp_rope_turns *rope, const void *const *q_seq, const void *const *k_seq,
+              const int *positions, int inverse, void *const *q_out, void *const *k_out, void *stream);
+
+/* ---- the edge between two blocks on the ranks' sequence shards: the norm behind a block, its gate and residual scale, the sum with
+ * the stream, and the norm before the next block, in one pass over the rows (hidden features each):
+ *   z = y w_post / sqrt(mean(y^2) + eps),   h = x + res_scale gate z,   n = h w_pre / sqrt(mean(h^2) + eps)
+ * Weights: bf16 [hidden], shared by all ranks.  w_post NULL: z = y.  gate NULL: 1.  w_pre NULL: no n (n_seq NULL too).  y_seq NULL: there
+ * is no block before (w_post, gate and h_seq NULL too): n of x alone.  n is formed from h before h is rounded to bf16.  h_seq[r] may be
+ * x_seq[r] or y_seq[r] itself, n_seq[r] the other of the two; no other overlap.
+ *
+ * The backward pass takes h (h_seq of the forward, or x_seq where there was no y; NULL without w_pre), y, dh_out (the gradient that
+ * reaches h from elsewhere; NULL: none) and dn (NULL without w_pre), and writes dx = the gradient of h in all, which is x's, dy, and
+ * the sums over all tokens dw_post, dgate, dw_pre (fp32 [hidden], written, not added to; NULL for what there is not).  y_seq NULL: no dy.
+ * y may be NULL with a dy wanted where neither w_post nor gate is there (dy = res_scale dx).  dx_seq[r] may be dh_out[r] or dn[r] itself,
+ * dy_seq[r] may be y_seq[r].  The same inputs give the same bits.
+ * fp32 arithmetic.  Requires hidden a multiple of 8 up to 16384, eps > 0 and res_scale finite. */
+int basp_block_norm(const basp_plan *plan, int hidden, const void *const *x_seq, const void *const *y_seq, const void *w_post,
+                    const void *gate, const void *w_pre, float res_scale, float eps, void *const *h_seq, void *const *n_seq,
+                    void *stream);
+int basp_block_norm_bwd(const basp_plan *plan, int hidden, const void *const *h_seq, const void *const *y_seq, const void *w_post,
+                        const void *gate, const void *w_pre, float res_scale, float eps, const void *const *dh_out,
+                        const void *const *dn, void *const *dx_seq, void *const *dy_seq, float *dw_post, float *dgate, float *dw_pre,
+                        void *workspace, size_t workspace_bytes, void *stream);
+size_t basp_block_norm_bwd_workspace_bytes(const basp_plan *plan, int hidden);
+
 /* ---- device status.  Every wait inside the kernels (on a shared-memory barrier) is bounded;
  * when one expires the kernel records where, lets its copies drain, frees its tensor memory
  * and returns.  basp_get_status synchronises `stream`, copies the four status words of the

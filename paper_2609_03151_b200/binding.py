@@ -39,6 +39,9 @@ EXPORTS = [
     "basp_qk_norm_rope", "basp_qk_norm_rope_bwd", "basp_qk_norm_rope_bwd_workspace_bytes",
     "basp_ckpt_bytes", "basp_ckpt_pack", "basp_ckpt_reshard_s2h", "basp_layer_bwd_ckpt",
     "basp_lm_loss_fwd", "basp_lm_loss_fwd_workspace_bytes", "basp_lm_loss_grad", "basp_lm_loss_grad_workspace_bytes",
+    "basp_mask_bytes", "basp_mask_ranges", "basp_mask_packed", "basp_attn_masked_fwd", "basp_attn_masked_bwd",
+    "basp_attn_masked_bwd_workspace_bytes", "basp_layer_masked_fwd", "basp_layer_masked_bwd", "basp_rope_make", "basp_rope",
+    "basp_block_norm", "basp_block_norm_bwd", "basp_block_norm_bwd_workspace_bytes",
 ]
 
 
@@ -105,6 +108,34 @@ lib.basp_lm_loss_fwd.argtypes = [c_void_p, c_int, c_int] + [c_void_p] * 6 + [c_s
 lib.basp_lm_loss_grad.argtypes = [c_void_p, c_int, c_int] + [c_void_p] * 8 + [c_int, c_void_p, c_size_t, c_void_p]
 for _n, _a in (("basp_qk_norm_rope_bwd_workspace_bytes", []), ("basp_ckpt_bytes", [c_int]),
                ("basp_lm_loss_fwd_workspace_bytes", [c_int]), ("basp_lm_loss_grad_workspace_bytes", [c_int] * 3)):
+    getattr(lib, _n).argtypes = [c_void_p] + _a
+    getattr(lib, _n).restype = c_size_t
+
+
+class _Score(Structure):
+    _fields_ = [("softcap", c_float), ("slopes", c_void_p), ("mask", c_void_p), ("mask_bytes", c_size_t)]
+
+
+class basp_rope_config(Structure):
+    _fields_ = [(n, c_int) for n in ("rotary_dim", "interleaved", "scaling")] + \
+               [(n, ctypes.c_double) for n in ("base", "stretch", "original_len", "slow", "fast", "factor")]
+
+
+class basp_rope_turns(Structure):
+    _fields_ = [("rotary_dim", c_int), ("interleaved", c_int), ("factor", c_float), ("turns", ctypes.c_ulonglong * 64)]
+
+
+lib.basp_mask_ranges.argtypes = [c_void_p] * 4 + [c_size_t, c_void_p]
+lib.basp_mask_packed.argtypes = [c_void_p] * 3 + [c_int, c_void_p, c_size_t, c_void_p]
+lib.basp_attn_masked_fwd.argtypes = [c_void_p, POINTER(_Score)] + [c_void_p] * 5 + [c_float, c_void_p]
+lib.basp_attn_masked_bwd.argtypes = [c_void_p, POINTER(_Score)] + [c_void_p] * 10 + [c_size_t, c_float, c_void_p]
+lib.basp_layer_masked_fwd.argtypes = [c_void_p, POINTER(_Score)] + [c_void_p] * 6 + [c_size_t, c_float, c_void_p]
+lib.basp_layer_masked_bwd.argtypes = [c_void_p, POINTER(_Score)] + [c_void_p] * 10 + [c_size_t, c_float, c_void_p]
+lib.basp_rope_make.argtypes = [POINTER(basp_rope_config), POINTER(basp_rope_turns)]
+lib.basp_rope.argtypes = [c_void_p, POINTER(basp_rope_turns)] + [c_void_p] * 3 + [c_int] + [c_void_p] * 3
+lib.basp_block_norm.argtypes = [c_void_p, c_int] + [c_void_p] * 5 + [c_float, c_float] + [c_void_p] * 3
+lib.basp_block_norm_bwd.argtypes = [c_void_p, c_int] + [c_void_p] * 5 + [c_float, c_float] + [c_void_p] * 8 + [c_size_t, c_void_p]
+for _n, _a in (("basp_mask_bytes", []), ("basp_attn_masked_bwd_workspace_bytes", []), ("basp_block_norm_bwd_workspace_bytes", [c_int])):
     getattr(lib, _n).argtypes = [c_void_p] + _a
     getattr(lib, _n).restype = c_size_t
 lib.basp_strerror.argtypes = [c_int]
@@ -426,7 +457,7 @@ def basp_out_proj(plan, hidden, o_seq, w_o, y_seq, stream=None):
                              _stream(stream)), "basp_out_proj")
 
 
-_BF16, _F32, _I64, _U8 = torch.bfloat16, torch.float32, torch.int64, torch.uint8
+_BF16, _F32, _I64, _U8, _I32 = torch.bfloat16, torch.float32, torch.int64, torch.uint8, torch.int32
 
 
 class _Marshal:
@@ -438,6 +469,7 @@ class _Marshal:
 
     def __init__(self):
         self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+        self.kept = None
 
     def _address(self, t, dtype, numel, what):
         if isinstance(t, torch.Tensor):
@@ -475,6 +507,8 @@ class _Marshal:
 
     def space(self, workspace):
         """Address and size of a workspace tensor."""
+        if workspace is None:
+            return None, 0
         if workspace.get_device() != self.device or not workspace.is_contiguous():
             raise ValueError(f"workspace: expected contiguous memory of the current device, got a tensor on {workspace.device}")
         return workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -596,6 +630,154 @@ def basp_lm_loss_grad(plan, hidden, vocab, x_seq, w, labels, token_weights, loss
                     ("dx_seq", _BF16, dx_seq, wide), ("dw", _BF16, dw, vocab * hidden))
     _check(lib.basp_lm_loss_grad(plan.handle, hidden, vocab, *a, int(piece_rows), *m.space(workspace), m.stream(stream)),
            "basp_lm_loss_grad")
+
+
+def basp_mask_bytes(plan) -> int:
+    return int(lib.basp_mask_bytes(plan.handle))
+
+
+def _tokens(plan):
+    """Tokens of the whole micro-batch, [B, S]."""
+    return plan.cfg.micro_batch * plan.S
+
+
+def basp_mask_ranges(plan, key_begin, key_end, mask, stream=None):
+    """The mask object of key ranges: query i of sequence b sees the keys [key_begin[b, i], key_end[b, i]) (int32 [B, S]);
+    mask: uint8 tensor of basp_mask_bytes(plan)."""
+    m, n = _Marshal(), _tokens(plan)
+    a = m.addresses(("key_begin", _I32, key_begin, n), ("key_end", _I32, key_end, n))
+    _check(lib.basp_mask_ranges(plan.handle, *a, *m.space(mask), m.stream(stream)), "basp_mask_ranges")
+
+
+def basp_mask_packed(plan, positions, mask, prefix=None, window=0, stream=None):
+    """The mask object of causal attention inside packed documents: positions in the own document (int32 [B, S], negative: padding),
+    prefix: how many of the document's first tokens all of it sees (int32 [B, S] or None), window: keys back, itself included
+    (0: all)."""
+    m, n = _Marshal(), _tokens(plan)
+    a = m.addresses(("positions", _I32, positions, n), ("prefix", _I32, prefix, n))
+    _check(lib.basp_mask_packed(plan.handle, *a, int(window), *m.space(mask), m.stream(stream)), "basp_mask_packed")
+
+
+class basp_score:
+    """What a score goes through and which keys are seen: softcap c (0: none), slopes of the bias by distance (fp32 [Hq] or None),
+    mask (a mask object, or None for the plan's own mask).  Holds its tensors."""
+
+    def __init__(self, softcap=0.0, slopes=None, mask=None):
+        self.softcap, self.slopes, self.mask = float(softcap), slopes, mask
+
+    def marshal(self, plan, m):
+        slopes = m.addresses(("slopes", _F32, self.slopes, plan.Hq))[0] if self.slopes is not None else None
+        kept = m.kept
+        mask, size = m.space(self.mask) if self.mask is not None else (None, 0)
+        return kept, byref(_Score(self.softcap, slopes, mask, size))
+
+
+def _head_sizes(plan):
+    sizes = plan.sizes.get("head")
+    if sizes is None:
+        vec, n = plan.Bl * plan.S, plan.N
+        sizes = plan.sizes["head"] = ((vec * plan.Hq_l * plan.D,) * n, (vec * plan.Hkv_l * plan.D,) * n, (vec * plan.Hq_l,) * n)
+    return sizes
+
+
+def basp_attn_masked_fwd(plan, score, q_head, k_head, v_head, o_head, lse_shards=None, softmax_scale=0.0, stream=None):
+    """basp_attn_fwd with capped, biased and masked scores (a basp_score); a query that sees no key has O = 0, LSE = -inf."""
+    m, (q, k, rows) = _Marshal(), _head_sizes(plan)
+    kept, s = score.marshal(plan, m)
+    a = m.addresses(("q_head", _BF16, q_head, q), ("k_head", _BF16, k_head, k), ("v_head", _BF16, v_head, k),
+                    ("o_head", _BF16, o_head, q), ("lse_shards", _F32, lse_shards, rows))
+    _check(lib.basp_attn_masked_fwd(plan.handle, s, *a, softmax_scale, m.stream(stream)), "basp_attn_masked_fwd")
+
+
+def basp_attn_masked_bwd_workspace_bytes(plan) -> int:
+    return int(lib.basp_attn_masked_bwd_workspace_bytes(plan.handle))
+
+
+def basp_attn_masked_bwd(plan, score, q_head, k_head, v_head, o_head, do_head, lse_shards, dq_head, dk_head, dv_head, workspace,
+                         softmax_scale=0.0, stream=None):
+    """Gradients of basp_attn_masked_fwd from its O and LSE."""
+    m, (q, k, rows) = _Marshal(), _head_sizes(plan)
+    kept, s = score.marshal(plan, m)
+    a = m.addresses(("q_head", _BF16, q_head, q), ("k_head", _BF16, k_head, k), ("v_head", _BF16, v_head, k),
+                    ("o_head", _BF16, o_head, q), ("do_head", _BF16, do_head, q), ("lse_shards", _F32, lse_shards, rows),
+                    ("dq_head", _BF16, dq_head, q), ("dk_head", _BF16, dk_head, k), ("dv_head", _BF16, dv_head, k))
+    _check(lib.basp_attn_masked_bwd(plan.handle, s, *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_attn_masked_bwd")
+
+
+def basp_layer_masked_fwd(plan, score, q_seq, k_seq, v_seq, o_seq, workspace, lse_shards=None, softmax_scale=0.0, stream=None):
+    """basp_layer_fwd with such scores (same workspace)."""
+    m, (q, k) = _Marshal(), _qk(plan)
+    kept, s = score.marshal(plan, m)
+    a = m.addresses(("q_seq", _BF16, q_seq, q), ("k_seq", _BF16, k_seq, k), ("v_seq", _BF16, v_seq, k), ("o_seq", _BF16, o_seq, q),
+                    ("lse_shards", _F32, lse_shards, _head_sizes(plan)[2]))
+    _check(lib.basp_layer_masked_fwd(plan.handle, s, *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_layer_masked_fwd")
+
+
+def basp_layer_masked_bwd(plan, score, q_head, k_head, v_head, o_head, lse_shards, do_seq, dq_seq, dk_seq, dv_seq, workspace,
+                          softmax_scale=0.0, stream=None):
+    """basp_layer_bwd with such scores (same workspace); q_head .. o_head as basp_layer_workspace_shards reports them."""
+    m, (q, k) = _Marshal(), _qk(plan)
+    qh, kh, rows = _head_sizes(plan)
+    kept, s = score.marshal(plan, m)
+    a = m.addresses(("q_head", _BF16, q_head, qh), ("k_head", _BF16, k_head, kh), ("v_head", _BF16, v_head, kh),
+                    ("o_head", _BF16, o_head, qh), ("lse_shards", _F32, lse_shards, rows), ("do_seq", _BF16, do_seq, q),
+                    ("dq_seq", _BF16, dq_seq, q), ("dk_seq", _BF16, dk_seq, k), ("dv_seq", _BF16, dv_seq, k))
+    _check(lib.basp_layer_masked_bwd(plan.handle, s, *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_layer_masked_bwd")
+
+
+_ROPE_SCALINGS = {"none": 0, "linear": 1, "yarn": 2, "wavelength": 3}
+
+
+def basp_rope_make(rotary_dim, theta=10000.0, interleaved=False, scaling="none", factor=1.0, original_len=0.0, slow=0.0, fast=0.0,
+                   attention_factor=0.0) -> basp_rope_turns:
+    """The frequencies of a rotation, made once for a model.  scaling: "none", "linear", "yarn" (BASP_ROPE_BY_PARTS) or "wavelength",
+    by `factor`; original_len: the length trained on; slow, fast: the borders in turns (0: the form's own); attention_factor: on the
+    rotated features (0: the form's own)."""
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError(f"scaling: expected one of {sorted(_ROPE_SCALINGS)}, got {scaling!r}")
+    cfg = basp_rope_config(int(rotary_dim), int(bool(interleaved)), _ROPE_SCALINGS[scaling], float(theta), float(factor),
+                           float(original_len), float(slow), float(fast), float(attention_factor))
+    out = basp_rope_turns()
+    _check(lib.basp_rope_make(byref(cfg), byref(out)), "basp_rope_make")
+    return out
+
+
+def basp_rope(plan, rope, q_seq, k_seq, q_out, k_out, positions=None, inverse=False, stream=None):
+    """Q and K rotated by their tokens' positions (int32 [B, S], None: the place in the sequence); inverse: the gradient of that.
+    q_out[r] may be q_seq[r], k_out[r] may be k_seq[r]."""
+    m, (q, k) = _Marshal(), _qk(plan)
+    x, xk, pos, y, yk = m.addresses(("q_seq", _BF16, q_seq, q), ("k_seq", _BF16, k_seq, k), ("positions", _I32, positions, _tokens(plan)),
+                                    ("q_out", _BF16, q_out, q), ("k_out", _BF16, k_out, k))
+    _check(lib.basp_rope(plan.handle, byref(rope), x, xk, pos, int(bool(inverse)), y, yk, m.stream(stream)), "basp_rope")
+
+
+def basp_block_norm(plan, hidden, x_seq, y_seq, h_seq, n_seq, w_post=None, gate=None, w_pre=None, res_scale=1.0, eps=1e-6, stream=None):
+    """h = x + res_scale gate norm(y; w_post), n = norm(h; w_pre) on the ranks' rows of `hidden` features; w_post, gate (bf16 [hidden])
+    None: not there; w_pre and n_seq None: no norm before the next block; y_seq and h_seq None: n of x alone."""
+    m, hidden = _Marshal(), int(hidden)
+    wide = _per_rank(plan, hidden)
+    x, y, wp, g, wn, h, n = m.addresses(("x_seq", _BF16, x_seq, wide), ("y_seq", _BF16, y_seq, wide), ("w_post", _BF16, w_post, hidden),
+                                        ("gate", _BF16, gate, hidden), ("w_pre", _BF16, w_pre, hidden), ("h_seq", _BF16, h_seq, wide),
+                                        ("n_seq", _BF16, n_seq, wide))
+    _check(lib.basp_block_norm(plan.handle, hidden, x, y, wp, g, wn, float(res_scale), float(eps), h, n, m.stream(stream)), "basp_block_norm")
+
+
+def basp_block_norm_bwd_workspace_bytes(plan, hidden) -> int:
+    return int(lib.basp_block_norm_bwd_workspace_bytes(plan.handle, int(hidden)))
+
+
+def basp_block_norm_bwd(plan, hidden, h_seq, y_seq, dh_out, dn, dx_seq, dy_seq, dw_post, dgate, dw_pre, workspace, w_post=None,
+                        gate=None, w_pre=None, res_scale=1.0, eps=1e-6, stream=None):
+    """Gradients of basp_block_norm: dx_seq, dy_seq (bf16) and dw_post, dgate, dw_pre (fp32 [hidden]) from h, y and the gradients that
+    reach h elsewhere (dh_out, None: none) and n (dn)."""
+    m, hidden = _Marshal(), int(hidden)
+    wide = _per_rank(plan, hidden)
+    h, y, wp, g, wn, dh, d, dx, dy, gp, gg, gn = m.addresses(
+        ("h_seq", _BF16, h_seq, wide), ("y_seq", _BF16, y_seq, wide), ("w_post", _BF16, w_post, hidden), ("gate", _BF16, gate, hidden),
+        ("w_pre", _BF16, w_pre, hidden), ("dh_out", _BF16, dh_out, wide), ("dn", _BF16, dn, wide), ("dx_seq", _BF16, dx_seq, wide),
+        ("dy_seq", _BF16, dy_seq, wide), ("dw_post", _F32, dw_post, hidden), ("dgate", _F32, dgate, hidden), ("dw_pre", _F32, dw_pre, hidden))
+    _check(lib.basp_block_norm_bwd(plan.handle, hidden, h, y, wp, g, wn, float(res_scale), float(eps), dh, d, dx, dy, gp, gg, gn,
+                                   *m.space(workspace), m.stream(stream)), "basp_block_norm_bwd")
 
 
 def basp_selftest_wait_timeout(limit_us: int, stream=None):

@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libbasp.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 SOURCES = ["plan.cpp", "status.cu", "reshard.cu", "attn_fwd.cu", "attn_bwd.cu", "proj_gemm.cu", "layer.cu", "layer_static.cu",
-           "norm_rope.cu", "ckpt.cu", "lm_loss.cu"]
+           "norm_rope.cu", "ckpt.cu", "lm_loss.cu", "attn_mask.cu", "attn_masked_fwd.cu", "attn_masked_bwd.cu", "rope.cu", "block_norm.cu"]
 
 
 def _nvcc() -> str:
@@ -33,7 +33,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "--threads", "0",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB]
     if verbose:
         cmd += ["-Xptxas", "-v"]

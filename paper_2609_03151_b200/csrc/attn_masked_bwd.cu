@@ -1,0 +1,303 @@
+// Backward of the attention with masked and shaped scores (attn_masked_fwd.cu) over each virtual rank's head slice:
+//
+//   P_ij = exp(z_ij - LSE_i) on visible pairs,  Delta_i = dO_i.O_i,  dV_j = sum_i P_ij dO_i,
+//   dZ_ij = P_ij (dO_i.v_j - Delta_i),  dS_ij = scale (1 - tanh^2(scale q_i.k_j / c)) dZ_ij,  dQ_i = sum_j dS_ij k_j,  dK_j = sum_i dS_ij q_i
+//
+// The kernels are those of attn_bwd.cu (five products per tile pair on tcgen05, dK and dV resident in TMEM, dQ added to an fp32
+// accumulator), walking the tile pairs of the mask object: a work item is a key tile and the query tiles that see some of it,
+// longest first.  A row without a key has LSE = -inf and takes no part; a key tile that nothing sees gets zeros.
+#include <cuda.h>
+#include <math.h>
+
+#include <type_traits>
+
+#include "common.cuh"
+#include "ptx.cuh"
+#include "tmap.cuh"
+#include "attn_bwd_common.cuh"
+#include "attn_mask.cuh"
+#include "score.cuh"
+#include "spans.h"
+
+int *basp_status_device_ptr();
+
+namespace {
+
+template <int R>
+struct MaskedBwdParams {
+    CUtensorMap q[R], k[R], v[R], dout[R];
+    CUtensorMap dq_acc[R];      // fp32 accumulator, box 32 floats x 1 head x 32 rows (reduce-add target of the 64-wide kernel)
+    float *dq_accp[R];          // the same accumulator as a plain pointer ([Bl*S][Hq_l][Dg] floats)
+    const float *lse[R];
+    const float *delta[R];
+    __nv_bfloat16 *dk[R], *dv[R];
+    ScoreArgs score;
+    int K, Bl, S, Hq_l, Hkv_l, q_per_kv, causal, n_tiles, total;      // total: work items
+    int Dg;                     // head dimension in memory
+    float scale, scale_log2;
+    int *status;
+    FastDiv div_items, div_hkv_l, div_B, div_bl;
+};
+
+struct MbItem {
+    int r, bl, seq, hkv, n, m0, n_qt;
+};
+
+template <int R>
+__device__ __forceinline__ bool mb_get_item(const MaskedBwdParams<R> &p, int round, MbItem &it) {
+    const int pos = (round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x;   // boustrophedon
+    const int i = round * (int)gridDim.x + pos;
+    if (i >= p.total) return false;
+    const int e = (int)fdiv((uint32_t)i, p.div_items), head = i - e * (int)p.div_items.d;
+    const int l = (int)fdiv((uint32_t)head, p.div_hkv_l);
+    it.hkv = head - l * p.Hkv_l;
+    if (p.score.range) {
+        const int4 a = __ldg(reinterpret_cast<const int4 *>(p.score.bwd + e));
+        it.seq = min(max(a.x, 0), p.score.B - 1);       // whatever the buffer holds, no tile outside the tensors
+        it.n = min(max(a.y, 0), p.n_tiles - 1);
+        it.m0 = max(a.z, 0);
+        it.n_qt = min(a.w, p.n_tiles);
+    } else {
+        it.n = (int)fdiv((uint32_t)e, p.div_B);          // low key tiles are seen by the most query tiles: longest first
+        it.seq = e - it.n * p.score.B;
+        it.m0 = p.causal ? it.n : 0;
+        it.n_qt = p.n_tiles;
+    }
+    const int g = (int)fdiv((uint32_t)it.seq, p.div_bl);
+    it.bl = it.seq - g * p.Bl;
+    it.r = g * p.K + l;
+    return true;
+}
+
+// A query's LSE in log2 units; one that sees no key gets the LSE at which every probability is zero.
+__device__ __forceinline__ float seen_lse(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
+
+// For the 128 queries of tile m, which rows [lo, hi) of key tile n they see, as lo | hi << 8, and whether that is to be looked at.
+template <int R>
+__device__ __forceinline__ void stage_windows(const MaskedBwdParams<R> &p, const MbItem &it, int m, int lane, uint16_t *win, int *edge) {
+    const int k0 = it.n * kT;
+    int lo[4], hi[4];
+    bool look;
+    if (p.score.range) {
+        const size_t tile = (size_t)it.seq * p.n_tiles + m;
+        const int4 t = __ldg(reinterpret_cast<const int4 *>(p.score.tiles + tile));
+        const int4 *at = reinterpret_cast<const int4 *>(p.score.range + tile * kT + 4 * lane);
+        const int4 a = __ldg(at), b = __ldg(at + 1);
+        look = it.n < t.z || it.n >= t.w || (m + 1) * kT > p.S;
+        lo[0] = a.x; hi[0] = a.y; lo[1] = a.z; hi[1] = a.w; lo[2] = b.x; hi[2] = b.y; lo[3] = b.z; hi[3] = b.w;
+    } else {
+        look = (p.causal && m == it.n) || (m + 1) * kT > p.S || (it.n + 1) * kT > p.S;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int q = m * kT + 4 * lane + e;
+            lo[e] = 0;
+            hi[e] = q < p.S ? (p.causal ? q + 1 : p.S) : 0;
+        }
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)min(max(lo[e] - k0, 0), kT) | (uint32_t)min(max(hi[e] - k0, 0), kT) << 8;
+    *reinterpret_cast<uint2 *>(win + 4 * lane) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    if (lane == 0) *edge = look;
+}
+
+// Thirty-two scores of a key row (queries side by side): the probabilities as bf16 to pk, and times the cap's derivative to st.
+// dist: the first query's position minus the key's; side: its sign, tile by tile; win: what stage_windows left, where it matters.
+template <bool kCap, bool kBias, bool kEdge>
+__device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t (&pk)[16], const float *lse, const uint16_t *win, int row,
+                                             const ScoreArgs &a, float scale_log2, float slope, int dist, int side) {
+    float sl = 0.f, base = 0.f;
+    if constexpr (kBias) {
+        sl = side < 0 ? slope : -slope;              // -slope |dist + c| = sl c + base on either side of the key
+        base = sl * (float)dist;
+    }
+    const uint64_t sl2 = both(sl), base2 = both(base), minus2 = both(-1.f);
+    bool far = false;
+    if constexpr (kCap) {
+        float top[2] = {0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 32; c += 4)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) top[k] = max3_abs(top[k], __uint_as_float(st[c + 2 * k]), __uint_as_float(st[c + 2 * k + 1]));
+        far = __any_sync(0xffffffffu, fmaxf(top[0], top[1]) * a.cap_in > kTanhNear);
+    }
+    const auto columns = [&](auto far_tag) {
+        [[maybe_unused]] constexpr bool kFar = decltype(far_tag)::value;
+#pragma unroll
+        for (int c = 0; c < 32; c += 4) {
+            const float4 l4 = *reinterpret_cast<const float4 *>(lse + c);
+            uint2 w4 = make_uint2(0, 0);
+            if constexpr (kEdge) w4 = *reinterpret_cast<const uint2 *>(win + c);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = c + 2 * h;
+                uint64_t off = mul2(h ? pack_f2(l4.z, l4.w) : pack_f2(l4.x, l4.y), minus2);
+                if constexpr (kBias) off = add2(off, fma2(pack_f2((float)i, (float)(i + 1)), sl2, base2));
+                const uint64_t s2 = pack_f2(__uint_as_float(st[i]), __uint_as_float(st[i + 1]));
+                [[maybe_unused]] uint64_t t = 0;
+                uint64_t z;
+                if constexpr (!kCap) {
+                    z = fma2(s2, both(scale_log2), off);
+                } else {
+                    if constexpr (kFar) {
+                        t = pack_f2(tanh_far(__uint_as_float(st[i]) * a.cap_in), tanh_far(__uint_as_float(st[i + 1]) * a.cap_in));
+                    } else {
+                        const uint64_t x = mul2(s2, both(a.cap_in));
+                        t = mul2(x, tanh_near_q(x));
+                    }
+                    z = fma2(t, both(a.cap_out), off);
+                }
+                float z0, z1;
+                unpack_f2(z, z0, z1);
+                if constexpr (kBias && kEdge) {       // the diagonal tile has queries on both sides of the key
+                    if (side == 0) {
+                        z0 += 2.f * slope * (float)min(dist + i, 0);
+                        z1 += 2.f * slope * (float)min(dist + i + 1, 0);
+                    }
+                }
+                float p0 = exp2_approx(z0), p1 = exp2_approx(z1);
+                if constexpr (kEdge) {
+                    const uint32_t w = h ? w4.y : w4.x;
+                    if (!(row >= (int)(w & 0xff) && row < (int)((w >> 8) & 0xff))) p0 = 0.f;
+                    if (!(row >= (int)((w >> 16) & 0xff) && row < (int)(w >> 24))) p1 = 0.f;
+                }
+                pk[i >> 1] = pack_bf16x2(p0, p1);
+                if constexpr (kCap) {
+                    const uint64_t g = mul2(pack_f2(p0, p1), fma2(mul2(t, minus2), t, both(1.f)));
+                    unpack_f2(g, p0, p1);
+                }
+                st[i] = __float_as_uint(p0);
+                st[i + 1] = __float_as_uint(p1);
+            }
+        }
+    };
+    if constexpr (kCap) {
+        if (far) columns(std::true_type{});
+        else columns(std::false_type{});
+    } else {
+        columns(std::false_type{});
+    }
+}
+
+// dK and dV of a key tile that no query sees: a quarter g of the compute warps takes 32 of the 128 columns of its row
+template <int R>
+__device__ __forceinline__ void store_zeros(const MaskedBwdParams<R> &p, const MbItem &it, int g, int row) {
+    const int key = it.n * kT + row;
+    if (key >= p.S) return;
+    const size_t off = (((size_t)it.bl * p.S + key) * p.Hkv_l + it.hkv) * p.Dg;
+    for (int c = 32 * g; c < min(32 * g + 32, p.Dg); c += 8) {
+        *reinterpret_cast<uint4 *>(p.dk[it.r] + off + c) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4 *>(p.dv[it.r] + off + c) = make_uint4(0, 0, 0, 0);
+    }
+}
+
+#include "attn_masked_bwd_d64.cuh"
+#include "attn_masked_bwd_d128.cuh"
+
+// accumulator and Delta of every rank
+size_t mb_workspace_bytes(const basp_plan *p) { return (size_t)p->N * (bwd_acc_bytes(p) + bwd_delta_bytes(p)); }
+
+template <int R>
+int mb_run(const basp_plan *pl, const basp_score *score, const void *const *q, const void *const *k, const void *const *v,
+           const void *const *o, const void *const *dout, const float *const *lse, void *const *dq, void *const *dk, void *const *dv,
+           char *ws, float scale, cudaStream_t st) {
+    MaskedBwdParams<R> prm;
+    BASP_TRY(basp_score_args(pl, score, scale, &prm.score));
+    const uint64_t rows = (uint64_t)pl->Bl * pl->S;
+    const size_t acc_b = bwd_acc_bytes(pl), del_b = bwd_delta_bytes(pl);
+    BwdHelperPtrs<R> hp;
+    for (int r = 0; r < pl->N; ++r) {
+        BASP_TRY(tmap::encode_rows_heads_d(&prm.q[r], q[r], rows, pl->Hq_l, pl->D, kT));
+        BASP_TRY(tmap::encode_rows_heads_d(&prm.k[r], k[r], rows, pl->Hkv_l, pl->D, kT));
+        BASP_TRY(tmap::encode_rows_heads_d(&prm.v[r], v[r], rows, pl->Hkv_l, pl->D, kT));
+        BASP_TRY(tmap::encode_rows_heads_d(&prm.dout[r], dout[r], rows, pl->Hq_l, pl->D, kT));
+        float *acc = reinterpret_cast<float *>(ws + (size_t)r * acc_b);
+        float *delta = reinterpret_cast<float *>(ws + (size_t)pl->N * acc_b + (size_t)r * del_b);
+        if (pl->D <= 64) BASP_TRY(tmap::encode_f32_rows_heads_d(&prm.dq_acc[r], acc, rows, pl->Hq_l, pl->D, 32));
+        prm.dq_accp[r] = acc;
+        prm.lse[r] = lse[r];
+        prm.delta[r] = delta;
+        prm.dk[r] = (__nv_bfloat16 *)dk[r];
+        prm.dv[r] = (__nv_bfloat16 *)dv[r];
+        hp.o[r] = (const __nv_bfloat16 *)o[r];
+        hp.dout[r] = (const __nv_bfloat16 *)dout[r];
+        hp.delta[r] = delta;
+        hp.acc[r] = acc;
+        hp.dq[r] = (__nv_bfloat16 *)dq[r];
+    }
+    prm.K = pl->K; prm.Bl = pl->Bl; prm.S = pl->S; prm.Hq_l = pl->Hq_l; prm.Hkv_l = pl->Hkv_l;
+    prm.q_per_kv = pl->Hq_l / pl->Hkv_l; prm.causal = pl->causal;
+    prm.n_tiles = (pl->S + kT - 1) / kT;
+    prm.Dg = pl->D;
+    const long long per = (long long)pl->K * pl->Hkv_l, total = (long long)pl->B * prm.n_tiles * per;
+    const long long row_threads = (long long)pl->Bl * pl->S * pl->Hq_l * 16, n8 = (long long)(acc_b / sizeof(float) / 8);
+    if (total >= (1ll << 31) - 4096 || rows >= (1ull << 31) || row_threads >= (1ll << 39)) return BASP_ERR_UNSUPPORTED;   // 31-bit items, rows, blocks
+    prm.total = (int)total;
+    prm.scale = scale;
+    prm.scale_log2 = scale * 1.4426950408889634f;
+    prm.status = basp_status_device_ptr();
+    if (!prm.status) return BASP_ERR_CUDA;
+    prm.div_items = make_fastdiv((uint32_t)per);
+    prm.div_hkv_l = make_fastdiv((uint32_t)pl->Hkv_l);
+    prm.div_B = make_fastdiv((uint32_t)pl->B);
+    prm.div_bl = make_fastdiv((uint32_t)pl->Bl);
+    int dev = 0, sms = 0;
+    BASP_CUDA_TRY(cudaGetDevice(&dev));
+    BASP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const int grid = (int)(total < sms ? total : sms);
+
+    BASP_CUDA_TRY(cudaMemsetAsync(ws, 0, (size_t)pl->N * acc_b, st));
+    bwd_delta_kernel<R><<<dim3((unsigned)((row_threads + 255) / 256), (unsigned)pl->N), 256, 0, st>>>(hp, pl->Bl, pl->S, pl->Hq_l, pl->D);
+    BASP_CUDA_TRY(cudaGetLastError());
+    BASP_TRY(dispatch_score(prm.score.cap_out > 0.f, prm.score.slopes != nullptr, [&](auto cap, auto bias) -> int {
+        constexpr bool kCap = decltype(cap)::value, kBias = decltype(bias)::value;
+        const auto go = [&](auto kernel, int smem) -> int {
+            BASP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+            kernel<<<grid, kBwdThreads, smem, st>>>(prm);
+            BASP_CUDA_TRY(cudaGetLastError());
+            return BASP_OK;
+        };
+        if (pl->D > 64)          // tiles, row statistics, windows, edge flags, barriers
+            return go(attn_masked_bwd_d128_kernel<R, kCap, kBias>, 7 * kT * 128 * 2 + 4 * kT * 4 + 2 * kT * 2 + 2 * 4 + (int)sizeof(BwdBars));
+        return go(attn_masked_bwd_d64_kernel<R, kCap, kBias>, (2 + 2 * 3) * kT * 64 * 2 + 4 * 16384 + 2 * 3 * kT * 4 + 3 * kT * 2 + 4 * 4 + (int)sizeof(BwdBars));
+    }));
+    bwd_dq_convert_kernel<R><<<dim3((unsigned)((n8 + 255) / 256), (unsigned)pl->N), 256, 0, st>>>(hp, n8);
+    BASP_CUDA_TRY(cudaGetLastError());
+    basp_count_launch(3);
+    return BASP_OK;
+}
+
+}  // namespace
+
+extern "C" size_t basp_attn_masked_bwd_workspace_bytes(const basp_plan *p) { return p ? mb_workspace_bytes(p) : 0; }
+
+extern "C" int basp_attn_masked_bwd(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                                    const void *const *v_head, const void *const *o_head, const void *const *do_head,
+                                    const float *const *lse_shards, void *const *dq_head, void *const *dk_head, void *const *dv_head,
+                                    void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
+    if (!pl || !score || !q_head || !k_head || !v_head || !o_head || !do_head || !lse_shards || !dq_head || !dk_head || !dv_head)
+        return BASP_ERR_NULL;
+    if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
+    if (pl->D < 16 || pl->D > 128 || pl->D % 16 != 0) return BASP_ERR_UNSUPPORTED;
+    SpanSet spans;
+    const size_t rows = (size_t)pl->Bl * pl->S, q_bytes = rows * pl->Hq_l * pl->D * 2, k_bytes = rows * pl->Hkv_l * pl->D * 2;
+    for (int r = 0; r < pl->N; ++r) {
+        const void *q_like[3] = {q_head[r], o_head[r], do_head[r]}, *k_like[2] = {k_head[r], v_head[r]};
+        for (const void *t : q_like) BASP_TRY(spans.add_in(t, q_bytes));
+        for (const void *t : k_like) BASP_TRY(spans.add_in(t, k_bytes));
+        BASP_TRY(spans.add_in(lse_shards[r], rows * pl->Hq_l * 4));
+        BASP_TRY(spans.add_out(dq_head[r], q_bytes));
+        BASP_TRY(spans.add_out(dk_head[r], k_bytes));
+        BASP_TRY(spans.add_out(dv_head[r], k_bytes));
+    }
+    if (score->slopes) BASP_TRY(spans.add_in(score->slopes, (size_t)pl->Hq * 4, 4));
+    if (score->mask) BASP_TRY(spans.add_in(score->mask, basp_mask_bytes(pl)));
+    BASP_TRY(spans.add_out(workspace, mb_workspace_bytes(pl)));
+    if (workspace_bytes < mb_workspace_bytes(pl)) return BASP_ERR_WORKSPACE;
+    BASP_TRY(spans.overlaps());
+    const float scale = softmax_scale == 0.f ? 1.f / sqrtf((float)pl->D) : softmax_scale;
+    return pl->N <= 8 ? mb_run<8>(pl, score, q_head, k_head, v_head, o_head, do_head, lse_shards, dq_head, dk_head, dv_head,
+                                  (char *)workspace, scale, (cudaStream_t)stream)
+                      : mb_run<BASP_MAX_RANKS>(pl, score, q_head, k_head, v_head, o_head, do_head, lse_shards, dq_head, dk_head, dv_head,
+                                               (char *)workspace, scale, (cudaStream_t)stream);
+}

@@ -30,9 +30,11 @@ extern "C" size_t basp_host_arena_bytes(const basp_plan *p) {
     return (size_t)p->N * (2 * q_shard_bytes(p) + 2 * kv_shard_bytes(p));  // sequence-sharded Q, K, V, O
 }
 
-extern "C" int basp_layer_fwd(const basp_plan *p, const void *const *q_seq, const void *const *k_seq,
-                              const void *const *v_seq, void *const *o_seq, float *const *lse_shards,
-                              void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
+namespace {
+// The three-launch layer with `attend(qh, kh, vh, oh)` as its attention.
+template <typename Attend>
+int layer_fwd_with(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *const *v_seq, void *const *o_seq,
+                   void *workspace, size_t workspace_bytes, float softmax_scale, void *stream, Attend &&attend) {
     if (!p || !workspace) return BASP_ERR_NULL;
     if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
     if (!aligned16(workspace)) return BASP_ERR_ALIGN;
@@ -48,9 +50,28 @@ extern "C" int basp_layer_fwd(const basp_plan *p, const void *const *q_seq, cons
     }
     int rc = basp_reshard_qkv_s2h(p, q_seq, k_seq, v_seq, qh, kh, vh, stream);
     if (rc != BASP_OK) return rc;
-    rc = basp_attn_dispatch(p, qh, kh, vh, oh, lse_shards, softmax_scale, false, stream);
+    rc = attend(qh, kh, vh, oh);
     if (rc != BASP_OK) return rc;
     return basp_reshard_h2s(p, p->Hq, oh, o_seq, stream);
+}
+}  // namespace
+
+extern "C" int basp_layer_fwd(const basp_plan *p, const void *const *q_seq, const void *const *k_seq,
+                              const void *const *v_seq, void *const *o_seq, float *const *lse_shards,
+                              void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
+    return layer_fwd_with(p, q_seq, k_seq, v_seq, o_seq, workspace, workspace_bytes, softmax_scale, stream,
+                          [&](void *const *qh, void *const *kh, void *const *vh, void *const *oh) {
+                              return basp_attn_dispatch(p, qh, kh, vh, oh, lse_shards, softmax_scale, false, stream);
+                          });
+}
+
+extern "C" int basp_layer_masked_fwd(const basp_plan *p, const basp_score *score, const void *const *q_seq, const void *const *k_seq,
+                                     const void *const *v_seq, void *const *o_seq, float *const *lse_shards, void *workspace,
+                                     size_t workspace_bytes, float softmax_scale, void *stream) {
+    return layer_fwd_with(p, q_seq, k_seq, v_seq, o_seq, workspace, workspace_bytes, softmax_scale, stream,
+                          [&](void *const *qh, void *const *kh, void *const *vh, void *const *oh) {
+                              return basp_attn_masked_fwd(p, score, qh, kh, vh, oh, lse_shards, softmax_scale, stream);
+                          });
 }
 
 extern "C" int basp_layer_workspace_shards(const basp_plan *p, void *workspace, void **q_head, void **k_head,
@@ -73,11 +94,11 @@ extern "C" size_t basp_layer_bwd_workspace_bytes(const basp_plan *p) {
     return (size_t)p->N * (2 * q_head_bytes(p) + 2 * kv_head_bytes(p)) + basp_attn_bwd_workspace_bytes(p);
 }
 
-extern "C" int basp_layer_bwd(const basp_plan *p, const void *const *q_head, const void *const *k_head,
-                              const void *const *v_head, const void *const *o_head, const float *const *lse_shards,
-                              const void *const *do_seq, void *const *dq_seq, void *const *dk_seq,
-                              void *const *dv_seq, void *workspace, size_t workspace_bytes, float softmax_scale,
-                              void *stream) {
+namespace {
+// The layer's backward pass with `attend(doh, dqh, dkh, dvh, workspace, bytes)` as that of its attention.
+template <typename Attend>
+int layer_bwd_with(const basp_plan *p, const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq,
+                   void *workspace, size_t workspace_bytes, float softmax_scale, void *stream, Attend &&attend) {
     if (!p || !workspace) return BASP_ERR_NULL;
     if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
     if (!aligned16(workspace)) return BASP_ERR_ALIGN;
@@ -94,10 +115,34 @@ extern "C" int basp_layer_bwd(const basp_plan *p, const void *const *q_head, con
     char *bwd_ws = w + (size_t)p->N * (2 * qb + 2 * kb);
     int rc = basp_reshard_s2h(p, p->Hq, do_seq, doh, stream);
     if (rc != BASP_OK) return rc;
-    rc = basp_attn_bwd(p, q_head, k_head, v_head, o_head, doh, lse_shards, dqh, dkh, dvh, bwd_ws,
-                       workspace_bytes - (size_t)(bwd_ws - w), softmax_scale, stream);
+    rc = attend(doh, dqh, dkh, dvh, bwd_ws, workspace_bytes - (size_t)(bwd_ws - w));
     if (rc != BASP_OK) return rc;
     return basp_reshard_grads_h2s(p, dqh, dkh, dvh, dq_seq, dk_seq, dv_seq, stream);
+}
+}  // namespace
+
+extern "C" int basp_layer_bwd(const basp_plan *p, const void *const *q_head, const void *const *k_head,
+                              const void *const *v_head, const void *const *o_head, const float *const *lse_shards,
+                              const void *const *do_seq, void *const *dq_seq, void *const *dk_seq,
+                              void *const *dv_seq, void *workspace, size_t workspace_bytes, float softmax_scale,
+                              void *stream) {
+    return layer_bwd_with(p, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes, softmax_scale, stream,
+                          [&](void *const *doh, void *const *dqh, void *const *dkh, void *const *dvh, void *ws, size_t bytes) {
+                              return basp_attn_bwd(p, q_head, k_head, v_head, o_head, doh, lse_shards, dqh, dkh, dvh, ws, bytes,
+                                                   softmax_scale, stream);
+                          });
+}
+
+// (the workspace holds that of basp_attn_bwd, which is the larger one)
+extern "C" int basp_layer_masked_bwd(const basp_plan *p, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                                     const void *const *v_head, const void *const *o_head, const float *const *lse_shards,
+                                     const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq,
+                                     void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
+    return layer_bwd_with(p, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes, softmax_scale, stream,
+                          [&](void *const *doh, void *const *dqh, void *const *dkh, void *const *dvh, void *ws, size_t bytes) {
+                              return basp_attn_masked_bwd(p, score, q_head, k_head, v_head, o_head, doh, lse_shards, dqh, dkh, dvh, ws,
+                                                          bytes, softmax_scale, stream);
+                          });
 }
 
 extern "C" size_t basp_layer_bwd_seq_workspace_bytes(const basp_plan *p) {
