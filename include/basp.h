@@ -431,7 +431,7 @@ size_t basp_lm_loss_grad_workspace_bytes(const basp_plan *plan, int hidden, int 
  *   z_ij = c tanh(scale q_i.k_j / c) - slope_h |i - j|     (i, j: places in the sequence),   visible iff begin_i <= j < end_i
  *   O_i = sum_j softmax_j(z_ij) v_j,   LSE_i = ln sum_j exp(z_ij);   a query that sees no key has O = 0 and LSE = -infinity
  * basp_score says which of it a call has:
- *   softcap    c; 0: no cap (negative, infinite, NaN, or a scale / c outside 1e-30..1e30: BASP_ERR_INVALID)
+ *   softcap    c; 0: no cap (negative, NaN, outside 1e-12..1e12, or a scale / c outside 1e-9..1e6: BASP_ERR_INVALID)
  *   slopes     device fp32 [Hq], the same for all sequences, of the whole layer's query heads in order; NULL: no bias.  Finite.
  *   mask       a mask object of this plan; NULL: the plan's own mask (causal or none)
  *
@@ -448,8 +448,8 @@ size_t basp_lm_loss_grad_workspace_bytes(const basp_plan *plan, int hidden, int 
  *                        begin_i = max(i - pos_i, i - window + 1),   end_i = max(i + 1, i - pos_i + prefix_i)
  *                      (where the two meet the window has the last word).  BASP_ERR_INVALID for a plan that is not causal.
  * Operands, layouts and limits as basp_attn_fwd and basp_attn_bwd; outputs may not overlap inputs (BASP_ERR_ALIAS).  bf16 operands, fp32
- * scores, softmax and sums, P and dS rounded to bf16 as operands.  K may hold anything where no query sees it; otherwise a hidden
- * element is multiplied by zero, so Q, K, V, O and dO have to be finite numbers in padding too.
+ * scores, softmax and sums, P and dS rounded to bf16 as operands.  What a mask hides is multiplied by zero: Q, K, V, O and dO have to
+ * be finite numbers in hidden places and padding too.
  * The backward pass takes the forward's O and LSE:
  *   P = exp(z - LSE),  dV_j = sum_i P_ij dO_i,  dZ_ij = P_ij (dO_i.v_j - dO_i.O_i),  dS = scale (1 - tanh^2) dZ,  dQ = dS K,  dK = dS^T Q
  * (no gradient for the slopes); keys that nothing sees get zeros.  dQ is summed by floating-point atomics.  workspace:

@@ -572,6 +572,149 @@ def lm_loss(x: np.ndarray, w: np.ndarray, labels: np.ndarray, weights: np.ndarra
     return out
 
 
+# --------------------------------------------------- masked and shaped attention, rotations of any positions, block norms
+def packed_ranges(positions: np.ndarray, prefix: np.ndarray | None = None, window: int = 0) -> tuple:
+    """Key ranges (begin, end) [B, S] of causal attention in packed documents, token by token: positions [B, S] in the own document
+    (negative: padding), prefix [B, S] tokens that all of the document sees, window keys back (0: all)."""
+    B, S = positions.shape
+    begin, end = np.zeros((B, S), dtype=np.int64), np.zeros((B, S), dtype=np.int64)
+    for b in range(B):
+        for i in range(S):
+            pos = int(positions[b, i])
+            if pos < 0:
+                continue
+            first, past = i - pos, i + 1
+            if prefix is not None:
+                past = max(past, first + int(prefix[b, i]))
+            if window:
+                first = max(first, i - window + 1)
+            first, past = max(0, min(S, first)), max(0, min(S, past))
+            if past > first:
+                begin[b, i], end[b, i] = first, past
+    return begin, end
+
+
+def attn_shaped(q, k, v, begin, end, cap: float = 0.0, slopes=None, scale: float | None = None, do=None, given=None) -> dict:
+    """Attention of one sequence with capped scores, a bias by distance and key ranges, in fp64: q [S, H, D], k, v [S, Hkv, D],
+    begin, end [S], slopes [H].  With do [S, H, D] its gradients too, from its own O and LSE or from given=(O [S, H, D], LSE [H, S]).
+    Besides the results: the sums of magnitudes that a rounding of P (`mag_o`, `mag_dv`) or dS (`mag_dq`, `mag_dk`) enters, those that
+    an error of a row's dO.v - dO.O enters (`row_dq`, `row_dk`, per unit of it in every row), and the largest |score| (`top`)."""
+    S, H, D = q.shape
+    g = H // k.shape[1]
+    scale = _scale(scale, D)
+    at = np.arange(S)
+    see = (at[None, :] >= begin[:, None]) & (at[None, :] < end[:, None])
+    any_key = see.any(1)
+    out = {n: np.zeros(q.shape) for n in ("o", "mag_o", "dq", "mag_dq", "row_dq")}
+    out.update({n: np.zeros(k.shape) for n in ("dk", "dv", "mag_dk", "mag_dv", "row_dk")})
+    out["lse"] = np.full((H, S), -np.inf)
+    out["top"] = 0.0
+    for h in range(H):
+        K, V = k[:, h // g], v[:, h // g]
+        s = scale * (q[:, h] @ K.T)
+        t = np.tanh(s / cap) if cap else np.zeros_like(s)
+        z = cap * t if cap else s
+        if slopes is not None:
+            z = z - slopes[h] * np.abs(at[:, None] - at[None, :])
+        out["top"] = max(out["top"], scale * float((np.abs(q[:, h]) @ np.abs(K).T).max()))
+        z = np.where(see, z, -np.inf)
+        top = np.where(any_key, z.max(1), 0.0)
+        e = np.exp(z - top[:, None])
+        total = e.sum(1)
+        with np.errstate(divide="ignore"):
+            out["lse"][h] = top + np.log(total)
+        p = e / np.where(any_key, total, 1.0)[:, None]
+        out["o"][:, h] = p @ V
+        out["mag_o"][:, h] = p @ np.abs(V)
+        if do is None:
+            continue
+        O = out["o"][:, h]
+        if given is not None:
+            O = given[0][:, h]
+            p = np.where(see & any_key[:, None], np.exp(z - np.where(any_key, given[1][h], 0.0)[:, None]), 0.0)
+        slope = scale * (1.0 - t * t)
+        ds = p * (do[:, h] @ V.T - (do[:, h] * O).sum(1)[:, None]) * slope
+        out["dq"][:, h] = ds @ K
+        out["mag_dq"][:, h] = np.abs(ds) @ np.abs(K)
+        out["row_dq"][:, h] = (p * slope) @ np.abs(K)
+        out["dk"][:, h // g] += ds.T @ q[:, h]
+        out["mag_dk"][:, h // g] += np.abs(ds).T @ np.abs(q[:, h])
+        out["row_dk"][:, h // g] += (p * slope).T @ np.abs(q[:, h])
+        out["dv"][:, h // g] += p.T @ do[:, h]
+        out["mag_dv"][:, h // g] += p.T @ np.abs(do[:, h])
+    return out
+
+
+def rope_frequencies(rotary: int, theta: float, scaling: str = "none", factor: float = 1.0, original_len: float = 0.0) -> tuple:
+    """Radians a token of every pair, and the factor on the rotated features, pair by pair."""
+    f, size = np.zeros(rotary // 2), 1.0
+    for j in range(rotary // 2):
+        w = theta ** (-2.0 * j / rotary)
+        turns = original_len * w / (2 * np.pi)
+        if scaling == "linear":
+            w = w / factor
+        elif scaling == "wavelength":                    # between one and four turns in the trained length: a mix
+            mix = min(1.0, max(0.0, (turns - 1.0) / 3.0))
+            w = mix * w + (1.0 - mix) * w / factor
+        elif scaling == "yarn":                          # between the pairs of 32 turns and of one: a ramp over the pairs
+            pair = lambda n: rotary * np.log(original_len / (n * 2 * np.pi)) / (2 * np.log(theta))
+            lo, hi = max(0.0, np.floor(pair(32.0))), min(rotary - 1.0, np.ceil(pair(1.0)))
+            mix = min(1.0, max(0.0, (j - lo) / max(hi - lo, 0.001)))
+            w = (1.0 - mix) * w + mix * w / factor
+            size = 0.1 * np.log(factor) + 1.0
+        f[j] = w
+    return f, size
+
+
+def rope_any(x: np.ndarray, positions, frequencies, factor: float = 1.0, interleaved: bool = False, inverse: bool = False) -> np.ndarray:
+    """Rotation of the first features of x [tokens, H, D] by the tokens' positions, pair by pair; the others stay."""
+    y = np.array(x, dtype=np.float64)
+    half = len(frequencies)
+    for j in range(half):
+        u, v = (2 * j, 2 * j + 1) if interleaved else (j, j + half)
+        a = np.asarray(positions, dtype=np.float64)[:, None] * frequencies[j] * (-1.0 if inverse else 1.0)
+        y[..., u] = factor * (x[..., u] * np.cos(a) - x[..., v] * np.sin(a))
+        y[..., v] = factor * (x[..., v] * np.cos(a) + x[..., u] * np.sin(a))
+    return y
+
+
+def block_norm(x, y, w_post, gate, w_pre, scale: float, eps: float) -> tuple:
+    """h = x + scale gate norm(y; w_post) and n = norm(h; w_pre) on rows [tokens, hidden] in fp64 (None: not there)."""
+    rms = lambda t: np.sqrt((t * t).mean(-1, keepdims=True) + eps)
+    h = x
+    if y is not None:
+        z = y if w_post is None else y / rms(y) * w_post
+        h = x + scale * (z if gate is None else z * gate)
+    return h, None if w_pre is None else h / rms(h) * w_pre
+
+
+def block_norm_bwd(h, y, w_post, gate, w_pre, scale: float, eps: float, dh, dn) -> dict:
+    """Gradients of `block_norm` by the chain rule, step by step, from the sum h (None: not there)."""
+    def norm_bwd(t, w, up):
+        s = (t * t).mean(-1, keepdims=True) + eps
+        dw = (up * t / np.sqrt(s)).sum(0)
+        up = up * w
+        ds = (up * t).sum(-1, keepdims=True) * (-0.5) * s ** -1.5
+        return up / np.sqrt(s) + ds * 2.0 * t / t.shape[-1], dw
+
+    out = {}
+    total = 0.0 if dh is None else dh
+    if w_pre is not None:
+        more, out["dw_pre"] = norm_bwd(h, w_pre, dn)
+        total = total + more
+    out["dx"] = total
+    dz = scale * total
+    if gate is not None:
+        s = (y * y).mean(-1, keepdims=True) + eps
+        z = y if w_post is None else y / np.sqrt(s) * w_post
+        out["dgate"] = (dz * z).sum(0)
+        dz = dz * gate
+    out["dy"] = dz
+    if w_post is not None:
+        out["dy"], out["dw_post"] = norm_bwd(y, w_post, dz)
+    return out
+
+
 # ----------------------------------------------------------------- bf16 helpers
 def bf16_bits_to_f64(bits: np.ndarray) -> np.ndarray:
     """Exact widening of bf16 bit patterns to fp64."""

@@ -3,7 +3,10 @@ basp_layer_fwd, backward = basp_layer_bwd, or with fused=True basp_layer_fwd_fus
 computed in Python).
 
     q_seq, k_seq = basp_qk_norm_rope(plan, q_seq, k_seq, w_q, w_k, cos, sin)   # head norms and rotation
+    q_seq, k_seq = basp_rope(plan, rope, q_seq, k_seq, positions)              # or the rotation alone, positions of packed documents
     o_seq = basp_attention(plan, q_seq, k_seq, v_seq)          # lists of n_ranks sequence-sharded bf16 tensors
+    o_seq = basp_attention(plan, q_seq, k_seq, v_seq, score=score)             # capped, biased, masked (binding.basp_score)
+    h_seq, n_seq = basp_block_norm(plan, x_seq, y_seq, w_post, gate, w_pre)    # norms, gate and sum between two blocks
     loss = basp_lm_loss(plan, x_seq, w, labels)                # cross entropy over the vocabulary, a scalar
     loss.backward()                                            # gradients arrive on the inputs
 
@@ -31,8 +34,10 @@ from . import binding
 
 class _BaspAttention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, plan, softmax_scale, fused, checkpoint8, grads, *shards):
+    def forward(ctx, plan, softmax_scale, fused, checkpoint8, score, grads, *shards):
         n = plan.N
+        if score is not None and fused:
+            raise ValueError("score goes without fused (the fused kernel has the plan's own mask)")
         if checkpoint8 and not fused:
             raise ValueError("checkpoint8 goes with fused=True (the other form keeps its head-sharded copies)")
         if len(shards) != 3 * n:
@@ -55,8 +60,13 @@ class _BaspAttention(torch.autograd.Function):
                 ctx.save_for_backward(*shards, *o_seq)
         else:
             ws = torch.empty(binding.basp_workspace_bytes(plan), dtype=torch.uint8, device=dev)
-            binding.basp_layer_fwd(plan, list(q_seq), list(k_seq), list(v_seq), o_seq, ws, lse_shards=lse,
-                                   softmax_scale=softmax_scale)
+            if score is not None:
+                with torch.cuda.device(dev):
+                    binding.basp_layer_masked_fwd(plan, score, q_seq, k_seq, v_seq, o_seq, ws, lse_shards=lse, softmax_scale=softmax_scale)
+            else:
+                binding.basp_layer_fwd(plan, list(q_seq), list(k_seq), list(v_seq), o_seq, ws, lse_shards=lse,
+                                       softmax_scale=softmax_scale)
+        ctx.score = score
         ctx.plan, ctx.softmax_scale, ctx.ws, ctx.lse, ctx.fused, ctx.checkpoint8 = plan, softmax_scale, ws, lse, fused, checkpoint8
         ctx.shapes = [t.shape for t in shards]
         return tuple(o_seq)
@@ -73,28 +83,125 @@ class _BaspAttention(torch.autograd.Function):
             ws2 = torch.empty(binding.basp_layer_bwd_seq_workspace_bytes(plan), dtype=torch.uint8, device=dev)
             binding.basp_layer_bwd_ckpt(plan, ctx.saved_tensors, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:], ws2,
                                         softmax_scale=ctx.softmax_scale)
-            return (None, None, None, None, None, *grads)
+            return (None, None, None, None, None, None, *grads)
         if ctx.fused:
             saved = ctx.saved_tensors
             q_seq, k_seq, v_seq, o_seq = (list(saved[i * n:(i + 1) * n]) for i in range(4))
             ws2 = torch.empty(binding.basp_layer_bwd_seq_workspace_bytes(plan), dtype=torch.uint8, device=dev)
             binding.basp_layer_bwd_seq(plan, q_seq, k_seq, v_seq, o_seq, ctx.lse, do_seq, grads[:n], grads[n:2 * n],
                                        grads[2 * n:], ws2, softmax_scale=ctx.softmax_scale)
-            return (None, None, None, None, None, *grads)
+            return (None, None, None, None, None, None, *grads)
         qh, kh, vh, oh = (binding.as_shards(a) for a in binding.basp_layer_workspace_shards(plan, ctx.ws))
         ws2 = torch.empty(binding.basp_layer_bwd_workspace_bytes(plan), dtype=torch.uint8, device=dev)
-        binding.basp_layer_bwd(plan, qh, kh, vh, oh, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:], ws2,
-                               softmax_scale=ctx.softmax_scale)
-        return (None, None, None, None, None, *grads)
+        if ctx.score is not None:
+            with torch.cuda.device(dev):
+                binding.basp_layer_masked_bwd(plan, ctx.score, qh, kh, vh, oh, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:],
+                                              ws2, softmax_scale=ctx.softmax_scale)
+        else:
+            binding.basp_layer_bwd(plan, qh, kh, vh, oh, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:], ws2,
+                                   softmax_scale=ctx.softmax_scale)
+        return (None, None, None, None, None, None, *grads)
 
 
-def basp_attention(plan, q_seq, k_seq, v_seq, softmax_scale: float = 0.0, fused: bool = False, checkpoint8: bool = False):
+def basp_attention(plan, q_seq, k_seq, v_seq, softmax_scale: float = 0.0, fused: bool = False, checkpoint8: bool = False, score=None):
     """Causal (or, per the plan, unmasked) attention over the group-sharded sequences of `plan`: the two group-local
     all-to-alls and the attention of Section IV-C, differentiable.  Returns the list of n_ranks output shards in the
     layout of q_seq.  checkpoint8 (with fused): keep Q, K, V and O in 8 bits for the backward; O besides what others keep of it.
-    Second derivatives are refused."""
-    return list(_BaspAttention.apply(plan, float(softmax_scale), bool(fused), bool(checkpoint8), torch.is_grad_enabled(), *q_seq,
+    score (without fused): a binding.basp_score, for capped scores, a bias by distance and masks of documents, prefixes, windows or
+    any key ranges; its tensors are read again by the backward and get no gradients.  Second derivatives are refused."""
+    if score is not None and score.slopes is not None and score.slopes.requires_grad:
+        raise ValueError("the slopes of a score are not differentiable")
+    return list(_BaspAttention.apply(plan, float(softmax_scale), bool(fused), bool(checkpoint8), score, torch.is_grad_enabled(), *q_seq,
                                      *k_seq, *v_seq))
+
+
+class _Rope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, plan, rope, positions, *shards):
+        n = plan.N
+        if len(shards) != 2 * n:
+            raise ValueError(f"expected {2 * n} shards (q, k of {n} ranks), got {len(shards)}")
+        out = [torch.empty_like(t) for t in shards]
+        with torch.cuda.device(shards[0].device):
+            binding.basp_rope(plan, rope, shards[:n], shards[n:], out[:n], out[n:], positions=positions)
+        ctx.plan, ctx.rope, ctx.has_positions = plan, rope, positions is not None
+        ctx.shapes = [t.shape for t in shards]
+        if positions is not None:
+            ctx.save_for_backward(positions)
+        return tuple(out)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *d_out):
+        plan, n = ctx.plan, ctx.plan.N
+        positions = ctx.saved_tensors[0] if ctx.has_positions else None
+        dev = next(g.device for g in d_out if g is not None)
+        d_out = [torch.zeros(s, dtype=torch.bfloat16, device=dev) if g is None else g.contiguous() for g, s in zip(d_out, ctx.shapes)]
+        grads = [torch.empty_like(t) for t in d_out]
+        with torch.cuda.device(dev):
+            binding.basp_rope(plan, ctx.rope, d_out[:n], d_out[n:], grads[:n], grads[n:], positions=positions, inverse=True)
+        return (None, None, None, *grads)
+
+
+def basp_rope(plan, rope, q_seq, k_seq, positions=None):
+    """Rotary positions on sequence-sharded Q and K (rope: of binding.basp_rope_make; positions: int32 [B, S], None: the place in the
+    sequence); differentiable in the shards.  Returns (q shards, k shards)."""
+    out = _Rope.apply(plan, rope, positions, *q_seq, *k_seq)
+    return list(out[:plan.N]), list(out[plan.N:])
+
+
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, plan, res_scale, eps, w_post, gate, w_pre, *shards):
+        n, has_y = plan.N, len(shards) == 2 * plan.N
+        if len(shards) not in (n, 2 * n):
+            raise ValueError(f"expected {n} or {2 * n} shards (x, and y where there is a block before, of {n} ranks), got {len(shards)}")
+        x, y = shards[:n], shards[n:] if has_y else None
+        hidden = x[0].shape[-1]
+        h = [torch.empty_like(t) for t in x] if has_y else None
+        after = [torch.empty_like(t) for t in x] if w_pre is not None else None
+        with torch.cuda.device(x[0].device):
+            binding.basp_block_norm(plan, hidden, x, y, h, after, w_post=w_post, gate=gate, w_pre=w_pre, res_scale=res_scale, eps=eps)
+        ctx.plan, ctx.res_scale, ctx.eps, ctx.hidden, ctx.has_y = plan, res_scale, eps, hidden, has_y
+        ctx.has = [t is not None for t in (w_post, gate, w_pre)]
+        ctx.shapes = [t.shape for t in x]
+        ctx.save_for_backward(*[t for t in (w_post, gate, w_pre) if t is not None], *((h if has_y else x) if w_pre is not None else ()),
+                              *(y if w_post is not None or gate is not None else ()))
+        return tuple((h or []) + (after or []))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *d_out):
+        plan, n = ctx.plan, ctx.plan.N
+        saved = list(ctx.saved_tensors)
+        w_post, gate, w_pre = [saved.pop(0) if there else None for there in ctx.has]
+        h = [saved.pop(0) for _ in range(n)] if w_pre is not None else None
+        y = saved if w_post is not None or gate is not None else None
+        dev = next(g.device for g in d_out if g is not None)
+        fill = lambda gs: [torch.zeros(s, dtype=torch.bfloat16, device=dev) if g is None else g.contiguous() for g, s in zip(gs, ctx.shapes)]
+        dh, dn = (d_out[:n], d_out[n:]) if ctx.has_y else ([], d_out)
+        dn = fill(dn) if w_pre is not None else None
+        # the stream's own gradient may be missing (the last sum's) where that through the norm is there
+        dh = None if dn is not None and all(g is None for g in dh) else fill(dh)
+        dx = [torch.empty(s, dtype=torch.bfloat16, device=dev) for s in ctx.shapes]
+        dy = [torch.empty_like(t) for t in dx] if ctx.has_y else None
+        sums = [torch.empty(ctx.hidden, dtype=torch.float32, device=dev) if there else None for there in ctx.has]
+        ws = torch.empty(binding.basp_block_norm_bwd_workspace_bytes(plan, ctx.hidden), dtype=torch.uint8, device=dev)
+        with torch.cuda.device(dev):
+            binding.basp_block_norm_bwd(plan, ctx.hidden, h, y, dh, dn, dx, dy, *sums, ws, w_post=w_post, gate=gate, w_pre=w_pre,
+                                        res_scale=ctx.res_scale, eps=ctx.eps)
+        return (None, None, None, *[None if s is None else s.to(torch.bfloat16) for s in sums], *dx, *(dy or []))
+
+
+def basp_block_norm(plan, x_seq, y_seq=None, w_post=None, gate=None, w_pre=None, res_scale: float = 1.0, eps: float = 1e-6):
+    """h = x + res_scale gate norm(y; w_post) and n = norm(h; w_pre) on the ranks' rows (bf16 [..., hidden]): the edge between two blocks.
+    Without y_seq (the first block) h is x itself; without w_pre (the last one) n is None.  Returns (h shards, n shards);
+    differentiable in the shards and the weights."""
+    n = plan.N
+    out = _BlockNorm.apply(plan, float(res_scale), float(eps), w_post, gate, w_pre, *x_seq, *(y_seq or []))
+    if y_seq is None:
+        return list(x_seq), list(out)
+    return list(out[:n]), list(out[n:]) or None
 
 
 class _QkNormRope(torch.autograd.Function):

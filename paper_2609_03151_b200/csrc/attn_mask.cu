@@ -192,10 +192,16 @@ int basp_score_args(const basp_plan *p, const basp_score *score, float scale, Sc
     if (!score) return BASP_ERR_NULL;
     if (!(score->softcap >= 0.f && score->softcap <= 3.0e38f)) return BASP_ERR_INVALID;
     if (score->softcap > 0.f) {
-        out->cap_in = scale / score->softcap;
-        out->cap_out = score->softcap * 1.4426950408889634f;
-        // both have to be ordinary numbers: the kernels divide by one and multiply by the other
-        if (!(out->cap_in >= 1e-30f && out->cap_in <= 1e30f && out->cap_out >= 1e-30f && out->cap_out <= 1e30f)) return BASP_ERR_INVALID;
+        const double in = (double)scale / score->softcap, log2e = 1.4426950408889634;
+        // (the kernels take one and the other, and its square and that's reciprocal, as fp32 numbers)
+        if (!(in >= 1e-9 && in <= 1e6 && score->softcap >= 1e-12f && score->softcap <= 1e12f)) return BASP_ERR_INVALID;
+        out->cap_in = (float)in;
+        out->cap_out = (float)(score->softcap * log2e);
+        const double c[4] = {0.99999988, -0.33331361, 0.13270971, -0.047553331};
+        double power = scale * log2e;                       // softcap log2(e) in^(2k + 1)
+        for (int k = 0; k < 4; ++k, power *= in * in) out->near[k] = (float)(c[k] * power);
+        // the powers have to be fp32 numbers: below 1e-6 the last one is not, and is not needed up to 0.05; above 1e3 they overflow
+        out->near_limit = in > 1e3 ? -1.f : (float)((in < 1e-6 ? 0.05 : 0.4) / in);
     }
     if ((uintptr_t)score->slopes & 3) return BASP_ERR_ALIGN;
     out->slopes = score->slopes;

@@ -46,7 +46,8 @@ struct ScoreArgs {
     const MaskFwdEntry *fwd;
     const MaskBwdEntry *bwd;
     const float *slopes;            // [Hq]
-    float cap_in, cap_out;          // scale / softcap and softcap * log2(e)
+    float cap_in, cap_out;          // scale / softcap and softcap * log2(e); 0: no cap
+    float near[4], near_limit;      // coefficients of the capped score near zero (score.cuh), and up to which raw score
     int B;
 };
 

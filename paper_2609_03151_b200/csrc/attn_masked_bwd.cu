@@ -101,28 +101,36 @@ __device__ __forceinline__ void stage_windows(const MaskedBwdParams<R> &p, const
     if (lane == 0) *edge = look;
 }
 
-// Thirty-two scores of a key row (queries side by side): the probabilities as bf16 to pk, and times the cap's derivative to st.
+// Thirty-two scores of a key row (queries side by side): the probabilities as bf16 to the tensor memory at `to`, sixteen at a time, and
+// times the cap's derivative to st.
 // dist: the first query's position minus the key's; side: its sign, tile by tile; win: what stage_windows left, where it matters.
 template <bool kCap, bool kBias, bool kEdge>
-__device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t (&pk)[16], const float *lse, const uint16_t *win, int row,
+__device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t to, const float *lse, const uint16_t *win, int row,
                                              const ScoreArgs &a, float scale_log2, float slope, int dist, int side) {
-    float sl = 0.f, base = 0.f;
+    [[maybe_unused]] float sl = 0.f, base = 0.f;
     if constexpr (kBias) {
         sl = side < 0 ? slope : -slope;              // -slope |dist + c| = sl c + base on either side of the key
         base = sl * (float)dist;
     }
-    const uint64_t sl2 = both(sl), base2 = both(base), minus2 = both(-1.f);
-    bool far = false;
+    [[maybe_unused]] const uint64_t shrink = both(-1.f / (a.cap_out * a.cap_out));
+    const uint64_t minus2 = both(-1.f);
+    [[maybe_unused]] bool far = false;
     if constexpr (kCap) {
         float top[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < 32; c += 4)
 #pragma unroll
             for (int k = 0; k < 2; ++k) top[k] = max3_abs(top[k], __uint_as_float(st[c + 2 * k]), __uint_as_float(st[c + 2 * k + 1]));
-        far = __any_sync(0xffffffffu, fmaxf(top[0], top[1]) * a.cap_in > kTanhNear);
+        far = __any_sync(0xffffffffu, fmaxf(top[0], top[1]) > a.near_limit);
+    }
+    [[maybe_unused]] uint64_t ramp[2], block = 0;    // the bias of pair c as ramp + block: no constants in the code
+    if constexpr (kBias) {
+        ramp[0] = pack_f2(0.f, sl);
+        ramp[1] = pack_f2(2.f * sl, 3.f * sl);
     }
     const auto columns = [&](auto far_tag) {
         [[maybe_unused]] constexpr bool kFar = decltype(far_tag)::value;
+        uint32_t pk[8];
 #pragma unroll
         for (int c = 0; c < 32; c += 4) {
             const float4 l4 = *reinterpret_cast<const float4 *>(lse + c);
@@ -131,28 +139,30 @@ __device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t (&pk)[
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int i = c + 2 * h;
-                uint64_t off = mul2(h ? pack_f2(l4.z, l4.w) : pack_f2(l4.x, l4.y), minus2);
-                if constexpr (kBias) off = add2(off, fma2(pack_f2((float)i, (float)(i + 1)), sl2, base2));
+                uint64_t off = h ? pack_f2(l4.z, l4.w) : pack_f2(l4.x, l4.y);          // -LSE and the bias
+                if constexpr (kBias) {
+                    if (h == 0) block = both(fmaf(sl, (float)c, base));
+                    off = fma2(off, minus2, add2(ramp[h], block));
+                } else off = mul2(off, minus2);
                 const uint64_t s2 = pack_f2(__uint_as_float(st[i]), __uint_as_float(st[i + 1]));
-                [[maybe_unused]] uint64_t t = 0;
+                [[maybe_unused]] uint64_t capped = 0;
                 uint64_t z;
                 if constexpr (!kCap) {
                     z = fma2(s2, both(scale_log2), off);
+                } else if constexpr (kFar) {
+                    capped = pack_f2(tanh_far(__uint_as_float(st[i]) * a.cap_in) * a.cap_out, tanh_far(__uint_as_float(st[i + 1]) * a.cap_in) * a.cap_out);
+                    z = add2(capped, off);
                 } else {
-                    if constexpr (kFar) {
-                        t = pack_f2(tanh_far(__uint_as_float(st[i]) * a.cap_in), tanh_far(__uint_as_float(st[i + 1]) * a.cap_in));
-                    } else {
-                        const uint64_t x = mul2(s2, both(a.cap_in));
-                        t = mul2(x, tanh_near_q(x));
-                    }
-                    z = fma2(t, both(a.cap_out), off);
+                    const uint64_t q = cap_near_q(mul2(s2, s2), a);
+                    capped = mul2(s2, q);
+                    z = fma2(s2, q, off);
                 }
                 float z0, z1;
                 unpack_f2(z, z0, z1);
                 if constexpr (kBias && kEdge) {       // the diagonal tile has queries on both sides of the key
                     if (side == 0) {
-                        z0 += 2.f * slope * (float)min(dist + i, 0);
-                        z1 += 2.f * slope * (float)min(dist + i + 1, 0);
+                        z0 = fmaf(2.f * slope, fminf((float)dist + (float)i, 0.f), z0);
+                        z1 = fmaf(2.f * slope, fminf((float)dist + (float)(i + 1), 0.f), z1);
                     }
                 }
                 float p0 = exp2_approx(z0), p1 = exp2_approx(z1);
@@ -161,14 +171,12 @@ __device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t (&pk)[
                     if (!(row >= (int)(w & 0xff) && row < (int)((w >> 8) & 0xff))) p0 = 0.f;
                     if (!(row >= (int)((w >> 16) & 0xff) && row < (int)(w >> 24))) p1 = 0.f;
                 }
-                pk[i >> 1] = pack_bf16x2(p0, p1);
-                if constexpr (kCap) {
-                    const uint64_t g = mul2(pack_f2(p0, p1), fma2(mul2(t, minus2), t, both(1.f)));
-                    unpack_f2(g, p0, p1);
-                }
+                pk[(i >> 1) & 7] = pack_bf16x2(p0, p1);
+                if constexpr (kCap) unpack_f2(mul2(pack_f2(p0, p1), fma2(mul2(capped, capped), shrink, both(1.f))), p0, p1);
                 st[i] = __float_as_uint(p0);
                 st[i + 1] = __float_as_uint(p1);
             }
+            if (c % 16 == 12) tmem_st_x8(to + c / 16 * 8, pk);
         }
     };
     if constexpr (kCap) {

@@ -79,13 +79,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
                     // P^T = exp2(z^T - LSE), the scores' shape included: needs the scores only.  What stays in st is P^T times the
                     // derivative of the cap
                     {
-                        uint32_t pk[16];
                         const int dist = (m - item.n) * kT + 32 * g - row;      // position of the first column's query minus the key's
                         if (s_edge[stage] || (kBias && m == item.n))
-                            shaped_probs<kCap, kBias, true>(st, pk, lse_b, s_win + stage * kT + 32 * g, row, p.score, p.scale_log2, slope, dist, m - item.n);
+                            shaped_probs<kCap, kBias, true>(st, st_col, lse_b, s_win + stage * kT + 32 * g, row, p.score, p.scale_log2, slope, dist, m - item.n);
                         else
-                            shaped_probs<kCap, kBias, false>(st, pk, lse_b, nullptr, row, p.score, p.scale_log2, slope, dist, m - item.n);
-                        tmem_st_x16(st_col, pk);
+                            shaped_probs<kCap, kBias, false>(st, st_col, lse_b, nullptr, row, p.score, p.scale_log2, slope, dist, m - item.n);
                     }
                     tmem_wait_st();
                     tc_fence_before();

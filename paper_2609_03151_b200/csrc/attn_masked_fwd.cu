@@ -11,9 +11,9 @@
 //   - only tiles that are not wholly visible are masked, with the bounds of the thread's row.  A row can meet such a
 //     tile before it has seen any key: its reference stays -inf and its exponentials are taken against 0.
 //   - items are dealt longest first in the mask object's order.
-//   - the scores are shaped in registers behind their load.  tanh runs on the FMA pipe as an odd polynomial where all of a warp's
-//     scores are below half the cap (Chebyshev nodes, relative error below 3e-8), since the exponentials already fill the special-
-//     function unit: with tanh as 1 - 2 / (exp(2x) + 1) everywhere that unit has 2.5 operations per score and not one.
+//   - the scores are shaped on their way into the exponentials.  tanh runs on the FMA pipe as an odd polynomial where all of a warp's
+//     scores are below 0.4 of the cap (score.cuh), since the exponentials already fill the special-function unit: 1 - 2 / (exp(2x) + 1)
+//     for every score would give that unit three operations where it has one.
 #include <cuda.h>
 #include <math.h>
 
@@ -44,7 +44,7 @@ struct MaskedFwdParams {
     int K, Bl, S, Hq, Hq_l, Hkv_l, n_tiles, n_blocks, total;   // total: work items
     int Dg;                      // head dimension in memory; the tile loads zero-fill the columns past it
     int causal, has_lse;         // causal: of the plan, where there is no mask object
-    float scale_log2;            // softmax scale * log2(e); 1 where the scores are shaped (they are in log2 units then)
+    float scale_log2;            // softmax scale * log2(e)
     int *status;
     FastDiv div_items, div_hq_l, div_q_per_kv, div_B, div_bl;
 };
@@ -199,8 +199,21 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
             } else if (s_pos < p.S) {
                 hi = p.causal ? s_pos + 1 : p.S;
             }
-            const float slope = kBias ? __ldg(p.score.slopes + (item.r % p.K) * p.Hq_l + item.h) * 1.4426950408889634f : 0.f;
+            // log2 units; the bound on a tile's bias is at most 127 |slope| above what any of its keys has, and a reference that is
+            // up to 2^96 too large leaves the exponentials ordinary numbers (24 bits above 2^-126)
+            [[maybe_unused]] const float slope = kBias ? __ldg(p.score.slopes + (item.r % p.K) * p.Hq_l + item.h) * 1.4426950408889634f : 0.f;
+            // With a cap no maximum is needed: |z| is at most the cap (in log2 units, 80 at most for this), so the exponentials of the
+            // row are ordinary numbers against the bias that its nearest key has (its furthest, for a negative slope), or 0.
+            [[maybe_unused]] const bool bounded = kCap && p.score.cap_out <= 80.f;
+            [[maybe_unused]] const bool steep = kBias && !bounded && fabsf(slope) * (float)(kTile - 1) > 96.f;
             float m_ref = -INFINITY, l_run = 0.f;
+            if (bounded) {
+                m_ref = 0.f;
+                if constexpr (kBias) {
+                    const int dist = slope >= 0.f ? max(max(lo - s_pos, s_pos - hi + 1), 0) : max(s_pos - lo, hi - 1 - s_pos);
+                    if (hi > lo) m_ref = -slope * (float)dist;
+                }
+            }
             for (int j = begin; j < end; ++j, ++it_cnt) {
                 MF_WAIT(&sh.s_full[t], it_cnt & 1, 10 + t, j);
                 tc_fence_after();
@@ -213,8 +226,29 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.s_free);       // the scores are in registers: the other tile's Q.K^T may overwrite S
-                if constexpr (kShaped) shape_scores<kCap, kBias>(s, p.score, p.scale_log2, slope, s_pos - j * kTile, j - qt);
-                if (j < full || j >= full_end) {     // keys outside of [lo, hi) are hidden
+                // Keys outside of [lo, hi) are hidden.  The scores stay raw and are shaped on the way into the exponentials: the maximum
+                // is taken over raw scores (the bias of a tile has a bound), or not at all (a capped score has one); only where neither
+                // holds (`slow`) are they shaped in place first.  What is rare is laid out of line: the loop has to fit the
+                // instruction caches.
+                const bool edge = j < full || j >= full_end;
+                [[maybe_unused]] float sl = 0.f, base = 0.f;                 // bias of key i: sl i + base
+                [[maybe_unused]] bool slow = kCap && !bounded, far = false;
+                if constexpr (kBias) {
+                    sl = j <= qt ? slope : -slope;
+                    base = -sl * (float)(s_pos - j * kTile);
+                    slow |= steep || (j == qt && __any_sync(0xffffffffu, min(hi - j * kTile, kTile) - 1 > row));
+                }
+                if constexpr (kCap) {
+                    float top[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < kTile; i += 8)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) top[k] = max3_abs(top[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+                    far = __any_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) > p.score.near_limit);
+                }
+                if constexpr (kShaped)
+                    if (__builtin_expect(slow, 0)) shape_scores<kCap, kBias>(s, p.score, p.scale_log2, slope, s_pos - j * kTile);
+                if (__builtin_expect(edge, 0)) {
                     const int first = lo - j * kTile, past = hi - j * kTile;
                     if (__any_sync(0xffffffffu, first > 0)) {
 #pragma unroll
@@ -227,45 +261,116 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
                             if (i >= past) s[i] = 0xff800000u;
                     }
                 }
-                float mxs[8];
+                float alpha = 1.f;
+                if (!kCap || slow) {
+                    float mxs[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) mxs[i] = max3(__uint_as_float(s[i]), __uint_as_float(s[8 + i]), __uint_as_float(s[16 + i]));
+                    for (int i = 0; i < 8; ++i) mxs[i] = max3(__uint_as_float(s[i]), __uint_as_float(s[8 + i]), __uint_as_float(s[16 + i]));
 #pragma unroll
-                for (int i = 24; i + 15 < kTile; i += 16)
+                    for (int i = 24; i + 15 < kTile; i += 16)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        mxs[k] = max3(mxs[k], __uint_as_float(s[i + k]), __uint_as_float(s[i + 8 + k]));
+                        for (int k = 0; k < 8; ++k)
+                            mxs[k] = max3(mxs[k], __uint_as_float(s[i + k]), __uint_as_float(s[i + 8 + k]));
 #pragma unroll
-                for (int k = 0; k < 8; ++k) mxs[k] = fmaxf(mxs[k], __uint_as_float(s[120 + k]));
-                float mx = fmaxf(fmaxf(fmaxf(mxs[0], mxs[1]), fmaxf(mxs[2], mxs[3])),
-                                 fmaxf(fmaxf(mxs[4], mxs[5]), fmaxf(mxs[6], mxs[7])));
-                if constexpr (!kShaped) mx = mx == -INFINITY ? mx : mx * p.scale_log2;     // (a scale of 0 is never passed on, but may underflow)
-                float m_new = m_ref, alpha = 1.f;
-                if (mx > m_ref + kMfRescale) { m_new = mx; alpha = exp2_approx(m_ref - m_new); }
+                    for (int k = 0; k < 8; ++k) mxs[k] = fmaxf(mxs[k], __uint_as_float(s[120 + k]));
+                    float mx = fmaxf(fmaxf(fmaxf(mxs[0], mxs[1]), fmaxf(mxs[2], mxs[3])),
+                                     fmaxf(fmaxf(mxs[4], mxs[5]), fmaxf(mxs[6], mxs[7])));
+                    if (!slow && mx != -INFINITY) {
+                        mx *= p.scale_log2;
+                        if constexpr (kBias) mx += fmaxf(base, fmaf(sl, (float)(kTile - 1), base));
+                    }
+                    if (mx > m_ref + kMfRescale) { alpha = exp2_approx(m_ref - mx); m_ref = mx; }
+                }
                 sh.alpha[t][it_cnt & 1][row] = alpha;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.alpha_full[t][it_cnt & 1]);
-                m_ref = m_new;
-                const float m_sub = m_new == -INFINITY ? 0.f : m_new;      // no key yet: every exponential is exp2(-inf) = 0
-                const uint64_t sc2 = pack_f2(p.scale_log2, p.scale_log2), nm2 = pack_f2(-m_sub, -m_sub);
+                const float m_sub = m_ref == -INFINITY ? 0.f : m_ref;      // no key yet: every exponential is exp2(-inf) = 0
                 uint64_t rs2[2] = {0ull, 0ull};
+                // kKind: 0 raw scores, 1 in log2 units already, 2 capped by the polynomial, 3 capped by the formula that holds everywhere;
+                // kEdge: some are -inf (where it makes a difference)
+                // kCols: of the first kCols scores; the bias of the first one is `from`
+                auto exp_row = [&](auto kind_tag, auto edge_tag, [[maybe_unused]] float from) {
+                    constexpr int kKind = decltype(kind_tag)::value, kCols = kShaped ? kTile / 2 : kTile;
+                    [[maybe_unused]] constexpr bool kEdge = decltype(edge_tag)::value;
+                    const uint64_t sc2 = both(p.scale_log2), nm2 = both(-m_sub);
+                    [[maybe_unused]] uint64_t ramp[4], block = 0;         // the bias of pair i as ramp + block: no constants in the code
+                    if constexpr (kBias && kKind != 1)
 #pragma unroll
-                for (int i = 0; i < kTile; i += 2) {
-                    const uint64_t s2 = pack_f2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-                    const uint64_t x2 = kShaped ? add2(s2, nm2) : fma2(s2, sc2, nm2);
-                    float x0, x1;
-                    unpack_f2(x2, x0, x1);
-                    const float e0 = exp2_approx(x0), e1 = exp2_approx(x1);
-                    rs2[(i >> 1) & 1] = add2(rs2[(i >> 1) & 1], pack_f2(e0, e1));
-                    s[i >> 1] = pack_bf16x2(e0, e1);
+                        for (int k = 0; k < 4; ++k) ramp[k] = pack_f2(sl * (float)(2 * k), sl * (float)(2 * k + 1));
+                    [[maybe_unused]] const float most = p.score.near_limit * p.score.near_limit;
+                    [[maybe_unused]] const uint64_t turn2 = both(p.score.cap_in * 2.8853900817779268f), fall2 = both(-2.f * p.score.cap_out),
+                                                    one2 = both(1.f), out2 = both(p.score.cap_out);
+#pragma unroll
+                    for (int i = 0; i < kCols; i += 2) {
+                        const uint64_t s2 = pack_f2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+                        uint64_t off = nm2, x2;
+                        if constexpr (kBias && kKind != 1) {
+                            if (i % 8 == 0) block = both(fmaf(sl, (float)i, from - m_sub));
+                            off = add2(ramp[(i >> 1) & 3], block);
+                        }
+                        if constexpr (kKind == 0) {
+                            x2 = fma2(s2, sc2, off);
+                        } else if constexpr (kKind == 1) {
+                            x2 = add2(s2, off);
+                        } else if constexpr (kKind == 2) {
+                            uint64_t y = mul2(s2, s2);
+                            if constexpr (kEdge) {                          // -inf: a finite positive q, and -inf again times it
+                                float y0, y1;
+                                unpack_f2(y, y0, y1);
+                                y = pack_f2(fminf(y0, most), fminf(y1, most));
+                            }
+                            x2 = fma2(s2, cap_near_q(y, p.score), off);
+                        } else {
+                            // c - 2 c / (exp(2x) + 1); the bound keeps exp(2x) finite
+                            float w0, w1;
+                            unpack_f2(mul2(s2, turn2), w0, w1);
+                            unpack_f2(add2(pack_f2(exp2_approx(w0 > 64.f ? 64.f : w0), exp2_approx(w1 > 64.f ? 64.f : w1)), one2), w0, w1);
+                            x2 = fma2(pack_f2(rcp_approx(w0), rcp_approx(w1)), fall2, add2(off, out2));
+                            if constexpr (kEdge) {                          // hidden: -inf stays -inf
+                                float x0, x1;
+                                unpack_f2(x2, x0, x1);
+                                x2 = pack_f2(s[i] == 0xff800000u ? -INFINITY : x0, s[i + 1] == 0xff800000u ? -INFINITY : x1);
+                            }
+                        }
+                        float x0, x1;
+                        unpack_f2(x2, x0, x1);
+                        const float e0 = exp2_approx(x0), e1 = exp2_approx(x1);
+                        rs2[(i >> 1) & 1] = add2(rs2[(i >> 1) & 1], pack_f2(e0, e1));
+                        s[i >> 1] = pack_bf16x2(e0, e1);
+                    }
+                };
+                using No = std::false_type;
+                using Yes = std::true_type;
+                // (the previous P_t V has read P_t before this step's replaces it)
+                if constexpr (!kShaped) {
+                    exp_row(std::integral_constant<int, 0>{}, No{}, 0.f);
+                    if (it_cnt > 0) { MF_WAIT(&sh.pv_done[t], (it_cnt - 1) & 1, 14 + t, j); tc_fence_after(); }
+                    tmem_st_x32(P_t + 0, *reinterpret_cast<const uint32_t(*)[32]>(&s[0]));
+                    tmem_st_x32(P_t + 32, *reinterpret_cast<const uint32_t(*)[32]>(&s[32]));
+                } else {
+                    if (it_cnt > 0) { MF_WAIT(&sh.pv_done[t], (it_cnt - 1) & 1, 14 + t, j); tc_fence_after(); }
+                    // Two passes of one copy of the loop over half of the row each: unrolled over the whole row the loop does not fit
+                    // the instruction cache beside the other warps' (12 times the misses, and a third of the time)
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        [[maybe_unused]] const float from = fmaf(sl, (float)(half * (kTile / 2)), base);
+                        if constexpr (kCap) {
+                            if (__builtin_expect(slow, 0)) exp_row(std::integral_constant<int, 1>{}, No{}, 0.f);
+                            else if (__builtin_expect(far, 0)) exp_row(std::integral_constant<int, 3>{}, Yes{}, from);
+                            else if (__builtin_expect(edge, 0)) exp_row(std::integral_constant<int, 2>{}, Yes{}, from);
+                            else exp_row(std::integral_constant<int, 2>{}, No{}, from);
+                        } else {
+                            if (__builtin_expect(slow, 0)) exp_row(std::integral_constant<int, 1>{}, No{}, 0.f);
+                            else exp_row(std::integral_constant<int, 0>{}, No{}, from);
+                        }
+                        tmem_st_x32(P_t + 32 * half, *reinterpret_cast<const uint32_t(*)[32]>(&s[0]));
+#pragma unroll
+                        for (int i = 0; i < kTile / 2; ++i) s[i] = s[kTile / 2 + i];
+                    }
                 }
                 float ra, rb;
                 unpack_f2(add2(rs2[0], rs2[1]), ra, rb);
                 l_run = l_run * alpha + (ra + rb);
-                // the previous P_t V has read P_t before this step's replaces it
-                if (it_cnt > 0) { MF_WAIT(&sh.pv_done[t], (it_cnt - 1) & 1, 14 + t, j); tc_fence_after(); }
-                tmem_st_x32(P_t + 0, *reinterpret_cast<const uint32_t(*)[32]>(&s[0]));
-                tmem_st_x32(P_t + 32, *reinterpret_cast<const uint32_t(*)[32]>(&s[32]));
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -275,7 +380,7 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.l_full[t][ep_cnt & 1]);
             ++ep_cnt;
-            if (lse_at) *lse_at = m_ref == -INFINITY ? -INFINITY : m_ref * 0.6931471805599453f + logf(l_run);
+            if (lse_at) *lse_at = l_run == 0.f ? -INFINITY : m_ref * 0.6931471805599453f + logf(l_run);
         }
     } else if (warp < 12) {
         // =============================================================== correction + epilogue
@@ -508,7 +613,7 @@ int mf_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
     prm.total = (int)total;
     prm.Dg = pl->D;
     prm.causal = pl->causal; prm.has_lse = lse != nullptr;
-    prm.scale_log2 = scale * 1.4426950408889634f;
+    prm.scale_log2 = fmaxf(scale * 1.4426950408889634f, 1e-30f);      // (0 times a hidden score would be NaN)
     prm.status = basp_status_device_ptr();
     if (!prm.status) return BASP_ERR_CUDA;
     prm.div_items = make_fastdiv((uint32_t)pl->Hq);

@@ -260,6 +260,13 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[
         ::BASP_R4(r, 0), BASP_R4(r, 4), BASP_R4(r, 8), BASP_R4(r, 12), "r"(taddr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7};"
+        ::BASP_R4(r, 0), BASP_R4(r, 4), "r"(taddr)
+        : "memory");
+}
 #undef BASP_R4
 
 // Register budget of the calling warpgroup (all four warps must execute it).
