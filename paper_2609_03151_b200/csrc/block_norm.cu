@@ -26,8 +26,8 @@ using namespace ptx;
 
 constexpr int kMaxHidden = 16384;
 constexpr int kMaxStages = 4;
+constexpr int kMaxWarps = 16;
 constexpr int kWarpRows = 8;               // groups of a block where a warp holds a row
-constexpr int kFwdThreads = 768, kBwdThreads = 512;      // resident per SM
 constexpr int kRingBytes = 192 * 1024;     // of all blocks of an SM, weights included
 
 // R: room for ranks (8 or BASP_MAX_RANKS; a launch takes longer the larger its parameters)
@@ -88,7 +88,8 @@ __device__ __forceinline__ float warp_sum(float v) {
 // What a block keeps in shared memory besides the ring and the weights.
 struct NormShared {
     uint64_t full[kWarpRows][kMaxStages];
-    float red[4][3][32];                   // sums of the warps, in turn
+    __nv_bfloat16 *to[kWarpRows][kMaxStages][2];  // where the row of a stage goes; nullptr: there is no such row
+    alignas(16) float red[4][3][kMaxWarps];       // sums of the warps, in turn
     int abort_flag;
 };
 
@@ -98,26 +99,48 @@ __device__ __forceinline__ bool group_sync(bool broken) {
     if constexpr (kWarp) return __any_sync(0xffffffffu, broken);
     else return __syncthreads_or(broken);
 }
-// Sums over the group of n values per thread, in all of its threads.  kWarp: the group is a warp.
-template <bool kWarp, int n>
-__device__ __forceinline__ bool group_sum(float (&v)[n], float (*red)[32], bool broken = false) {
+// Sums over the warp of three values per thread, the k-th one in the lanes with lane % 4 == k: two steps halve what a lane carries, three
+// more go over the lanes that carry the same.
+__device__ __forceinline__ float warp_sum3(float a, float b, float c) {
+    const int lane = threadIdx.x & 31;
+    const bool odd = lane & 1, upper = lane & 2;
+    // lanes with bit 0 keep b (and nothing), the others a and c
+    const float keep = (odd ? b : a) + __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+    const float other = (odd ? 0.f : c) + __shfl_xor_sync(0xffffffffu, odd ? c : 0.f, 1);
+    float v = (upper ? other : keep) + __shfl_xor_sync(0xffffffffu, upper ? keep : other, 2);
 #pragma unroll
-    for (int i = 0; i < n; ++i) v[i] = warp_sum(v[i]);
+    for (int o = 4; o <= 16; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// Sums over the group of n (1 or 3) values per thread, in all of its threads.  kWarp: the group is a warp.
+template <bool kWarp, int n>
+__device__ __forceinline__ bool group_sum(float (&v)[n], float (*red)[kMaxWarps], bool broken = false) {
+    float mine;
+    if constexpr (n == 3) mine = warp_sum3(v[0], v[1], v[2]);
+    else mine = warp_sum(v[0]);
     if constexpr (kWarp) {
+        if constexpr (n == 3)
+#pragma unroll
+            for (int i = 0; i < n; ++i) v[i] = __shfl_sync(0xffffffffu, mine, i);
+        else v[0] = mine;
         __syncwarp();
         return group_sync<true>(broken);
     } else {
-        const int warp = threadIdx.x / 32, warps = blockDim.x / 32;
-        if (threadIdx.x % 32 == 0)
-#pragma unroll
-            for (int i = 0; i < n; ++i) red[i][warp] = v[i];
+        const int warp = threadIdx.x / 32, warps = blockDim.x / 32, lane = threadIdx.x % 32;
+        if (lane < n) red[lane][warp] = mine;
         broken = group_sync<false>(broken);
+        // (the places of warps that are not there hold zeros)
+        uint64_t s[n];
 #pragma unroll
-        for (int i = 0; i < n; ++i) {
-            float s = 0.f;
-            for (int k = 0; k < warps; ++k) s += red[i][k];
-            v[i] = s;
-        }
+        for (int i = 0; i < n; ++i) s[i] = 0;
+        for (int k = 0; k < warps; k += 4)
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const ulonglong2 f = *reinterpret_cast<const ulonglong2 *>(&red[i][k]);
+                s[i] = add2(s[i], add2(f.x, f.y));
+            }
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = sum2(s[i]);
         return broken;
     }
 }
@@ -133,13 +156,14 @@ __device__ __forceinline__ bool place_of(const NormParams<R> &p, uint32_t i, uin
 
 // kBwd: which pass; kWarp: a warp holds a row; V: vectors of eight features per thread
 template <bool kBwd, bool kWarp, int V, int R>
-__global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) block_norm_kernel(const __grid_constant__ NormParams<R> p) {
+__global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp || (!kBwd && V < 4) ? 2 : 1) block_norm_kernel(const __grid_constant__ NormParams<R> p) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ NormShared sh;
     const int warp = threadIdx.x / 32, group = kWarp ? warp : 0, groups = kWarp ? kWarpRows : 1;
     const int lanes = kWarp ? 32 : (int)blockDim.x, lane = kWarp ? (int)threadIdx.x % 32 : (int)threadIdx.x;
     const uint32_t row_bytes = (uint32_t)p.hidden * 2;
     uint8_t *weights = smem, *ring = smem + 3 * row_bytes + (size_t)group * p.stages * p.n_in * row_bytes;
+    for (int i = threadIdx.x; i < 4 * 3 * kMaxWarps; i += blockDim.x) (&sh.red[0][0][0])[i] = 0.f;
     if (threadIdx.x == 0) {
         sh.abort_flag = 0;
         for (int g = 0; g < groups; ++g)
@@ -158,7 +182,15 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
     auto ask = [&](uint32_t i, int s) {
         uint32_t r;
         size_t off;
-        if (i >= p.rows || !place_of(p, i, r, off)) return;
+        if (i >= p.rows) return;
+        const bool there = place_of(p, i, r, off);
+        // (forward without a block before: no sum is written, and the place only says that the row is there)
+        sh.to[group][s][0] = there ? (p.out[0][r] ? p.out[0][r] : p.out[1][r]) + off : nullptr;
+        sh.to[group][s][1] = there && p.out[1][r] ? p.out[1][r] + off : nullptr;
+        if (!there) {                              // a short last rank: nothing comes
+            mbar_arrive(&sh.full[group][s]);
+            return;
+        }
         mbar_arrive_expect_tx(&sh.full[group][s], p.n_in * row_bytes);
         uint8_t *to = ring + (size_t)s * p.n_in * row_bytes;
 #pragma unroll
@@ -172,14 +204,14 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
         for (int s = 0; s < p.stages; ++s) ask(first + s * step, s);
 
     const bool post = p.w[0], gated = p.w[1], pre = p.w[2];
-    float acc[kBwd ? 3 : 1][kBwd ? V : 1][8];
+    uint64_t acc[kBwd ? 3 : 1][kBwd ? V : 1][4];     // pairs of the three weight sums
     if constexpr (kBwd)
 #pragma unroll
         for (int k = 0; k < 3; ++k)
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[k][v][e] = 0.f;
+                for (int e = 0; e < 4; ++e) acc[k][v][e] = 0;
     const auto weight = [&](int k, int v) { return widen(reinterpret_cast<const uint4 *>(weights + k * row_bytes)[lane + v * lanes]); };
     const uint64_t scale2 = both(p.scale);
 
@@ -187,20 +219,14 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
     uint32_t phases = 0, turn = 0;                 // a bit for each stage
     bool broken = false;
     for (uint32_t i = first; i < p.rows; i += step, ++turn) {
-        uint32_t r;
-        size_t off;
         const int at = stage;
         stage = stage + 1 == p.stages ? 0 : stage + 1;
-        const bool there = place_of(p, i, r, off);
-        if (!there) {                              // a short last rank: its stage is free at once
-            if (lane == 0) ask(i + p.stages * step, at);
-            continue;
-        }
         if (!mbar_wait(&sh.full[group][at], (phases >> at) & 1, &sh.abort_flag)) {
             if (atomicCAS(p.status, 0, 6) == 0) { p.status[1] = 1; p.status[2] = (int)blockIdx.x; p.status[3] = (int)i; }
             sh.abort_flag = 1;
             broken = true;                         // the group leaves together, at its next meeting and before it stores anything
         }
+        __nv_bfloat16 *const out0 = sh.to[group][at][0], *const out1 = sh.to[group][at][1];
         phases ^= 1u << at;
         uint4 raw[kBwd ? 4 : 2][V];
         {
@@ -215,7 +241,7 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
                 if (p.has[k]) from += row_bytes;
             }
         }
-        float (*red)[3][32] = sh.red + 2 * (turn & 1);
+        float (*red)[3][kMaxWarps] = sh.red + 2 * (turn & 1);
         if constexpr (!kBwd) {
             float ry = 1.f, sums[1];
             if (post) {
@@ -235,6 +261,7 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
             }
             if (broken) break;
             if (lane == 0) ask(i + p.stages * step, at);       // everyone has its part of the row
+            if (!out0) continue;
             const uint64_t ry2 = both(ry);
             uint64_t sq = 0;
             F8 h[V];
@@ -246,7 +273,7 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
                     const F8 y = widen(raw[1][v]), wp = post ? weight(0, v) : ones(), g = gated ? weight(1, v) : ones();
 #pragma unroll
                     for (int e = 0; e < 4; ++e) h[v].p[e] = fma2(mul2(g.p[e], scale2), mul2(mul2(y.p[e], ry2), wp.p[e]), h[v].p[e]);
-                    st16(p.out[0][r] + off + (size_t)(lane + v * lanes) * 8, narrow(h[v]));
+                    st16(out0 + (lane + v * lanes) * 8, narrow(h[v]));
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sq = fma2(h[v].p[e], h[v].p[e], sq);
@@ -262,7 +289,7 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
                         F8 n;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) n.p[e] = mul2(mul2(h[v].p[e], rh2), w.p[e]);
-                        st16(p.out[1][r] + off + (size_t)(lane + v * lanes) * 8, narrow(n));
+                        st16(out1 + (lane + v * lanes) * 8, narrow(n));
                     }
             }
         } else {
@@ -270,10 +297,11 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
             uint64_t s0 = 0, s1 = 0, s2 = 0;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
+                if ((lane + v * lanes) * 8 >= p.hidden) continue;
                 const F8 y = widen(raw[1][v]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s0 = fma2(y.p[e], y.p[e], s0);
-                if (pre && (lane + v * lanes) * 8 < p.hidden) {
+                if (pre) {
                     const F8 h = widen(raw[0][v]), dn = widen(raw[3][v]), w = weight(2, v);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -286,6 +314,7 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
             broken = group_sum<kWarp>(sums, red[0], broken);
             if (broken) break;
             if (lane == 0) ask(i + p.stages * step, at);       // everyone has its part of the row
+            if (!out0) continue;
             const float ry = post ? rsqrtf(fmaf(sums[0], p.inv, p.eps)) : 1.f, rh = rsqrtf(fmaf(sums[1], p.inv, p.eps));
             // in this order: r^3 alone leaves fp32 for zeros and a tiny eps
             const uint64_t rh2 = both(rh), ch2 = both(-(rh * sums[2] * p.inv) * rh * rh), ry2 = both(ry);
@@ -300,31 +329,23 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const uint64_t t = mul2(dn.p[e], rh2);
-                        float lo, hi;
-                        unpack_f2(mul2(t, h.p[e]), lo, hi);
-                        acc[2][v][2 * e] += lo;
-                        acc[2][v][2 * e + 1] += hi;
+                        acc[2][v][e] = fma2(t, h.p[e], acc[2][v][e]);
                         dh.p[e] = add2(dh.p[e], fma2(t, w.p[e], mul2(h.p[e], ch2)));
                     }
                 }
-                st16(p.out[0][r] + off + (size_t)(lane + v * lanes) * 8, narrow(dh));
-                if (!p.out[1][r]) continue;
+                st16(out0 + (lane + v * lanes) * 8, narrow(dh));
+                if (!out1) continue;
                 const F8 y = widen(raw[1][v]), wp = post ? weight(0, v) : ones(), g = gated ? weight(1, v) : ones();
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const uint64_t u = mul2(dh.p[e], scale2), yr = mul2(y.p[e], ry2);
-                    float lo, hi;
-                    unpack_f2(mul2(u, mul2(yr, wp.p[e])), lo, hi);
-                    acc[1][v][2 * e] += lo;
-                    acc[1][v][2 * e + 1] += hi;
+                    acc[1][v][e] = fma2(u, mul2(yr, wp.p[e]), acc[1][v][e]);
                     const uint64_t d = mul2(u, g.p[e]);
-                    unpack_f2(mul2(d, yr), lo, hi);
-                    acc[0][v][2 * e] += lo;
-                    acc[0][v][2 * e + 1] += hi;
+                    acc[0][v][e] = fma2(d, yr, acc[0][v][e]);
                     dz[v].p[e] = mul2(d, wp.p[e]);
                     s3 = fma2(dz[v].p[e], y.p[e], s3);
                 }
-                if (!post) st16(p.out[1][r] + off + (size_t)(lane + v * lanes) * 8, narrow(dz[v]));
+                if (!post) st16(out1 + (lane + v * lanes) * 8, narrow(dz[v]));
             }
             if (post) {
                 float dot[1] = {sum2(s3)};
@@ -337,7 +358,7 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
                         F8 dy;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) dy.p[e] = fma2(dz[v].p[e], ry2, mul2(y.p[e], cy2));
-                        st16(p.out[1][r] + off + (size_t)(lane + v * lanes) * 8, narrow(dy));
+                        st16(out1 + (lane + v * lanes) * 8, narrow(dy));
                     }
             }
         }
@@ -359,9 +380,9 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
 #pragma unroll
                             for (int k = 0; k < 3; ++k)
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    float *f = sum + k * p.hidden + (lane + v * lanes) * 8 + e;
-                                    *f = g == 0 ? acc[k][v][e] : *f + acc[k][v][e];
+                                for (int e = 0; e < 4; ++e) {
+                                    uint64_t *f = reinterpret_cast<uint64_t *>(sum + k * p.hidden + (lane + v * lanes) * 8 + 2 * e);
+                                    *f = g == 0 ? acc[k][v][e] : add2(*f, acc[k][v][e]);
                                 }
             }
             __syncthreads();
@@ -372,9 +393,9 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp ? 2 : 1) b
                 if ((lane + v * lanes) * 8 < p.hidden)
 #pragma unroll
                     for (int k = 0; k < 3; ++k) {
-                        float4 *f = reinterpret_cast<float4 *>(to + (size_t)k * p.hidden + (lane + v * lanes) * 8);
-                        f[0] = make_float4(acc[k][v][0], acc[k][v][1], acc[k][v][2], acc[k][v][3]);
-                        f[1] = make_float4(acc[k][v][4], acc[k][v][5], acc[k][v][6], acc[k][v][7]);
+                        ulonglong2 *f = reinterpret_cast<ulonglong2 *>(to + (size_t)k * p.hidden + (lane + v * lanes) * 8);
+                        f[0] = make_ulonglong2(acc[k][v][0], acc[k][v][1]);
+                        f[1] = make_ulonglong2(acc[k][v][2], acc[k][v][3]);
                     }
         }
     }
@@ -402,14 +423,18 @@ struct NormShape {
     int vectors, threads, stages, wave;            // per thread, per block, of the ring, blocks of a full GPU
     size_t smem;
 };
-// One warp a row up to 512 features; above that two vectors a thread, four above 8192 features (512 threads).
+// One warp a row up to 512 features, one vector a lane up to 256.  Above that a block: what a row costs beside its features (its place, its
+// sums over the block) is paid by every warp, so two vectors a thread (four above 8192 features: 512 threads), but forward, where
+// a block of two warps would be the measure, one up to 2048 (64K rows of 1024 / 2048 / 4096 forward: one vector 100 / 191 / 395 us,
+// two 112 / 202 / 372).  Blocks per SM by the registers, 128 and 64 a thread.
 NormShape shape_of(int hidden, int n_in, bool bwd) {
     NormShape s;
     const int nv = hidden / 8;
     const bool warp = nv <= 64;
-    s.vectors = warp || nv <= 1024 ? 2 : 4;
+    s.vectors = warp ? (nv <= 32 ? 1 : 2) : !bwd && nv <= 256 ? 1 : nv <= 1024 ? 2 : 4;
     s.threads = warp ? 32 * kWarpRows : 32 * ((nv + 32 * s.vectors - 1) / (32 * s.vectors));
-    int per_sm = (bwd ? kBwdThreads : kFwdThreads) / s.threads;
+    const int resident = bwd || s.vectors == 4 ? 512 : !warp ? 1024 : s.vectors == 1 ? 1024 : 768;      // threads of an SM
+    int per_sm = resident / s.threads;
     if (per_sm < 1) per_sm = 1;
     const size_t row = (size_t)hidden * 2, stage = row * (n_in < 1 ? 1 : n_in) * (warp ? kWarpRows : 1);
     while (per_sm > 1 && kRingBytes / per_sm < (long long)(3 * row + 2 * stage)) --per_sm;
@@ -451,7 +476,9 @@ int launch(const basp_plan *pl, NormParams<R> &prm, int hidden, cudaStream_t st,
         basp_count_launch(1);
         return BASP_OK;
     };
-    if (warp) return go(block_norm_kernel<kBwd, true, 2, R>);
+    if (warp) return s.vectors == 1 ? go(block_norm_kernel<kBwd, true, 1, R>) : go(block_norm_kernel<kBwd, true, 2, R>);
+    if constexpr (!kBwd)
+        if (s.vectors == 1) return go(block_norm_kernel<false, false, 1, R>);
     return s.vectors == 2 ? go(block_norm_kernel<kBwd, false, 2, R>) : go(block_norm_kernel<kBwd, false, 4, R>);
 }
 

@@ -7,9 +7,11 @@
 // the angle comes out to 2^-32 of a turn at any position, where fp32 (2^-24 of the angle) is 0.01 radian off at 128K.  So a lane makes
 // its eight angles from the position alone (an integer product and a sine and a cosine each) and no table is read.
 //
-// HBM-bound: 2 bytes read and 2 written per element.  A lane holds two vectors of 16 bytes: those of eight pairs (their two halves,
-// or sixteen neighbouring features), or sixteen features that are only copied; D / 16 lanes hold a head, a warp 32 / (D / 16) heads
-// of one token, Q's and K's in one list, so the angles are made once for a token's share of heads.
+// HBM-bound: 2 bytes read and 2 written per element.  A lane holds two vectors of 16 bytes, D / 16 lanes a head: in the half layout the two
+// halves of eight pairs or two vectors that are only copied, interleaved one of each half of the head.  Neighbouring lanes have
+// neighbouring vectors, so every access is of whole sectors (a lane with sixteen neighbouring features reads each twice: 64K tokens
+// interleaved 234 us, against 205).  A warp holds 32 / (D / 16) heads of one token, Q's and K's in one list, so the angles are made once for a
+// token's share of heads.  80 registers, three blocks per SM: 64K tokens, 40 heads of 128: 206 us (6.5 TB/s); at 96 registers and two blocks 228 us.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -52,32 +54,34 @@ __device__ __forceinline__ void st16(__nv_bfloat16 *p, const uint4 &v) {
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// The eight rotated pairs of a lane's two vectors
-__device__ __forceinline__ void turn(uint4 &a, uint4 &b, const float (&c)[8], const float (&s)[8], bool interleaved) {
+// Eight pairs whose halves are in two vectors
+__device__ __forceinline__ void turn_halves(uint4 &a, uint4 &b, const float (&c)[8], const float (&s)[8]) {
     uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
-    if (interleaved) {                 // a word is a pair
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float u = low(x[i]), v = high(x[i]), w = low(y[i]), z = high(y[i]);
-            x[i] = pack_bf16x2(fmaf(u, c[i], -(v * s[i])), fmaf(v, c[i], u * s[i]));
-            y[i] = pack_bf16x2(fmaf(w, c[4 + i], -(z * s[4 + i])), fmaf(z, c[4 + i], w * s[4 + i]));
-        }
-    } else {                           // a's features pair with b's
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float u0 = low(x[i]), u1 = high(x[i]), v0 = low(y[i]), v1 = high(y[i]);
-            const int e = 2 * i;
-            x[i] = pack_bf16x2(fmaf(u0, c[e], -(v0 * s[e])), fmaf(u1, c[e + 1], -(v1 * s[e + 1])));
-            y[i] = pack_bf16x2(fmaf(v0, c[e], u0 * s[e]), fmaf(v1, c[e + 1], u1 * s[e + 1]));
-        }
+    for (int i = 0; i < 4; ++i) {
+        const float u0 = low(x[i]), u1 = high(x[i]), v0 = low(y[i]), v1 = high(y[i]);
+        const int e = 2 * i;
+        x[i] = pack_bf16x2(fmaf(u0, c[e], -(v0 * s[e])), fmaf(u1, c[e + 1], -(v1 * s[e + 1])));
+        y[i] = pack_bf16x2(fmaf(v0, c[e], u0 * s[e]), fmaf(v1, c[e + 1], u1 * s[e + 1]));
     }
     a = make_uint4(x[0], x[1], x[2], x[3]);
     b = make_uint4(y[0], y[1], y[2], y[3]);
 }
+// Four pairs side by side; their angles start at `first`
+template <int first>
+__device__ __forceinline__ void turn_pairs(uint4 &a, const float (&c)[8], const float (&s)[8]) {
+    uint32_t x[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float u = low(x[i]), v = high(x[i]);
+        x[i] = pack_bf16x2(fmaf(u, c[first + i], -(v * s[first + i])), fmaf(v, c[first + i], u * s[first + i]));
+    }
+    a = make_uint4(x[0], x[1], x[2], x[3]);
+}
 
 // N = D / 16 lanes hold a head
 template <int N, int R>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams<R> p) {
+__global__ void __launch_bounds__(kThreads, 3) rope_kernel(const __grid_constant__ RopeParams<R> p) {
     constexpr int kHeads = 32 / N;     // heads of a warp's step
     const int warp_lane = threadIdx.x & 31, slot = warp_lane / N, lane = warp_lane - slot * N;
     const uint32_t item = blockIdx.x * kWarps + threadIdx.x / 32;
@@ -89,10 +93,15 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
     const uint32_t Tr = last ? p.T_last : p.T;
     if (row >= p.Bl * Tr) return;      // a short last rank
     const uint32_t bl = fdiv(row, last ? p.div_T_last : p.div_T), place = l * p.T + (row - bl * Tr);
-    // the lane's two vectors: of a rotated lane its pairs' halves, or sixteen features side by side
-    const bool rotated = 16 * lane < p.rotary;
-    const bool split = rotated && !p.interleaved;
-    const int at = split ? 8 * lane : 16 * lane, other = split ? at + p.half : at + 8;
+    // the lane's two vectors, and which of them are rotated
+    const int turned = p.rotary / 16;                          // half layout: lanes with pairs
+    int at = 8 * lane, other = at + 8 * N;
+    bool turn_a = at < p.rotary, turn_b = other < p.rotary;    // interleaved
+    if (!p.interleaved) {
+        turn_a = turn_b = lane < turned;
+        if (!turn_a) at = p.rotary + 8 * (lane - turned);
+        other = at + (turn_a ? p.half : 8 * (N - turned));
+    }
     const int first = (int)(chunk * p.chunk_heads), past = min(first + (int)p.chunk_heads, p.H);
     const __nv_bfloat16 *q = p.q[r] + (size_t)row * p.Hq * p.D, *k = p.k[r] + (size_t)row * (p.H - p.Hq) * p.D;
     __nv_bfloat16 *qo = p.q_out[r] + (size_t)row * p.Hq * p.D, *ko = p.k_out[r] + (size_t)row * (p.H - p.Hq) * p.D;
@@ -108,12 +117,13 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
                 b[u] = ld16(x + other);
             }
         }
-        if (h0 == first + slot && rotated) {                   // behind the first loads: their latencies overlap
+        if (h0 == first + slot && (turn_a || turn_b)) {        // behind the first loads: their latencies overlap
             const long long pos = p.positions ? (long long)__ldg(p.positions + (size_t)(g * p.Bl + bl) * p.S + place) : (long long)place;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 // the fraction of a turn as a signed 32-bit number, halves of a turn as sincospi takes them
-                const unsigned long long t = (unsigned long long)pos * p.turns[8 * lane + e];
+                const int pair = p.interleaved ? (e < 4 ? 4 * lane + e : 4 * (lane + N) + e - 4) : 8 * lane + e;      // (below D / 2)
+                const unsigned long long t = (unsigned long long)pos * p.turns[pair];
                 float sn, cs;
                 sincospif((float)(int)(t >> 32) * 4.656612873077393e-10f, &sn, &cs);
                 c[e] = cs * p.factor;
@@ -124,7 +134,12 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
         for (int u = 0; u < kUnroll; ++u) {
             const int h = h0 + u * kHeads;
             if (h < past) {
-                if (rotated) turn(a[u], b[u], c, s, p.interleaved);
+                if (!p.interleaved) {
+                    if (turn_a) turn_halves(a[u], b[u], c, s);
+                } else {
+                    if (turn_a) turn_pairs<0>(a[u], c, s);
+                    if (turn_b) turn_pairs<4>(b[u], c, s);
+                }
                 __nv_bfloat16 *y = h < p.Hq ? qo + (size_t)h * p.D : ko + (size_t)(h - p.Hq) * p.D;
                 st16(y + at, a[u]);
                 st16(y + other, b[u]);
