@@ -472,7 +472,8 @@ int basp_attn_masked_bwd(const basp_plan *plan, const basp_score *score, const v
                          void *workspace, size_t workspace_bytes, float softmax_scale, void *stream);
 size_t basp_attn_masked_bwd_workspace_bytes(const basp_plan *plan);
 /* The whole layer with such scores, on sequence-sharded shards: basp_layer_fwd and basp_layer_bwd with the attention above in
- * their middle (same workspaces; after the forward basp_layer_workspace_shards has what the backward takes). */
+ * their middle.  The forward's workspace is that of basp_layer_fwd (afterwards basp_layer_workspace_shards has what the backward
+ * takes), the backward's has a size of its own. */
 int basp_layer_masked_fwd(const basp_plan *plan, const basp_score *score, const void *const *q_seq, const void *const *k_seq,
                           const void *const *v_seq, void *const *o_seq, float *const *lse_shards, void *workspace,
                           size_t workspace_bytes, float softmax_scale, void *stream);
@@ -480,6 +481,7 @@ int basp_layer_masked_bwd(const basp_plan *plan, const basp_score *score, const 
                           const void *const *v_head, const void *const *o_head, const float *const *lse_shards,
                           const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq, void *workspace,
                           size_t workspace_bytes, float softmax_scale, void *stream);
+size_t basp_layer_masked_bwd_workspace_bytes(const basp_plan *plan);
 
 /* ---- rotary positions of any token order: Q and K of every rank rotated by the token's own position, which restarts in packed
  * documents, goes on behind a cache, or is that in the sequence.  With theta_j the frequency of pair j and a = position theta_j:

@@ -92,7 +92,8 @@ class _BaspAttention(torch.autograd.Function):
                                        grads[2 * n:], ws2, softmax_scale=ctx.softmax_scale)
             return (None, None, None, None, None, None, *grads)
         qh, kh, vh, oh = (binding.as_shards(a) for a in binding.basp_layer_workspace_shards(plan, ctx.ws))
-        ws2 = torch.empty(binding.basp_layer_bwd_workspace_bytes(plan), dtype=torch.uint8, device=dev)
+        size = binding.basp_layer_bwd_workspace_bytes if ctx.score is None else binding.basp_layer_masked_bwd_workspace_bytes
+        ws2 = torch.empty(size(plan), dtype=torch.uint8, device=dev)
         if ctx.score is not None:
             with torch.cuda.device(dev):
                 binding.basp_layer_masked_bwd(plan, ctx.score, qh, kh, vh, oh, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:],

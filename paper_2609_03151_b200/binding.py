@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import POINTER, Structure, byref, c_char_p, c_float, c_int, c_longlong, c_size_t, c_void_p
 
 import torch
@@ -40,7 +41,7 @@ EXPORTS = [
     "basp_ckpt_bytes", "basp_ckpt_pack", "basp_ckpt_reshard_s2h", "basp_layer_bwd_ckpt",
     "basp_lm_loss_fwd", "basp_lm_loss_fwd_workspace_bytes", "basp_lm_loss_grad", "basp_lm_loss_grad_workspace_bytes",
     "basp_mask_bytes", "basp_mask_ranges", "basp_mask_packed", "basp_attn_masked_fwd", "basp_attn_masked_bwd",
-    "basp_attn_masked_bwd_workspace_bytes", "basp_layer_masked_fwd", "basp_layer_masked_bwd", "basp_rope_make", "basp_rope",
+    "basp_attn_masked_bwd_workspace_bytes", "basp_layer_masked_fwd", "basp_layer_masked_bwd", "basp_layer_masked_bwd_workspace_bytes", "basp_rope_make", "basp_rope",
     "basp_block_norm", "basp_block_norm_bwd", "basp_block_norm_bwd_workspace_bytes",
 ]
 
@@ -127,15 +128,16 @@ class basp_rope_turns(Structure):
 
 lib.basp_mask_ranges.argtypes = [c_void_p] * 4 + [c_size_t, c_void_p]
 lib.basp_mask_packed.argtypes = [c_void_p] * 3 + [c_int, c_void_p, c_size_t, c_void_p]
-lib.basp_attn_masked_fwd.argtypes = [c_void_p, POINTER(_Score)] + [c_void_p] * 5 + [c_float, c_void_p]
-lib.basp_attn_masked_bwd.argtypes = [c_void_p, POINTER(_Score)] + [c_void_p] * 10 + [c_size_t, c_float, c_void_p]
-lib.basp_layer_masked_fwd.argtypes = [c_void_p, POINTER(_Score)] + [c_void_p] * 6 + [c_size_t, c_float, c_void_p]
-lib.basp_layer_masked_bwd.argtypes = [c_void_p, POINTER(_Score)] + [c_void_p] * 10 + [c_size_t, c_float, c_void_p]
+lib.basp_attn_masked_fwd.argtypes = [c_void_p, c_void_p] + [c_void_p] * 5 + [c_float, c_void_p]
+lib.basp_attn_masked_bwd.argtypes = [c_void_p, c_void_p] + [c_void_p] * 10 + [c_size_t, c_float, c_void_p]
+lib.basp_layer_masked_fwd.argtypes = [c_void_p, c_void_p] + [c_void_p] * 6 + [c_size_t, c_float, c_void_p]
+lib.basp_layer_masked_bwd.argtypes = [c_void_p, c_void_p] + [c_void_p] * 10 + [c_size_t, c_float, c_void_p]
 lib.basp_rope_make.argtypes = [POINTER(basp_rope_config), POINTER(basp_rope_turns)]
 lib.basp_rope.argtypes = [c_void_p, POINTER(basp_rope_turns)] + [c_void_p] * 3 + [c_int] + [c_void_p] * 3
 lib.basp_block_norm.argtypes = [c_void_p, c_int] + [c_void_p] * 5 + [c_float, c_float] + [c_void_p] * 3
 lib.basp_block_norm_bwd.argtypes = [c_void_p, c_int] + [c_void_p] * 5 + [c_float, c_float] + [c_void_p] * 8 + [c_size_t, c_void_p]
-for _n, _a in (("basp_mask_bytes", []), ("basp_attn_masked_bwd_workspace_bytes", []), ("basp_block_norm_bwd_workspace_bytes", [c_int])):
+for _n, _a in (("basp_mask_bytes", []), ("basp_attn_masked_bwd_workspace_bytes", []), ("basp_layer_masked_bwd_workspace_bytes", []),
+               ("basp_block_norm_bwd_workspace_bytes", [c_int])):
     getattr(lib, _n).argtypes = [c_void_p] + _a
     getattr(lib, _n).restype = c_size_t
 lib.basp_strerror.argtypes = [c_int]
@@ -658,6 +660,9 @@ def basp_mask_packed(plan, positions, mask, prefix=None, window=0, stream=None):
     _check(lib.basp_mask_packed(plan.handle, *a, int(window), *m.space(mask), m.stream(stream)), "basp_mask_packed")
 
 
+_pack_score = struct.Struct("f4xPPN").pack          # the fields of _Score
+
+
 class basp_score:
     """What a score goes through and which keys are seen: softcap c (0: none), slopes of the bias by distance (fp32 [Hq] or None),
     mask (a mask object, or None for the plan's own mask).  Holds its tensors."""
@@ -665,11 +670,10 @@ class basp_score:
     def __init__(self, softcap=0.0, slopes=None, mask=None):
         self.softcap, self.slopes, self.mask = float(softcap), slopes, mask
 
-    def marshal(self, plan, m):
-        slopes = m.addresses(("slopes", _F32, self.slopes, plan.Hq))[0] if self.slopes is not None else None
-        kept = m.kept
-        mask, size = m.space(self.mask) if self.mask is not None else (None, 0)
-        return kept, byref(_Score(self.softcap, slopes, mask, size))
+    def pack(self, m, slopes):
+        """The library's structure, `slopes`: the address."""
+        mask, size = m.space(self.mask)
+        return _pack_score(self.softcap, slopes or 0, mask or 0, size)
 
 
 def _head_sizes(plan):
@@ -683,10 +687,9 @@ def _head_sizes(plan):
 def basp_attn_masked_fwd(plan, score, q_head, k_head, v_head, o_head, lse_shards=None, softmax_scale=0.0, stream=None):
     """basp_attn_fwd with capped, biased and masked scores (a basp_score); a query that sees no key has O = 0, LSE = -inf."""
     m, (q, k, rows) = _Marshal(), _head_sizes(plan)
-    kept, s = score.marshal(plan, m)
-    a = m.addresses(("q_head", _BF16, q_head, q), ("k_head", _BF16, k_head, k), ("v_head", _BF16, v_head, k),
-                    ("o_head", _BF16, o_head, q), ("lse_shards", _F32, lse_shards, rows))
-    _check(lib.basp_attn_masked_fwd(plan.handle, s, *a, softmax_scale, m.stream(stream)), "basp_attn_masked_fwd")
+    sl, *a = m.addresses(("slopes", _F32, score.slopes, plan.Hq), ("q_head", _BF16, q_head, q), ("k_head", _BF16, k_head, k),
+                        ("v_head", _BF16, v_head, k), ("o_head", _BF16, o_head, q), ("lse_shards", _F32, lse_shards, rows))
+    _check(lib.basp_attn_masked_fwd(plan.handle, score.pack(m, sl), *a, softmax_scale, m.stream(stream)), "basp_attn_masked_fwd")
 
 
 def basp_attn_masked_bwd_workspace_bytes(plan) -> int:
@@ -697,32 +700,33 @@ def basp_attn_masked_bwd(plan, score, q_head, k_head, v_head, o_head, do_head, l
                          softmax_scale=0.0, stream=None):
     """Gradients of basp_attn_masked_fwd from its O and LSE."""
     m, (q, k, rows) = _Marshal(), _head_sizes(plan)
-    kept, s = score.marshal(plan, m)
-    a = m.addresses(("q_head", _BF16, q_head, q), ("k_head", _BF16, k_head, k), ("v_head", _BF16, v_head, k),
+    sl, *a = m.addresses(("slopes", _F32, score.slopes, plan.Hq), ("q_head", _BF16, q_head, q), ("k_head", _BF16, k_head, k), ("v_head", _BF16, v_head, k),
                     ("o_head", _BF16, o_head, q), ("do_head", _BF16, do_head, q), ("lse_shards", _F32, lse_shards, rows),
                     ("dq_head", _BF16, dq_head, q), ("dk_head", _BF16, dk_head, k), ("dv_head", _BF16, dv_head, k))
-    _check(lib.basp_attn_masked_bwd(plan.handle, s, *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_attn_masked_bwd")
+    _check(lib.basp_attn_masked_bwd(plan.handle, score.pack(m, sl), *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_attn_masked_bwd")
 
 
 def basp_layer_masked_fwd(plan, score, q_seq, k_seq, v_seq, o_seq, workspace, lse_shards=None, softmax_scale=0.0, stream=None):
     """basp_layer_fwd with such scores (same workspace)."""
     m, (q, k) = _Marshal(), _qk(plan)
-    kept, s = score.marshal(plan, m)
-    a = m.addresses(("q_seq", _BF16, q_seq, q), ("k_seq", _BF16, k_seq, k), ("v_seq", _BF16, v_seq, k), ("o_seq", _BF16, o_seq, q),
+    sl, *a = m.addresses(("slopes", _F32, score.slopes, plan.Hq), ("q_seq", _BF16, q_seq, q), ("k_seq", _BF16, k_seq, k), ("v_seq", _BF16, v_seq, k), ("o_seq", _BF16, o_seq, q),
                     ("lse_shards", _F32, lse_shards, _head_sizes(plan)[2]))
-    _check(lib.basp_layer_masked_fwd(plan.handle, s, *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_layer_masked_fwd")
+    _check(lib.basp_layer_masked_fwd(plan.handle, score.pack(m, sl), *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_layer_masked_fwd")
+
+
+def basp_layer_masked_bwd_workspace_bytes(plan) -> int:
+    return int(lib.basp_layer_masked_bwd_workspace_bytes(plan.handle))
 
 
 def basp_layer_masked_bwd(plan, score, q_head, k_head, v_head, o_head, lse_shards, do_seq, dq_seq, dk_seq, dv_seq, workspace,
                           softmax_scale=0.0, stream=None):
-    """basp_layer_bwd with such scores (same workspace); q_head .. o_head as basp_layer_workspace_shards reports them."""
+    """basp_layer_bwd with such scores (workspace: basp_layer_masked_bwd_workspace_bytes); q_head .. o_head as basp_layer_workspace_shards reports them."""
     m, (q, k) = _Marshal(), _qk(plan)
     qh, kh, rows = _head_sizes(plan)
-    kept, s = score.marshal(plan, m)
-    a = m.addresses(("q_head", _BF16, q_head, qh), ("k_head", _BF16, k_head, kh), ("v_head", _BF16, v_head, kh),
+    sl, *a = m.addresses(("slopes", _F32, score.slopes, plan.Hq), ("q_head", _BF16, q_head, qh), ("k_head", _BF16, k_head, kh), ("v_head", _BF16, v_head, kh),
                     ("o_head", _BF16, o_head, qh), ("lse_shards", _F32, lse_shards, rows), ("do_seq", _BF16, do_seq, q),
                     ("dq_seq", _BF16, dq_seq, q), ("dk_seq", _BF16, dk_seq, k), ("dv_seq", _BF16, dv_seq, k))
-    _check(lib.basp_layer_masked_bwd(plan.handle, s, *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_layer_masked_bwd")
+    _check(lib.basp_layer_masked_bwd(plan.handle, score.pack(m, sl), *a, *m.space(workspace), softmax_scale, m.stream(stream)), "basp_layer_masked_bwd")
 
 
 _ROPE_SCALINGS = {"none": 0, "linear": 1, "yarn": 2, "wavelength": 3}

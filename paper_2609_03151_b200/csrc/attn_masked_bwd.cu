@@ -31,26 +31,34 @@ struct MaskedBwdParams {
     const float *lse[R];
     const float *delta[R];
     __nv_bfloat16 *dk[R], *dv[R];
+    __nv_bfloat16 *dq[R];       // written at once where a sequence is one key tile (direct)
+    float *kv_part;             // [rank][part][dK, dV][kv_elems]: where the query heads of a key head are divided
+    size_t kv_elems;
+    int parts, part_heads, direct;
     ScoreArgs score;
     int K, Bl, S, Hq_l, Hkv_l, q_per_kv, causal, n_tiles, total;      // total: work items
     int Dg;                     // head dimension in memory
     float scale, scale_log2;
     int *status;
-    FastDiv div_items, div_hkv_l, div_B, div_bl;
+    FastDiv div_items, div_parts, div_hkv_l, div_B, div_bl;
 };
 
 struct MbItem {
     int r, bl, seq, hkv, n, m0, n_qt;
+    int part;                   // which part of the key head's query heads (see mb_heads)
 };
 
-template <int R>
+// kSmall: the query heads of a key head may be divided (parts), and dQ may leave at once (direct).  A variant of its own: in one, the
+// code for both cost the large plans a tenth (16K causal tokens: 5.6 and 6.2 ms).
+template <bool kSmall, int R>
 __device__ __forceinline__ bool mb_get_item(const MaskedBwdParams<R> &p, int round, MbItem &it) {
     const int pos = (round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x;   // boustrophedon
     const int i = round * (int)gridDim.x + pos;
     if (i >= p.total) return false;
     const int e = (int)fdiv((uint32_t)i, p.div_items), head = i - e * (int)p.div_items.d;
-    const int l = (int)fdiv((uint32_t)head, p.div_hkv_l);
-    it.hkv = head - l * p.Hkv_l;
+    const int lh = kSmall ? (int)fdiv((uint32_t)head, p.div_parts) : head, l = (int)fdiv((uint32_t)lh, p.div_hkv_l);
+    it.part = kSmall ? head - lh * p.parts : 0;
+    it.hkv = lh - l * p.Hkv_l;
     if (p.score.range) {
         const int4 a = __ldg(reinterpret_cast<const int4 *>(p.score.bwd + e));
         it.seq = min(max(a.x, 0), p.score.B - 1);       // whatever the buffer holds, no tile outside the tensors
@@ -69,22 +77,65 @@ __device__ __forceinline__ bool mb_get_item(const MaskedBwdParams<R> &p, int rou
     return true;
 }
 
+// Query heads of an item, and the first of them among the rank's
+template <bool kSmall, int R>
+__device__ __forceinline__ int mb_heads(const MaskedBwdParams<R> &p, const MbItem &it) {
+    return kSmall ? min(p.part_heads, p.q_per_kv - it.part * p.part_heads) : p.q_per_kv;
+}
+template <bool kSmall, int R>
+__device__ __forceinline__ int mb_first_head(const MaskedBwdParams<R> &p, const MbItem &it) {
+    return it.hkv * p.q_per_kv + (kSmall ? it.part * p.part_heads : 0);
+}
+
 // A query's LSE in log2 units; one that sees no key gets the LSE at which every probability is zero.
 __device__ __forceinline__ float seen_lse(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
 
-// For the 128 queries of tile m, which rows [lo, hi) of key tile n they see, as lo | hi << 8, and whether that is to be looked at.
+// What the producer warp brings for a query tile besides Q and dO, four queries a lane: LSE and Delta, and which rows [lo, hi) of the key
+// tile they see.
+struct MbStats {
+    float4 lse, delta;
+    int4 tile, range[2];
+};
 template <int R>
-__device__ __forceinline__ void stage_windows(const MaskedBwdParams<R> &p, const MbItem &it, int m, int lane, uint16_t *win, int *edge) {
+__device__ __forceinline__ MbStats fetch_stats(const MaskedBwdParams<R> &p, const MbItem &it, int h, int m, int lane) {
+    MbStats s;
+    const size_t off = ((size_t)it.bl * p.Hq_l + h) * p.S + (size_t)m * kT + 4 * lane;
+    if ((p.S & 3) == 0 && (m + 1) * kT <= p.S) {
+        s.lse = *reinterpret_cast<const float4 *>(p.lse[it.r] + off);
+        s.delta = *reinterpret_cast<const float4 *>(p.delta[it.r] + off);
+    } else {                       // ragged: rows of (bl, h) are not 16-byte aligned, or the tile runs past S
+        float lv[4], dv[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in_seq = m * kT + 4 * lane + e < p.S;
+            lv[e] = in_seq ? p.lse[it.r][off + e] : 0.f;
+            dv[e] = in_seq ? p.delta[it.r][off + e] : 0.f;
+        }
+        s.lse = make_float4(lv[0], lv[1], lv[2], lv[3]);
+        s.delta = make_float4(dv[0], dv[1], dv[2], dv[3]);
+    }
+    if (p.score.range) {
+        const size_t tile = (size_t)it.seq * p.n_tiles + m;
+        s.tile = __ldg(reinterpret_cast<const int4 *>(p.score.tiles + tile));
+        const int4 *at = reinterpret_cast<const int4 *>(p.score.range + tile * kT + 4 * lane);
+        s.range[0] = __ldg(at);
+        s.range[1] = __ldg(at + 1);
+    }
+    return s;
+}
+// To shared memory: LSE in log2 units, -Delta times the scale, the windows as lo | hi << 8, and whether the windows are to be looked at.
+template <int R>
+__device__ __forceinline__ void stage_stats(const MaskedBwdParams<R> &p, const MbItem &it, int m, int lane, const MbStats &s, float *lse,
+                                            float *delta, uint16_t *win, int *edge) {
+    *reinterpret_cast<float4 *>(lse + 4 * lane) = make_float4(seen_lse(s.lse.x), seen_lse(s.lse.y), seen_lse(s.lse.z), seen_lse(s.lse.w));
+    *reinterpret_cast<float4 *>(delta + 4 * lane) = make_float4(s.delta.x * -p.scale, s.delta.y * -p.scale, s.delta.z * -p.scale, s.delta.w * -p.scale);
     const int k0 = it.n * kT;
     int lo[4], hi[4];
     bool look;
     if (p.score.range) {
-        const size_t tile = (size_t)it.seq * p.n_tiles + m;
-        const int4 t = __ldg(reinterpret_cast<const int4 *>(p.score.tiles + tile));
-        const int4 *at = reinterpret_cast<const int4 *>(p.score.range + tile * kT + 4 * lane);
-        const int4 a = __ldg(at), b = __ldg(at + 1);
-        look = it.n < t.z || it.n >= t.w || (m + 1) * kT > p.S;
-        lo[0] = a.x; hi[0] = a.y; lo[1] = a.z; hi[1] = a.w; lo[2] = b.x; hi[2] = b.y; lo[3] = b.z; hi[3] = b.w;
+        look = it.n < s.tile.z || it.n >= s.tile.w || (m + 1) * kT > p.S;
+        lo[0] = s.range[0].x; hi[0] = s.range[0].y; lo[1] = s.range[0].z; hi[1] = s.range[0].w;
+        lo[2] = s.range[1].x; hi[2] = s.range[1].y; lo[3] = s.range[1].z; hi[3] = s.range[1].w;
     } else {
         look = (p.causal && m == it.n) || (m + 1) * kT > p.S || (it.n + 1) * kT > p.S;
 #pragma unroll
@@ -103,7 +154,7 @@ __device__ __forceinline__ void stage_windows(const MaskedBwdParams<R> &p, const
 
 // Thirty-two scores of a key row (queries side by side): the probabilities as bf16 to the tensor memory at `to`, sixteen at a time, and
 // times the cap's derivative to st.
-// dist: the first query's position minus the key's; side: its sign, tile by tile; win: what stage_windows left, where it matters.
+// dist: the first query's position minus the key's; side: its sign, tile by tile; win: what stage_stats left, where it matters.
 template <bool kCap, bool kBias, bool kEdge>
 __device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t to, const float *lse, const uint16_t *win, int row,
                                              const ScoreArgs &a, float scale_log2, float slope, int dist, int side) {
@@ -187,23 +238,139 @@ __device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t to, co
     }
 }
 
-// dK and dV of a key tile that no query sees: a quarter g of the compute warps takes 32 of the 128 columns of its row
-template <int R>
-__device__ __forceinline__ void store_zeros(const MaskedBwdParams<R> &p, const MbItem &it, int g, int row) {
+// Where 32 columns from `col` on of a key row's dK (which 0) or dV (which 1) go: the result, or a part's fp32 sums
+template <bool kSmall, int R>
+__device__ __forceinline__ void store_kv(const MaskedBwdParams<R> &p, const MbItem &it, int which, int row, int col, const uint32_t (&rr)[32]) {
     const int key = it.n * kT + row;
     if (key >= p.S) return;
-    const size_t off = (((size_t)it.bl * p.S + key) * p.Hkv_l + it.hkv) * p.Dg;
-    for (int c = 32 * g; c < min(32 * g + 32, p.Dg); c += 8) {
-        *reinterpret_cast<uint4 *>(p.dk[it.r] + off + c) = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4 *>(p.dv[it.r] + off + c) = make_uint4(0, 0, 0, 0);
+    const size_t off = (((size_t)it.bl * p.S + key) * p.Hkv_l + it.hkv) * p.Dg + col;
+    if (kSmall && p.parts > 1) {
+        float *to = p.kv_part + ((size_t)(it.r * p.parts + it.part) * 2 + which) * p.kv_elems + off;
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+            if (col + i < p.Dg) *reinterpret_cast<uint4 *>(to + i) = make_uint4(rr[i], rr[i + 1], rr[i + 2], rr[i + 3]);
+        return;
     }
+    __nv_bfloat16 *to = (which ? p.dv[it.r] : p.dk[it.r]) + off;
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+        uint4 o4;
+        o4.x = pack_bf16x2(__uint_as_float(rr[i + 0]), __uint_as_float(rr[i + 1]));
+        o4.y = pack_bf16x2(__uint_as_float(rr[i + 2]), __uint_as_float(rr[i + 3]));
+        o4.z = pack_bf16x2(__uint_as_float(rr[i + 4]), __uint_as_float(rr[i + 5]));
+        o4.w = pack_bf16x2(__uint_as_float(rr[i + 6]), __uint_as_float(rr[i + 7]));
+        if (col + i < p.Dg) *reinterpret_cast<uint4 *>(to + i) = o4;
+    }
+}
+// dK and dV of a key tile that no query sees: a quarter g of the compute warps takes 32 of the 128 columns of its row.  Where a sequence is
+// one key tile its queries see nothing either, and dQ is zero.
+template <bool kSmall, int R>
+__device__ __forceinline__ void store_zeros(const MaskedBwdParams<R> &p, const MbItem &it, int g, int row) {
+    const uint32_t zeros[32] = {};
+    for (int which = 0; which < 2; ++which)
+        if (32 * g < p.Dg) store_kv<kSmall>(p, it, which, row, 32 * g, zeros);
+    if (kSmall && p.direct && row < p.S)
+        for (int h = mb_first_head<kSmall>(p, it); h < mb_first_head<kSmall>(p, it) + mb_heads<kSmall>(p, it); ++h)
+            for (int c = 32 * g; c < min(32 * g + 32, p.Dg); c += 8)
+                *reinterpret_cast<uint4 *>(p.dq[it.r] + (((size_t)it.bl * p.S + row) * p.Hq_l + h) * p.Dg + c) = make_uint4(0, 0, 0, 0);
 }
 
 #include "attn_masked_bwd_d64.cuh"
 #include "attn_masked_bwd_d128.cuh"
 
-// accumulator and Delta of every rank
-size_t mb_workspace_bytes(const basp_plan *p) { return (size_t)p->N * (bwd_acc_bytes(p) + bwd_delta_bytes(p)); }
+// In front of the products: Delta[bl][h][s] = sum_d O[bl][s][h][d] dO[bl][s][h][d] (16 lanes a row), and the dQ accumulator set to zero.
+// One launch for every rank: blockIdx.y = rank.
+template <int R>
+__global__ void __launch_bounds__(256) mb_prepare_kernel(const __grid_constant__ BwdHelperPtrs<R> hp, int S, int H, int D, long long rows, int zero) {
+    const int part = threadIdx.x % 16;
+    const long long row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
+    const bool mine = row < rows && part * 8 < D;
+    allow_next_kernel();
+    float acc = 0.f;
+    if (mine) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(hp.o[blockIdx.y] + row * D + part * 8);
+        const uint4 b = *reinterpret_cast<const uint4 *>(hp.dout[blockIdx.y] + row * D + part * 8);
+        const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            acc += __uint_as_float(av[i] << 16) * __uint_as_float(bv[i] << 16);
+            acc += __uint_as_float(av[i] & 0xffff0000u) * __uint_as_float(bv[i] & 0xffff0000u);
+        }
+        if (zero) {
+            float4 *to = reinterpret_cast<float4 *>(const_cast<float *>(hp.acc[blockIdx.y]) + row * D + part * 8);
+            to[0] = to[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) acc += __shfl_down_sync(0xffffffffu, acc, off, 16);
+    if (mine && part == 0) {
+        const long long sb = row / H, h = row - sb * H, bl = sb / S, s = sb - bl * S;
+        hp.delta[blockIdx.y][(bl * H + h) * S + s] = acc;
+    }
+}
+
+// Behind the products: dQ's accumulator to bf16 (n_q vectors of eight a rank) and the parts of dK and dV added up in order (n_kv vectors of
+// each; none where the heads are not divided).  blockIdx.y = rank.
+template <int R>
+struct FinishParams {
+    const float *acc[R];
+    __nv_bfloat16 *dq[R], *dk[R], *dv[R];
+    const float *kv_part;
+    long long n_q, n_kv;
+    int parts;
+};
+template <int R>
+__global__ void __launch_bounds__(256) mb_finish_kernel(const __grid_constant__ FinishParams<R> p) {
+    const int r = blockIdx.y;
+    long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    wait_previous_kernel();
+    float4 a, b;
+    __nv_bfloat16 *to;
+    if (i < p.n_q) {
+        const float4 *from = reinterpret_cast<const float4 *>(p.acc[r]) + 2 * i;
+        a = from[0];
+        b = from[1];
+        to = p.dq[r] + 8 * i;
+    } else {
+        i -= p.n_q;
+        const int which = i >= p.n_kv;
+        if (which) i -= p.n_kv;
+        if (i >= p.n_kv) return;
+        const float4 *from = reinterpret_cast<const float4 *>(p.kv_part) + ((long long)r * p.parts * 2 + which) * 2 * p.n_kv + 2 * i;
+        a = from[0];
+        b = from[1];
+        for (int k = 1; k < p.parts; ++k) {
+            from += 4 * p.n_kv;
+            const float4 c = from[0], d = from[1];
+            a.x += c.x; a.y += c.y; a.z += c.z; a.w += c.w;
+            b.x += d.x; b.y += d.y; b.z += d.z; b.w += d.w;
+        }
+        to = (which ? p.dv[r] : p.dk[r]) + 8 * i;
+    }
+    *reinterpret_cast<uint4 *>(to) = make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y), pack_bf16x2(b.z, b.w));
+}
+
+// Query heads of a key head that one work item takes.  All of them keep dK and dV in the tensor memory; but where the items are few, the
+// longest one (a key tile that all query tiles see) is much of the whole: they are divided until it is below 0.6 of an SM's share, and the
+// parts of dK and dV are added up behind (3001 tokens, 12/4 heads of 64, capped and biased: XX).
+int mb_part_heads(const basp_plan *p) {
+    const int q_per_kv = p->Hq_l / p->Hkv_l;
+    const double n = (p->S + kT - 1) / kT, pairs = p->causal ? n * (n + 1) / 2 : n * n;
+    const double share = pairs * p->N * p->Bl * p->Hkv_l * q_per_kv / 148.0;
+    int heads = q_per_kv;
+    while (heads > 1 && heads * n > 0.6 * share) --heads;
+    return heads;
+}
+int mb_parts(const basp_plan *p) {
+    const int heads = mb_part_heads(p), q_per_kv = p->Hq_l / p->Hkv_l;
+    return (q_per_kv + heads - 1) / heads;
+}
+size_t mb_kv_elems(const basp_plan *p) { return (size_t)p->Bl * p->S * p->Hkv_l * p->D; }
+// accumulator and Delta of every rank, and the parts of dK and dV
+size_t mb_workspace_bytes(const basp_plan *p) {
+    const int parts = mb_parts(p);
+    return (size_t)p->N * (bwd_acc_bytes(p) + bwd_delta_bytes(p) + (parts > 1 ? parts * 2 * mb_kv_elems(p) * sizeof(float) : 0));
+}
 
 template <int R>
 int mb_run(const basp_plan *pl, const basp_score *score, const void *const *q, const void *const *k, const void *const *v,
@@ -214,6 +381,7 @@ int mb_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
     const uint64_t rows = (uint64_t)pl->Bl * pl->S;
     const size_t acc_b = bwd_acc_bytes(pl), del_b = bwd_delta_bytes(pl);
     BwdHelperPtrs<R> hp;
+    FinishParams<R> fin;
     for (int r = 0; r < pl->N; ++r) {
         BASP_TRY(tmap::encode_rows_heads_d(&prm.q[r], q[r], rows, pl->Hq_l, pl->D, kT));
         BASP_TRY(tmap::encode_rows_heads_d(&prm.k[r], k[r], rows, pl->Hkv_l, pl->D, kT));
@@ -231,47 +399,66 @@ int mb_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
         hp.dout[r] = (const __nv_bfloat16 *)dout[r];
         hp.delta[r] = delta;
         hp.acc[r] = acc;
-        hp.dq[r] = (__nv_bfloat16 *)dq[r];
+        prm.dq[r] = (__nv_bfloat16 *)dq[r];
+        fin.acc[r] = acc;
+        fin.dq[r] = (__nv_bfloat16 *)dq[r];
+        fin.dk[r] = (__nv_bfloat16 *)dk[r];
+        fin.dv[r] = (__nv_bfloat16 *)dv[r];
     }
+    prm.parts = mb_parts(pl);
+    prm.part_heads = mb_part_heads(pl);
+    prm.kv_part = reinterpret_cast<float *>(ws + (size_t)pl->N * (acc_b + del_b));
+    prm.kv_elems = mb_kv_elems(pl);
+    prm.direct = pl->S <= kT;            // one key tile: nothing to add up, dQ leaves as bf16
     prm.K = pl->K; prm.Bl = pl->Bl; prm.S = pl->S; prm.Hq_l = pl->Hq_l; prm.Hkv_l = pl->Hkv_l;
     prm.q_per_kv = pl->Hq_l / pl->Hkv_l; prm.causal = pl->causal;
     prm.n_tiles = (pl->S + kT - 1) / kT;
     prm.Dg = pl->D;
-    const long long per = (long long)pl->K * pl->Hkv_l, total = (long long)pl->B * prm.n_tiles * per;
-    const long long row_threads = (long long)pl->Bl * pl->S * pl->Hq_l * 16, n8 = (long long)(acc_b / sizeof(float) / 8);
-    if (total >= (1ll << 31) - 4096 || rows >= (1ull << 31) || row_threads >= (1ll << 39)) return BASP_ERR_UNSUPPORTED;   // 31-bit items, rows, blocks
+    const long long per = (long long)pl->K * pl->Hkv_l * prm.parts, total = (long long)pl->B * prm.n_tiles * per;
+    const long long q_rows = (long long)rows * pl->Hq_l;
+    fin.n_q = prm.direct ? 0 : (long long)(acc_b / sizeof(float) / 8);
+    fin.n_kv = prm.parts > 1 ? (long long)(prm.kv_elems / 8) : 0;
+    fin.kv_part = prm.kv_part;
+    fin.parts = prm.parts;
+    const long long n_fin = fin.n_q + 2 * fin.n_kv;
+    if (total >= (1ll << 31) - 4096 || rows >= (1ull << 31) || q_rows >= (1ll << 35) || n_fin >= (1ll << 39)) return BASP_ERR_UNSUPPORTED;   // 31-bit items, rows, blocks
     prm.total = (int)total;
     prm.scale = scale;
     prm.scale_log2 = scale * 1.4426950408889634f;
     prm.status = basp_status_device_ptr();
     if (!prm.status) return BASP_ERR_CUDA;
     prm.div_items = make_fastdiv((uint32_t)per);
+    prm.div_parts = make_fastdiv((uint32_t)prm.parts);
     prm.div_hkv_l = make_fastdiv((uint32_t)pl->Hkv_l);
     prm.div_B = make_fastdiv((uint32_t)pl->B);
     prm.div_bl = make_fastdiv((uint32_t)pl->Bl);
-    int dev = 0, sms = 0;
-    BASP_CUDA_TRY(cudaGetDevice(&dev));
-    BASP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    int sms = 0;
+    BASP_TRY(sm_count(&sms));
     const int grid = (int)(total < sms ? total : sms);
 
-    BASP_CUDA_TRY(cudaMemsetAsync(ws, 0, (size_t)pl->N * acc_b, st));
-    bwd_delta_kernel<R><<<dim3((unsigned)((row_threads + 255) / 256), (unsigned)pl->N), 256, 0, st>>>(hp, pl->Bl, pl->S, pl->Hq_l, pl->D);
+    mb_prepare_kernel<R><<<dim3((unsigned)((q_rows + 15) / 16), (unsigned)pl->N), 256, 0, st>>>(hp, pl->S, pl->Hq_l, pl->D, q_rows, !prm.direct);
     BASP_CUDA_TRY(cudaGetLastError());
     BASP_TRY(dispatch_score(prm.score.cap_out > 0.f, prm.score.slopes != nullptr, [&](auto cap, auto bias) -> int {
         constexpr bool kCap = decltype(cap)::value, kBias = decltype(bias)::value;
-        const auto go = [&](auto kernel, int smem) -> int {
-            BASP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-            kernel<<<grid, kBwdThreads, smem, st>>>(prm);
-            BASP_CUDA_TRY(cudaGetLastError());
+        // tiles, row statistics, windows, edge flags, barriers
+        constexpr int smem128 = 7 * kT * 128 * 2 + 4 * kT * 4 + 2 * kT * 2 + 2 * 4 + (int)sizeof(BwdBars);
+        constexpr int smem64 = (2 + 2 * 3) * kT * 64 * 2 + 4 * 16384 + 2 * 3 * kT * 4 + 3 * kT * 2 + 4 * 4 + (int)sizeof(BwdBars);
+        const auto go = [&](auto small) -> int {
+            constexpr bool kSmall = decltype(small)::value;
+            if (pl->D > 64) {
+                BASP_TRY((allow_smem<attn_masked_bwd_d128_kernel<R, kCap, kBias, kSmall>, smem128>()));
+                BASP_CUDA_TRY(launch_early_smem(attn_masked_bwd_d128_kernel<R, kCap, kBias, kSmall>, dim3(grid), kBwdThreads, smem128, st, prm));
+            } else {
+                BASP_TRY((allow_smem<attn_masked_bwd_d64_kernel<R, kCap, kBias, kSmall>, smem64>()));
+                BASP_CUDA_TRY(launch_early_smem(attn_masked_bwd_d64_kernel<R, kCap, kBias, kSmall>, dim3(grid), kBwdThreads, smem64, st, prm));
+            }
             return BASP_OK;
         };
-        if (pl->D > 64)          // tiles, row statistics, windows, edge flags, barriers
-            return go(attn_masked_bwd_d128_kernel<R, kCap, kBias>, 7 * kT * 128 * 2 + 4 * kT * 4 + 2 * kT * 2 + 2 * 4 + (int)sizeof(BwdBars));
-        return go(attn_masked_bwd_d64_kernel<R, kCap, kBias>, (2 + 2 * 3) * kT * 64 * 2 + 4 * 16384 + 2 * 3 * kT * 4 + 3 * kT * 2 + 4 * 4 + (int)sizeof(BwdBars));
+        return prm.parts > 1 || prm.direct ? go(std::true_type{}) : go(std::false_type{});
     }));
-    bwd_dq_convert_kernel<R><<<dim3((unsigned)((n8 + 255) / 256), (unsigned)pl->N), 256, 0, st>>>(hp, n8);
-    BASP_CUDA_TRY(cudaGetLastError());
-    basp_count_launch(3);
+    if (n_fin > 0)
+        BASP_CUDA_TRY(launch_early(mb_finish_kernel<R>, dim3((unsigned)((n_fin + 255) / 256), (unsigned)pl->N), 256, st, fin));
+    basp_count_launch(n_fin > 0 ? 3 : 2);
     return BASP_OK;
 }
 

@@ -4,9 +4,12 @@
 // the cap and the bias, and dS the cap's derivative.
 #pragma once
 
-template <int R, bool kCap, bool kBias>
+template <int R, bool kCap, bool kBias, bool kSmall>
 __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(const __grid_constant__ MaskedBwdParams<R> p) {
     constexpr int D = 128;
+    // How far the issuing loops are unrolled: the code of all roles together has to stay in the instruction cache (16K causal tokens, 32/8
+    // heads of 128, cap 50: 7.0 ms at four, 7.6 in full; without a cap 5.6 in full, 6.1 at four)
+    constexpr int kUnroll = kCap ? 4 : 8;
     constexpr int kTileBytes = kT * D * 2;             // 32 KiB: two slabs of [128 rows][64 columns]
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t *sK = smem, *sV = smem + kTileBytes;
@@ -16,7 +19,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
     uint8_t *sdS = smem + (4 + kDoStages) * kTileBytes;   // dS^T [key rows][query cols], two 64-column slabs
     float *s_lse = reinterpret_cast<float *>(smem + 7 * kTileBytes);   // [2][128], already times log2(e)
     float *s_delta = s_lse + 2 * kT;                                   // [2][128], already times -scale
-    uint16_t *s_win = reinterpret_cast<uint16_t *>(s_delta + 2 * kT);  // [2][128], see stage_windows
+    uint16_t *s_win = reinterpret_cast<uint16_t *>(s_delta + 2 * kT);  // [2][128], see stage_stats
     int *s_edge = reinterpret_cast<int *>(s_win + 2 * kT);             // [2]
     BwdBars *bars = reinterpret_cast<BwdBars *>(s_edge + 2);
 
@@ -48,6 +51,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
+    wait_previous_kernel();        // (nothing of another kernel's was touched up to here)
+    allow_next_kernel();
     constexpr uint32_t kColST = 0, kColDP = 128, kColDK = 256, kColDV = 384;
     if (bars->abort_flag) goto bwd_done;
 
@@ -59,13 +64,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
         const uint32_t st_col = tmem + kColST + 32 * g + lane_addr;
         uint32_t it_g = 0, item_n = 0;
         MbItem item;
-        for (int round = 0; mb_get_item(p, round, item); ++round) {
+        for (int round = 0; mb_get_item<kSmall>(p, round, item); ++round) {
             if (item.m0 >= item.n_qt) {                 // no query sees a key of the tile
-                store_zeros(p, item, g, row);
+                store_zeros<kSmall>(p, item, g, row);
                 continue;
             }
-            for (int hq = 0; hq < p.q_per_kv; ++hq) {
-                const float slope = kBias ? __ldg(p.score.slopes + (item.r % p.K) * p.Hq_l + item.hkv * p.q_per_kv + hq) * 1.4426950408889634f : 0.f;
+            for (int hq = 0; hq < mb_heads<kSmall>(p, item); ++hq) {
+                const float slope = kBias ? __ldg(p.score.slopes + (item.r % p.K) * p.Hq_l + mb_first_head<kSmall>(p, item) + hq) * 1.4426950408889634f : 0.f;
                 for (int m = item.m0; m < item.n_qt; ++m, ++it_g) {
                     const uint32_t stage = it_g & 1, sph = (it_g >> 1) & 1;     // Q stage of the step (row statistics with it)
                     BWD_WAIT(&bars->stats_full[stage], sph, 10, m);             // LSE and Delta of the query tile
@@ -126,25 +131,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
             tc_fence_after();
             {
                 constexpr int kHalf = D / 2;
-                __nv_bfloat16 *base = (g < 2 ? p.dk[item.r] : p.dv[item.r]) +
-                                      (((size_t)item.bl * p.S + (size_t)item.n * kT + row) * p.Hkv_l + item.hkv) * p.Dg +
-                                      kHalf * (g & 1);
                 const uint32_t col0 = (g < 2 ? kColDK : kColDV) + kHalf * (g & 1);
 #pragma unroll
                 for (int cc = 0; cc < kHalf / 32; ++cc) {
                     uint32_t rr[32];
                     tmem_ld_x32(tmem + col0 + cc * 32 + lane_addr, rr);
                     tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint4 o4;
-                        o4.x = pack_bf16x2(__uint_as_float(rr[8 * i + 0]), __uint_as_float(rr[8 * i + 1]));
-                        o4.y = pack_bf16x2(__uint_as_float(rr[8 * i + 2]), __uint_as_float(rr[8 * i + 3]));
-                        o4.z = pack_bf16x2(__uint_as_float(rr[8 * i + 4]), __uint_as_float(rr[8 * i + 5]));
-                        o4.w = pack_bf16x2(__uint_as_float(rr[8 * i + 6]), __uint_as_float(rr[8 * i + 7]));
-                        if (kHalf * (g & 1) + cc * 32 + i * 8 < p.Dg && item.n * kT + row < p.S)
-                            *reinterpret_cast<uint4 *>(base + cc * 32 + i * 8) = o4;
-                    }
+                    store_kv<kSmall>(p, item, g >= 2, row, kHalf * (g & 1) + cc * 32, rr);
                 }
             }
             tc_fence_before();
@@ -164,12 +157,28 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
         const int d = wq * 32 + lane;                   // this thread's feature
         uint32_t it_g = 0;
         MbItem item;
-        for (int round = 0; mb_get_item(p, round, item); ++round) {
-            for (int hq = 0; hq < p.q_per_kv; ++hq) {
-                const int h = item.hkv * p.q_per_kv + hq;
+        for (int round = 0; mb_get_item<kSmall>(p, round, item); ++round) {
+            for (int hq = 0; hq < mb_heads<kSmall>(p, item); ++hq) {
+                const int h = mb_first_head<kSmall>(p, item) + hq;
                 for (int m = item.m0; m < item.n_qt; ++m, ++it_g) {
                     BWD_WAIT(&bars->dq_full, it_g & 1, 14, m);
                     tc_fence_after();
+                    if (kSmall && p.direct) {         // the only key tile: dQ as bf16
+                        __nv_bfloat16 *to = p.dq[item.r] + (((size_t)item.bl * p.S + (size_t)m * kT) * p.Hq_l + h) * p.Dg + d;
+#pragma unroll 1
+                        for (int c0 = 0; c0 < kT; c0 += 32) {
+                            uint32_t v[32];
+                            tmem_ld_x32(tmem + kColDP + c0 + lane_addr, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int c = 0; c < 32; ++c)
+                                if (d < p.Dg && m * kT + c0 + c < p.S) to[(size_t)(c0 + c) * p.Hq_l * p.Dg] = __float2bfloat16(__uint_as_float(v[c]));
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bars->dq_read);
+                        continue;
+                    }
                     // accumulator element (query row m*128 + c, head h, feature d); a row past the end of the sequence
                     // (ragged last tile) and a feature past the head dimension have none
                     const size_t acc_row = (size_t)p.Hq_l * p.Dg;
@@ -211,7 +220,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
         // ======================================================================= TMA producer
         uint32_t it_g = 0, item_n = 0;
         MbItem item;
-        for (int round = 0; mb_get_item(p, round, item); ++round) {
+        for (int round = 0; mb_get_item<kSmall>(p, round, item); ++round) {
             if (item.m0 >= item.n_qt) continue;
             BWD_WAIT(&bars->kv_empty, (item_n & 1) ^ 1, 20, item.n);
             ++item_n;
@@ -223,8 +232,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
                     tma_load_3d(sV + s * 16384, &p.v[item.r], &bars->kv_full, s * 64, item.hkv, row0);
                 }
             }
-            for (int hq = 0; hq < p.q_per_kv; ++hq) {
-                const int h = item.hkv * p.q_per_kv + hq;
+            for (int hq = 0; hq < mb_heads<kSmall>(p, item); ++hq) {
+                const int h = mb_first_head<kSmall>(p, item) + hq;
                 for (int m = item.m0; m < item.n_qt; ++m, ++it_g) {
                     const uint32_t stage = it_g & 1, ph = (it_g >> 1) & 1;
                     const int row0 = item.bl * p.S + m * kT;
@@ -237,27 +246,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
                             tma_load_3d(sQ + stage * kTileBytes + s * 16384, &p.q[item.r], &bars->qdo_full[stage], s * 64, h, row0);
                     }
                     {
-                        const size_t off = ((size_t)item.bl * p.Hq_l + h) * p.S + (size_t)m * kT + 4 * lane;
-                        float4 l4, d4;
-                        if ((p.S & 3) == 0 && (m + 1) * kT <= p.S) {
-                            l4 = *reinterpret_cast<const float4 *>(p.lse[item.r] + off);
-                            d4 = *reinterpret_cast<const float4 *>(p.delta[item.r] + off);
-                        } else {                       // ragged: rows of (bl, h) are not 16-byte aligned, or the tile runs past S
-                            float lv[4], dv4[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const bool in_seq = m * kT + 4 * lane + e < p.S;
-                                lv[e] = in_seq ? p.lse[item.r][off + e] : 0.f;
-                                dv4[e] = in_seq ? p.delta[item.r][off + e] : 0.f;
-                            }
-                            l4 = make_float4(lv[0], lv[1], lv[2], lv[3]);
-                            d4 = make_float4(dv4[0], dv4[1], dv4[2], dv4[3]);
-                        }
-                        l4.x = seen_lse(l4.x); l4.y = seen_lse(l4.y); l4.z = seen_lse(l4.z); l4.w = seen_lse(l4.w);
-                        d4.x *= -p.scale; d4.y *= -p.scale; d4.z *= -p.scale; d4.w *= -p.scale;
-                        *reinterpret_cast<float4 *>(s_lse + stage * kT + 4 * lane) = l4;
-                        *reinterpret_cast<float4 *>(s_delta + stage * kT + 4 * lane) = d4;
-                        stage_windows(p, item, m, lane, s_win + stage * kT, s_edge + stage);
+                        const MbStats stats = fetch_stats(p, item, h, m, lane);
+                        stage_stats(p, item, m, lane, stats, s_lse + stage * kT, s_delta + stage * kT, s_win + stage * kT, s_edge + stage);
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&bars->stats_full[stage]);
                     }
@@ -283,9 +273,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
                        adO = smem_u32(sdO) >> 4, adS = smem_u32(sdS) >> 4;
         uint32_t it_g = 0, item_n = 0;
         MbItem item;
-        for (int round = 0; mb_get_item(p, round, item); ++round) {
+        for (int round = 0; mb_get_item<kSmall>(p, round, item); ++round) {
             if (item.m0 >= item.n_qt) continue;
-            const uint32_t steps = (uint32_t)p.q_per_kv * (uint32_t)(item.n_qt - item.m0);
+            const uint32_t steps = (uint32_t)mb_heads<kSmall>(p, item) * (uint32_t)(item.n_qt - item.m0);
             BWD_WAIT(&bars->kv_full, item_n & 1, 30, item.n);
             // (1) S^T = K Q^T of step `it` into X (its last reader, product (3) of step it-1, was issued before)
             auto issue_s = [&](uint32_t it) -> bool {
@@ -294,7 +284,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
                 tc_fence_after();
                 if (lane == 0) {
                     const uint32_t q16 = aQ + stage * (kTileBytes >> 4);
-#pragma unroll
+#pragma unroll kUnroll
                     for (int kk = 0; kk < D / 16; ++kk) {
                         const uint32_t off = ((kk / 4) * 16384 + (kk % 4) * 32) >> 4;
                         mma_ss(tmem + kColST, desc_k | (uint64_t)(aK + off), desc_k | (uint64_t)(q16 + off), idesc_kk, kk > 0);
@@ -310,7 +300,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
                 tc_fence_after();
                 if (lane == 0) {
                     const uint32_t do16 = adO + (it % kDoStages) * (kTileBytes >> 4);
-#pragma unroll
+#pragma unroll kUnroll
                     for (int kk = 0; kk < D / 16; ++kk) {
                         const uint32_t off = ((kk / 4) * 16384 + (kk % 4) * 32) >> 4;
                         mma_ss(tmem + kColDP, desc_k | (uint64_t)(aV + off), desc_k | (uint64_t)(do16 + off), idesc_kk, kk > 0);
@@ -328,7 +318,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
                 tc_fence_after();
                 if (lane == 0) {
                     const uint32_t do16 = adO + (it % kDoStages) * (kTileBytes >> 4);
-#pragma unroll
+#pragma unroll kUnroll
                     for (int kk = 0; kk < kT / 16; ++kk)
                         mma_ts(tmem + kColDV, tmem + kColST + (kk / 2) * 32 + (kk % 2) * 8,
                                desc_mn | (uint64_t)(do16 + kk * 128), idesc_kn, kk > 0 ? 1u : (first ? 0u : 1u));
@@ -350,13 +340,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
                     const uint32_t acc0 = j == 0 ? 0u : 1u;
                     // (5) dQ_m^T = K^T dS^T : A = K read MN-major (rows of the result = features), B = the dS^T buffer read
                     //     MN-major (columns = query rows); transposed so that the drain warps add whole lines
-#pragma unroll
+#pragma unroll kUnroll
                     for (int kk = 0; kk < kT / 16; ++kk)
                         mma_ss(tmem + kColDP, desc_mn | (uint64_t)(aK + kk * 128), desc_mn | (uint64_t)(adS + kk * 128),
                                idesc_nn, kk > 0);
                     tc_commit(&bars->dq_full);
                     // (4) dK += dS^T Q : A = dS^T from shared memory (K-major: query columns), B = Q MN-major
-#pragma unroll
+#pragma unroll kUnroll
                     for (int kk = 0; kk < kT / 16; ++kk) {
                         const uint32_t off = ((kk / 4) * 16384 + (kk % 4) * 32) >> 4;
                         mma_ss(tmem + kColDK, desc_k | (uint64_t)(adS + off), desc_mn | (uint64_t)(q16 + kk * 128),

@@ -2,7 +2,7 @@
 // attn_masked_bwd_d128.cuh names.
 #pragma once
 
-template <int R, bool kCap, bool kBias>
+template <int R, bool kCap, bool kBias, bool kSmall>
 __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(const __grid_constant__ MaskedBwdParams<R> p) {
     constexpr int D = 64;
     constexpr int kTileBytes = kT * D * 2;             // 16 KiB: one slab of [128 rows][64 columns]
@@ -16,7 +16,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
     uint8_t *sStage = sdS + 2 * 16384;                 // dQ staging: two chunks of [128 rows][32 floats] (32 KiB)
     float *s_lse = reinterpret_cast<float *>(sStage + 2 * 16384);      // [kQS][128], already times log2(e)
     float *s_delta = s_lse + kQS * kT;                                 // [kQS][128], already times -scale
-    uint16_t *s_win = reinterpret_cast<uint16_t *>(s_delta + kQS * kT);      // [kQS][128], see stage_windows
+    uint16_t *s_win = reinterpret_cast<uint16_t *>(s_delta + kQS * kT);      // [kQS][128], see stage_stats
     int *s_edge = reinterpret_cast<int *>(s_win + kQS * kT);                 // [kQS] (and a gap that keeps the barriers aligned)
     BwdBars *bars = reinterpret_cast<BwdBars *>(s_edge + 4);
 
@@ -47,6 +47,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
+    wait_previous_kernel();        // (nothing of another kernel's was touched up to here)
+    allow_next_kernel();
     constexpr uint32_t kColST = 0 /* + 128 * buffer */, kColDP = 256, kColDK = 384, kColDV = 448;
     if (bars->abort_flag) goto bwd_done;
 
@@ -57,13 +59,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         uint32_t it_g = 0, item_n = 0;
         MbItem item;
-        for (int round = 0; mb_get_item(p, round, item); ++round) {
-            if (item.m0 >= item.n_qt) {                 // no query sees a key of the tile
-                store_zeros(p, item, g, row);
+        for (int round = 0; mb_get_item<kSmall>(p, round, item); ++round) {
+            if (__builtin_expect(item.m0 >= item.n_qt, 0)) {    // no query sees a key of the tile
+                store_zeros<kSmall>(p, item, g, row);
                 continue;
             }
-            for (int hq = 0; hq < p.q_per_kv; ++hq) {
-                const float slope = kBias ? __ldg(p.score.slopes + (item.r % p.K) * p.Hq_l + item.hkv * p.q_per_kv + hq) * 1.4426950408889634f : 0.f;
+            for (int hq = 0; hq < mb_heads<kSmall>(p, item); ++hq) {
+                const float slope = kBias ? __ldg(p.score.slopes + (item.r % p.K) * p.Hq_l + mb_first_head<kSmall>(p, item) + hq) * 1.4426950408889634f : 0.f;
                 for (int m = item.m0; m < item.n_qt; ++m, ++it_g) {
                     const int buf = it_g & 1;                                   // S^T buffer of the step
                     const uint32_t stage = it_g % kQS, sph = (it_g / kQS) & 1;  // its Q / dO stage (row statistics with it)
@@ -125,22 +127,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
             BWD_WAIT(&bars->dkdv_full, item_n & 1, 13, item.n);
             tc_fence_after();
             {
-                __nv_bfloat16 *base = (g < 2 ? p.dk[item.r] : p.dv[item.r]) +
-                                      (((size_t)item.bl * p.S + (size_t)item.n * kT + row) * p.Hkv_l + item.hkv) * p.Dg +
-                                      32 * (g & 1);
                 uint32_t rr[32];
                 tmem_ld_x32(tmem + (g < 2 ? kColDK : kColDV) + 32 * (g & 1) + lane_addr, rr);
                 tmem_wait_ld();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint4 o4;
-                    o4.x = pack_bf16x2(__uint_as_float(rr[8 * i + 0]), __uint_as_float(rr[8 * i + 1]));
-                    o4.y = pack_bf16x2(__uint_as_float(rr[8 * i + 2]), __uint_as_float(rr[8 * i + 3]));
-                    o4.z = pack_bf16x2(__uint_as_float(rr[8 * i + 4]), __uint_as_float(rr[8 * i + 5]));
-                    o4.w = pack_bf16x2(__uint_as_float(rr[8 * i + 6]), __uint_as_float(rr[8 * i + 7]));
-                    if (32 * (g & 1) + i * 8 < p.Dg && item.n * kT + row < p.S)
-                        *reinterpret_cast<uint4 *>(base + i * 8) = o4;
-                }
+                if (32 * (g & 1) < p.Dg) store_kv<kSmall>(p, item, g >= 2, row, 32 * (g & 1), rr);
             }
             tc_fence_before();
             __syncwarp();
@@ -157,9 +147,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
         const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
         uint32_t it_g = 0;
         MbItem item;
-        for (int round = 0; mb_get_item(p, round, item); ++round) {
-            for (int hq = 0; hq < p.q_per_kv; ++hq) {
-                const int h = item.hkv * p.q_per_kv + hq;
+        for (int round = 0; mb_get_item<kSmall>(p, round, item); ++round) {
+            for (int hq = 0; hq < mb_heads<kSmall>(p, item); ++hq) {
+                const int h = mb_first_head<kSmall>(p, item) + hq;
                 for (int m = item.m0; m < item.n_qt; ++m, ++it_g) {
                     BWD_WAIT(&bars->dq_full, it_g & 1, 14, m);
                     tc_fence_after();
@@ -170,6 +160,16 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars->dq_read);          // TMEM is free for the next dP^T
+                    if (kSmall && p.direct) { // the only key tile: dQ as bf16, a row a thread
+                        __nv_bfloat16 *to = p.dq[item.r] + (((size_t)item.bl * p.S + row) * p.Hq_l + h) * p.Dg;
+#pragma unroll
+                        for (int i = 0; i < 64; i += 8)
+                            if (row < p.S && i < p.Dg)
+                                *reinterpret_cast<uint4 *>(to + i) = make_uint4(
+                                    pack_bf16x2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), pack_bf16x2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])),
+                                    pack_bf16x2(__uint_as_float(v[i + 4]), __uint_as_float(v[i + 5])), pack_bf16x2(__uint_as_float(v[i + 6]), __uint_as_float(v[i + 7])));
+                        continue;
+                    }
                     // this warp's rows of the staging buffer are free: lane 0 waited for the previous reduce-add's reads
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
         // ======================================================================= TMA producer
         uint32_t it_g = 0, item_n = 0;
         MbItem item;
-        for (int round = 0; mb_get_item(p, round, item); ++round) {
+        for (int round = 0; mb_get_item<kSmall>(p, round, item); ++round) {
             if (item.m0 >= item.n_qt) continue;
             BWD_WAIT(&bars->kv_empty, (item_n & 1) ^ 1, 20, item.n);
             ++item_n;
@@ -210,8 +210,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
                 tma_load_3d(sK, &p.k[item.r], &bars->kv_full, 0, item.hkv, row0);
                 tma_load_3d(sV, &p.v[item.r], &bars->kv_full, 0, item.hkv, row0);
             }
-            for (int hq = 0; hq < p.q_per_kv; ++hq) {
-                const int h = item.hkv * p.q_per_kv + hq;
+            for (int hq = 0; hq < mb_heads<kSmall>(p, item); ++hq) {
+                const int h = mb_first_head<kSmall>(p, item) + hq;
                 for (int m = item.m0; m < item.n_qt; ++m, ++it_g) {
                     const uint32_t stage = it_g % kQS, ph = (it_g / kQS) & 1;
                     // the stage (tiles and row statistics) is free once products (3) and (4) of three steps ago are done
@@ -223,27 +223,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
                         tma_load_3d(sdO + stage * kTileBytes, &p.dout[item.r], &bars->qdo_full[stage], 0, h, row0);
                     }
                     {
-                        const size_t off = ((size_t)item.bl * p.Hq_l + h) * p.S + (size_t)m * kT + 4 * lane;
-                        float4 l4, d4;
-                        if ((p.S & 3) == 0 && (m + 1) * kT <= p.S) {
-                            l4 = *reinterpret_cast<const float4 *>(p.lse[item.r] + off);
-                            d4 = *reinterpret_cast<const float4 *>(p.delta[item.r] + off);
-                        } else {                       // ragged: rows of (bl, h) are not 16-byte aligned, or the tile runs past S
-                            float lv[4], dv4[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const bool in_seq = m * kT + 4 * lane + e < p.S;
-                                lv[e] = in_seq ? p.lse[item.r][off + e] : 0.f;
-                                dv4[e] = in_seq ? p.delta[item.r][off + e] : 0.f;
-                            }
-                            l4 = make_float4(lv[0], lv[1], lv[2], lv[3]);
-                            d4 = make_float4(dv4[0], dv4[1], dv4[2], dv4[3]);
-                        }
-                        l4.x = seen_lse(l4.x); l4.y = seen_lse(l4.y); l4.z = seen_lse(l4.z); l4.w = seen_lse(l4.w);
-                        d4.x *= -p.scale; d4.y *= -p.scale; d4.z *= -p.scale; d4.w *= -p.scale;
-                        *reinterpret_cast<float4 *>(s_lse + stage * kT + 4 * lane) = l4;
-                        *reinterpret_cast<float4 *>(s_delta + stage * kT + 4 * lane) = d4;
-                        stage_windows(p, item, m, lane, s_win + stage * kT, s_edge + stage);
+                        const MbStats stats = fetch_stats(p, item, h, m, lane);
+                        stage_stats(p, item, m, lane, stats, s_lse + stage * kT, s_delta + stage * kT, s_win + stage * kT, s_edge + stage);
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&bars->stats_full[stage]);
                     }
@@ -261,9 +242,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d64_kernel(con
                        adO = smem_u32(sdO) >> 4, adS = smem_u32(sdS) >> 4;
         uint32_t it_g = 0, item_n = 0;
         MbItem item;
-        for (int round = 0; mb_get_item(p, round, item); ++round) {
+        for (int round = 0; mb_get_item<kSmall>(p, round, item); ++round) {
             if (item.m0 >= item.n_qt) continue;
-            const uint32_t steps = (uint32_t)p.q_per_kv * (uint32_t)(item.n_qt - item.m0);
+            const uint32_t steps = (uint32_t)mb_heads<kSmall>(p, item) * (uint32_t)(item.n_qt - item.m0);
             BWD_WAIT(&bars->kv_full, item_n & 1, 30, item.n);
             // (1) S^T = K Q^T of step `it` into its S^T buffer (the P^T that lived there was read by product (3) of step
             //     it-2, issued before)

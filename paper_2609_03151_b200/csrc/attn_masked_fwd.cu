@@ -11,9 +11,8 @@
 //   - only tiles that are not wholly visible are masked, with the bounds of the thread's row.  A row can meet such a
 //     tile before it has seen any key: its reference stays -inf and its exponentials are taken against 0.
 //   - items are dealt longest first in the mask object's order.
-//   - the scores are shaped on their way into the exponentials.  tanh runs on the FMA pipe as an odd polynomial where all of a warp's
-//     scores are below 0.4 of the cap (score.cuh), since the exponentials already fill the special-function unit: 1 - 2 / (exp(2x) + 1)
-//     for every score would give that unit three operations where it has one.
+// Capped or biased scores have a kernel of their own (attn_shaped_fwd.cuh): four softmax warpgroups instead of two.  For plain scores two
+// are better (16K causal tokens, 32/8 heads of 128: 1.55-1.7 ms and 1.8).
 #include <cuda.h>
 #include <math.h>
 
@@ -129,11 +128,10 @@ constexpr uint32_t kMfSleepNs = 32;      // back-off of the correction and produ
         }                                                                       \
     } while (0)
 
-template <int D, int R, bool kCap, bool kBias>
+template <int D, int R>
 __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __grid_constant__ MaskedFwdParams<R> p) {
     constexpr int kSlabs = D / 64;
     constexpr int kTileBytes = kTile * D * 2;
-    constexpr bool kShaped = kCap || kBias;            // the scores are brought to log2 units before the maximum is taken
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t *sQ = smem;                                // 2 tiles
@@ -168,6 +166,8 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
+    wait_previous_kernel();        // (nothing of another kernel's was touched up to here)
+    allow_next_kernel();
     // One score tile S at columns 0..127 (the two query tiles take turns), P_t at 128 + 64 t, O_t at 256 + 128 t.
 
     if (warp < 8) {
@@ -199,21 +199,7 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
             } else if (s_pos < p.S) {
                 hi = p.causal ? s_pos + 1 : p.S;
             }
-            // log2 units; the bound on a tile's bias is at most 127 |slope| above what any of its keys has, and a reference that is
-            // up to 2^96 too large leaves the exponentials ordinary numbers (24 bits above 2^-126)
-            [[maybe_unused]] const float slope = kBias ? __ldg(p.score.slopes + (item.r % p.K) * p.Hq_l + item.h) * 1.4426950408889634f : 0.f;
-            // With a cap no maximum is needed: |z| is at most the cap (in log2 units, 80 at most for this), so the exponentials of the
-            // row are ordinary numbers against the bias that its nearest key has (its furthest, for a negative slope), or 0.
-            [[maybe_unused]] const bool bounded = kCap && p.score.cap_out <= 80.f;
-            [[maybe_unused]] const bool steep = kBias && !bounded && fabsf(slope) * (float)(kTile - 1) > 96.f;
             float m_ref = -INFINITY, l_run = 0.f;
-            if (bounded) {
-                m_ref = 0.f;
-                if constexpr (kBias) {
-                    const int dist = slope >= 0.f ? max(max(lo - s_pos, s_pos - hi + 1), 0) : max(s_pos - lo, hi - 1 - s_pos);
-                    if (hi > lo) m_ref = -slope * (float)dist;
-                }
-            }
             for (int j = begin; j < end; ++j, ++it_cnt) {
                 MF_WAIT(&sh.s_full[t], it_cnt & 1, 10 + t, j);
                 tc_fence_after();
@@ -226,29 +212,7 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.s_free);       // the scores are in registers: the other tile's Q.K^T may overwrite S
-                // Keys outside of [lo, hi) are hidden.  The scores stay raw and are shaped on the way into the exponentials: the maximum
-                // is taken over raw scores (the bias of a tile has a bound), or not at all (a capped score has one); only where neither
-                // holds (`slow`) are they shaped in place first.  What is rare is laid out of line: the loop has to fit the
-                // instruction caches.
-                const bool edge = j < full || j >= full_end;
-                [[maybe_unused]] float sl = 0.f, base = 0.f;                 // bias of key i: sl i + base
-                [[maybe_unused]] bool slow = kCap && !bounded, far = false;
-                if constexpr (kBias) {
-                    sl = j <= qt ? slope : -slope;
-                    base = -sl * (float)(s_pos - j * kTile);
-                    slow |= steep || (j == qt && __any_sync(0xffffffffu, min(hi - j * kTile, kTile) - 1 > row));
-                }
-                if constexpr (kCap) {
-                    float top[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int i = 0; i < kTile; i += 8)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) top[k] = max3_abs(top[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
-                    far = __any_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) > p.score.near_limit);
-                }
-                if constexpr (kShaped)
-                    if (__builtin_expect(slow, 0)) shape_scores<kCap, kBias>(s, p.score, p.scale_log2, slope, s_pos - j * kTile);
-                if (__builtin_expect(edge, 0)) {
+                if (__builtin_expect(j < full || j >= full_end, 0)) {     // keys outside of [lo, hi) are hidden
                     const int first = lo - j * kTile, past = hi - j * kTile;
                     if (__any_sync(0xffffffffu, first > 0)) {
 #pragma unroll
@@ -261,113 +225,38 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
                             if (i >= past) s[i] = 0xff800000u;
                     }
                 }
+                float mxs[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mxs[i] = max3(__uint_as_float(s[i]), __uint_as_float(s[8 + i]), __uint_as_float(s[16 + i]));
+#pragma unroll
+                for (int i = 24; i + 15 < kTile; i += 16)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        mxs[k] = max3(mxs[k], __uint_as_float(s[i + k]), __uint_as_float(s[i + 8 + k]));
+#pragma unroll
+                for (int k = 0; k < 8; ++k) mxs[k] = fmaxf(mxs[k], __uint_as_float(s[120 + k]));
+                const float mx = fmaxf(fmaxf(fmaxf(mxs[0], mxs[1]), fmaxf(mxs[2], mxs[3])),
+                                       fmaxf(fmaxf(mxs[4], mxs[5]), fmaxf(mxs[6], mxs[7]))) * p.scale_log2;
                 float alpha = 1.f;
-                if (!kCap || slow) {
-                    float mxs[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) mxs[i] = max3(__uint_as_float(s[i]), __uint_as_float(s[8 + i]), __uint_as_float(s[16 + i]));
-#pragma unroll
-                    for (int i = 24; i + 15 < kTile; i += 16)
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            mxs[k] = max3(mxs[k], __uint_as_float(s[i + k]), __uint_as_float(s[i + 8 + k]));
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) mxs[k] = fmaxf(mxs[k], __uint_as_float(s[120 + k]));
-                    float mx = fmaxf(fmaxf(fmaxf(mxs[0], mxs[1]), fmaxf(mxs[2], mxs[3])),
-                                     fmaxf(fmaxf(mxs[4], mxs[5]), fmaxf(mxs[6], mxs[7])));
-                    if (!slow && mx != -INFINITY) {
-                        mx *= p.scale_log2;
-                        if constexpr (kBias) mx += fmaxf(base, fmaf(sl, (float)(kTile - 1), base));
-                    }
-                    if (mx > m_ref + kMfRescale) { alpha = exp2_approx(m_ref - mx); m_ref = mx; }
-                }
+                if (mx > m_ref + kMfRescale) { alpha = exp2_approx(m_ref - mx); m_ref = mx; }
                 sh.alpha[t][it_cnt & 1][row] = alpha;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.alpha_full[t][it_cnt & 1]);
                 const float m_sub = m_ref == -INFINITY ? 0.f : m_ref;      // no key yet: every exponential is exp2(-inf) = 0
                 uint64_t rs2[2] = {0ull, 0ull};
-                // kKind: 0 raw scores, 1 in log2 units already, 2 capped by the polynomial, 3 capped by the formula that holds everywhere;
-                // kEdge: some are -inf (where it makes a difference)
-                // kCols: of the first kCols scores; the bias of the first one is `from`
-                auto exp_row = [&](auto kind_tag, auto edge_tag, [[maybe_unused]] float from) {
-                    constexpr int kKind = decltype(kind_tag)::value, kCols = kShaped ? kTile / 2 : kTile;
-                    [[maybe_unused]] constexpr bool kEdge = decltype(edge_tag)::value;
-                    const uint64_t sc2 = both(p.scale_log2), nm2 = both(-m_sub);
-                    [[maybe_unused]] uint64_t ramp[4], block = 0;         // the bias of pair i as ramp + block: no constants in the code
-                    if constexpr (kBias && kKind != 1)
+                const uint64_t sc2 = both(p.scale_log2), nm2 = both(-m_sub);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) ramp[k] = pack_f2(sl * (float)(2 * k), sl * (float)(2 * k + 1));
-                    [[maybe_unused]] const float most = p.score.near_limit * p.score.near_limit;
-                    [[maybe_unused]] const uint64_t turn2 = both(p.score.cap_in * 2.8853900817779268f), fall2 = both(-2.f * p.score.cap_out),
-                                                    one2 = both(1.f), out2 = both(p.score.cap_out);
-#pragma unroll
-                    for (int i = 0; i < kCols; i += 2) {
-                        const uint64_t s2 = pack_f2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-                        uint64_t off = nm2, x2;
-                        if constexpr (kBias && kKind != 1) {
-                            if (i % 8 == 0) block = both(fmaf(sl, (float)i, from - m_sub));
-                            off = add2(ramp[(i >> 1) & 3], block);
-                        }
-                        if constexpr (kKind == 0) {
-                            x2 = fma2(s2, sc2, off);
-                        } else if constexpr (kKind == 1) {
-                            x2 = add2(s2, off);
-                        } else if constexpr (kKind == 2) {
-                            uint64_t y = mul2(s2, s2);
-                            if constexpr (kEdge) {                          // -inf: a finite positive q, and -inf again times it
-                                float y0, y1;
-                                unpack_f2(y, y0, y1);
-                                y = pack_f2(fminf(y0, most), fminf(y1, most));
-                            }
-                            x2 = fma2(s2, cap_near_q(y, p.score), off);
-                        } else {
-                            // c - 2 c / (exp(2x) + 1); the bound keeps exp(2x) finite
-                            float w0, w1;
-                            unpack_f2(mul2(s2, turn2), w0, w1);
-                            unpack_f2(add2(pack_f2(exp2_approx(w0 > 64.f ? 64.f : w0), exp2_approx(w1 > 64.f ? 64.f : w1)), one2), w0, w1);
-                            x2 = fma2(pack_f2(rcp_approx(w0), rcp_approx(w1)), fall2, add2(off, out2));
-                            if constexpr (kEdge) {                          // hidden: -inf stays -inf
-                                float x0, x1;
-                                unpack_f2(x2, x0, x1);
-                                x2 = pack_f2(s[i] == 0xff800000u ? -INFINITY : x0, s[i + 1] == 0xff800000u ? -INFINITY : x1);
-                            }
-                        }
-                        float x0, x1;
-                        unpack_f2(x2, x0, x1);
-                        const float e0 = exp2_approx(x0), e1 = exp2_approx(x1);
-                        rs2[(i >> 1) & 1] = add2(rs2[(i >> 1) & 1], pack_f2(e0, e1));
-                        s[i >> 1] = pack_bf16x2(e0, e1);
-                    }
-                };
-                using No = std::false_type;
-                using Yes = std::true_type;
-                // (the previous P_t V has read P_t before this step's replaces it)
-                if constexpr (!kShaped) {
-                    exp_row(std::integral_constant<int, 0>{}, No{}, 0.f);
-                    if (it_cnt > 0) { MF_WAIT(&sh.pv_done[t], (it_cnt - 1) & 1, 14 + t, j); tc_fence_after(); }
-                    tmem_st_x32(P_t + 0, *reinterpret_cast<const uint32_t(*)[32]>(&s[0]));
-                    tmem_st_x32(P_t + 32, *reinterpret_cast<const uint32_t(*)[32]>(&s[32]));
-                } else {
-                    if (it_cnt > 0) { MF_WAIT(&sh.pv_done[t], (it_cnt - 1) & 1, 14 + t, j); tc_fence_after(); }
-                    // Two passes of one copy of the loop over half of the row each: unrolled over the whole row the loop does not fit
-                    // the instruction cache beside the other warps' (12 times the misses, and a third of the time)
-#pragma unroll 1
-                    for (int half = 0; half < 2; ++half) {
-                        [[maybe_unused]] const float from = fmaf(sl, (float)(half * (kTile / 2)), base);
-                        if constexpr (kCap) {
-                            if (__builtin_expect(slow, 0)) exp_row(std::integral_constant<int, 1>{}, No{}, 0.f);
-                            else if (__builtin_expect(far, 0)) exp_row(std::integral_constant<int, 3>{}, Yes{}, from);
-                            else if (__builtin_expect(edge, 0)) exp_row(std::integral_constant<int, 2>{}, Yes{}, from);
-                            else exp_row(std::integral_constant<int, 2>{}, No{}, from);
-                        } else {
-                            if (__builtin_expect(slow, 0)) exp_row(std::integral_constant<int, 1>{}, No{}, 0.f);
-                            else exp_row(std::integral_constant<int, 0>{}, No{}, from);
-                        }
-                        tmem_st_x32(P_t + 32 * half, *reinterpret_cast<const uint32_t(*)[32]>(&s[0]));
-#pragma unroll
-                        for (int i = 0; i < kTile / 2; ++i) s[i] = s[kTile / 2 + i];
-                    }
+                for (int i = 0; i < kTile; i += 2) {
+                    float x0, x1;
+                    unpack_f2(fma2(pack_f2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), sc2, nm2), x0, x1);
+                    const float e0 = exp2_approx(x0), e1 = exp2_approx(x1);
+                    rs2[(i >> 1) & 1] = add2(rs2[(i >> 1) & 1], pack_f2(e0, e1));
+                    s[i >> 1] = pack_bf16x2(e0, e1);
                 }
+                // the previous P_t V has read P_t before this step's replaces it
+                if (it_cnt > 0) { MF_WAIT(&sh.pv_done[t], (it_cnt - 1) & 1, 14 + t, j); tc_fence_after(); }
+                tmem_st_x32(P_t + 0, *reinterpret_cast<const uint32_t(*)[32]>(&s[0]));
+                tmem_st_x32(P_t + 32, *reinterpret_cast<const uint32_t(*)[32]>(&s[32]));
                 float ra, rb;
                 unpack_f2(add2(rs2[0], rs2[1]), ra, rb);
                 l_run = l_run * alpha + (ra + rb);
@@ -582,12 +471,22 @@ mf_done:
 
 #undef MF_WAIT
 
-template <int D, int R, bool kCap, bool kBias>
+#include "attn_shaped_fwd.cuh"
+
+template <int D, int R, int kForm, bool kBias>
+int sf_launch(const MaskedFwdParams<R> &prm, int grid, cudaStream_t st) {
+    constexpr int smem = (2 + kMfStages) * kTile * D * 2 + 1024;
+    BASP_TRY((allow_smem<attn_shaped_fwd_kernel<D, R, kForm, kBias>, smem>()));
+    BASP_CUDA_TRY(launch_early_smem(attn_shaped_fwd_kernel<D, R, kForm, kBias>, dim3(grid), kSfThreads, smem, st, prm));
+    basp_count_launch(1);
+    return BASP_OK;
+}
+
+template <int D, int R>
 int mf_launch(const MaskedFwdParams<R> &prm, int grid, cudaStream_t st) {
-    const int smem = (2 + kMfStages) * kTile * D * 2 + 1024;
-    BASP_CUDA_TRY(cudaFuncSetAttribute(attn_masked_fwd_kernel<D, R, kCap, kBias>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    attn_masked_fwd_kernel<D, R, kCap, kBias><<<grid, kMfThreads, smem, st>>>(prm);
-    BASP_CUDA_TRY(cudaGetLastError());
+    constexpr int smem = (2 + kMfStages) * kTile * D * 2 + 1024;
+    BASP_TRY((allow_smem<attn_masked_fwd_kernel<D, R>, smem>()));
+    BASP_CUDA_TRY(launch_early_smem(attn_masked_fwd_kernel<D, R>, dim3(grid), kMfThreads, smem, st, prm));
     basp_count_launch(1);
     return BASP_OK;
 }
@@ -621,13 +520,21 @@ int mf_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
     prm.div_q_per_kv = make_fastdiv((uint32_t)(pl->Hq_l / pl->Hkv_l));
     prm.div_B = make_fastdiv((uint32_t)pl->B);
     prm.div_bl = make_fastdiv((uint32_t)pl->Bl);
-    int dev = 0, sms = 0;
-    BASP_CUDA_TRY(cudaGetDevice(&dev));
-    BASP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    int sms = 0;
+    BASP_TRY(sm_count(&sms));
     const int grid = (int)(total < sms ? total : sms);
     return dispatch_score(prm.score.cap_out > 0.f, prm.score.slopes != nullptr, [&](auto cap, auto bias) {
         constexpr bool kCap = decltype(cap)::value, kBias = decltype(bias)::value;
-        return pl->D > 64 ? mf_launch<128, R, kCap, kBias>(prm, grid, st) : mf_launch<64, R, kCap, kBias>(prm, grid, st);
+        const auto shaped = [&](auto form) {
+            constexpr int kForm = decltype(form)::value;
+            return pl->D > 64 ? sf_launch<128, R, kForm, kBias>(prm, grid, st) : sf_launch<64, R, kForm, kBias>(prm, grid, st);
+        };
+        if constexpr (kCap)
+            return prm.score.cap_out <= 80.f ? shaped(std::integral_constant<int, 0>{}) : shaped(std::integral_constant<int, 2>{});
+        else if constexpr (kBias)
+            return shaped(std::integral_constant<int, 1>{});
+        else
+            return pl->D > 64 ? mf_launch<128, R>(prm, grid, st) : mf_launch<64, R>(prm, grid, st);
     });
 }
 

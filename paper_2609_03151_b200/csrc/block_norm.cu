@@ -28,6 +28,7 @@ constexpr int kMaxHidden = 16384;
 constexpr int kMaxStages = 4;
 constexpr int kMaxWarps = 16;
 constexpr int kWarpRows = 8;               // groups of a block where a warp holds a row
+constexpr int kMaxSmem = 225 * 1024;       // of a block, beside its barriers and sums
 constexpr int kRingBytes = 192 * 1024;     // of all blocks of an SM, weights included
 
 // R: room for ranks (8 or BASP_MAX_RANKS; a launch takes longer the larger its parameters)
@@ -469,17 +470,21 @@ int launch(const basp_plan *pl, NormParams<R> &prm, int hidden, cudaStream_t st,
     const bool warp = s.threads == 32 * kWarpRows && hidden <= 512;
     const long long units = warp ? (prm.rows + kWarpRows - 1) / kWarpRows : prm.rows;
     *blocks = (int)(units < s.wave ? units : s.wave);
-    const auto go = [&](auto kernel) -> int {
-        BASP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem));
+    const auto go = [&](auto vectors, auto warp_tag) -> int {
+        constexpr auto kernel = block_norm_kernel<kBwd, decltype(warp_tag)::value, decltype(vectors)::value, R>;
+        BASP_TRY((allow_smem<block_norm_kernel<kBwd, decltype(warp_tag)::value, decltype(vectors)::value, R>, kMaxSmem>()));
         kernel<<<*blocks, s.threads, s.smem, st>>>(prm);
         BASP_CUDA_TRY(cudaGetLastError());
         basp_count_launch(1);
         return BASP_OK;
     };
-    if (warp) return s.vectors == 1 ? go(block_norm_kernel<kBwd, true, 1, R>) : go(block_norm_kernel<kBwd, true, 2, R>);
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using Four = std::integral_constant<int, 4>;
+    if (warp) return s.vectors == 1 ? go(One{}, std::true_type{}) : go(Two{}, std::true_type{});
     if constexpr (!kBwd)
-        if (s.vectors == 1) return go(block_norm_kernel<false, false, 1, R>);
-    return s.vectors == 2 ? go(block_norm_kernel<kBwd, false, 2, R>) : go(block_norm_kernel<kBwd, false, 4, R>);
+        if (s.vectors == 1) return go(One{}, std::false_type{});
+    return s.vectors == 2 ? go(Two{}, std::false_type{}) : go(Four{}, std::false_type{});
 }
 
 // Adds one tensor's shards to the spans and the parameter block

@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "plan.h"
 
 #define BASP_CUDA_TRY(expr)                                                   \
@@ -43,6 +45,42 @@ cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, cuda
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Lets a kernel have up to so much dynamic shared memory: set once per kernel and device (a microsecond of host time at every launch
+// otherwise).
+template <auto kKernel, int kBytes>
+int allow_smem() {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    BASP_CUDA_TRY(cudaGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return BASP_OK;
+    BASP_CUDA_TRY(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes));
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return BASP_OK;
+}
+inline int sm_count(int *sms) {
+    int dev = 0;
+    BASP_CUDA_TRY(cudaGetDevice(&dev));
+    BASP_CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+    return BASP_OK;
+}
+
+// The same with dynamic shared memory
+template <typename... Params, typename... Args>
+cudaError_t launch_early_smem(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const Args &...args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -98,11 +98,11 @@ namespace {
 // The layer's backward pass with `attend(doh, dqh, dkh, dvh, workspace, bytes)` as that of its attention.
 template <typename Attend>
 int layer_bwd_with(const basp_plan *p, const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq,
-                   void *workspace, size_t workspace_bytes, float softmax_scale, void *stream, Attend &&attend) {
+                   void *workspace, size_t workspace_bytes, size_t need, float softmax_scale, void *stream, Attend &&attend) {
     if (!p || !workspace) return BASP_ERR_NULL;
     if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
     if (!aligned16(workspace)) return BASP_ERR_ALIGN;
-    if (workspace_bytes < basp_layer_bwd_workspace_bytes(p)) return BASP_ERR_WORKSPACE;
+    if (workspace_bytes < need) return BASP_ERR_WORKSPACE;
     char *w = (char *)workspace;
     void *doh[BASP_MAX_RANKS], *dqh[BASP_MAX_RANKS], *dkh[BASP_MAX_RANKS], *dvh[BASP_MAX_RANKS];
     const size_t qb = q_head_bytes(p), kb = kv_head_bytes(p);
@@ -126,19 +126,23 @@ extern "C" int basp_layer_bwd(const basp_plan *p, const void *const *q_head, con
                               const void *const *do_seq, void *const *dq_seq, void *const *dk_seq,
                               void *const *dv_seq, void *workspace, size_t workspace_bytes, float softmax_scale,
                               void *stream) {
-    return layer_bwd_with(p, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes, softmax_scale, stream,
+    return layer_bwd_with(p, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes, basp_layer_bwd_workspace_bytes(p), softmax_scale, stream,
                           [&](void *const *doh, void *const *dqh, void *const *dkh, void *const *dvh, void *ws, size_t bytes) {
                               return basp_attn_bwd(p, q_head, k_head, v_head, o_head, doh, lse_shards, dqh, dkh, dvh, ws, bytes,
                                                    softmax_scale, stream);
                           });
 }
 
-// (the workspace holds that of basp_attn_bwd, which is the larger one)
+extern "C" size_t basp_layer_masked_bwd_workspace_bytes(const basp_plan *p) {
+    if (!p) return 0;
+    return (size_t)p->N * (2 * q_head_bytes(p) + 2 * kv_head_bytes(p)) + basp_attn_masked_bwd_workspace_bytes(p);
+}
+
 extern "C" int basp_layer_masked_bwd(const basp_plan *p, const basp_score *score, const void *const *q_head, const void *const *k_head,
                                      const void *const *v_head, const void *const *o_head, const float *const *lse_shards,
                                      const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq,
                                      void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
-    return layer_bwd_with(p, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes, softmax_scale, stream,
+    return layer_bwd_with(p, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes, basp_layer_masked_bwd_workspace_bytes(p), softmax_scale, stream,
                           [&](void *const *doh, void *const *dqh, void *const *dkh, void *const *dvh, void *ws, size_t bytes) {
                               return basp_attn_masked_bwd(p, score, q_head, k_head, v_head, o_head, doh, lse_shards, dqh, dkh, dvh, ws,
                                                           bytes, softmax_scale, stream);

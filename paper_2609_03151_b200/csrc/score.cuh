@@ -33,14 +33,13 @@ __device__ __forceinline__ float tanh_far(float x) {
     return fmaf(-2.f, rcp_approx(exp2_approx(w) + 1.f), 1.f);
 }
 
-// The 128 raw scores of a query row against one key tile brought to log2 units in place, by the formulas that hold everywhere: where the
-// cap is reached, where the bias is steep, where a row has keys on both sides.  dist0: the row's position minus that of the tile's
-// first key.
-template <bool kCap, bool kBias>
-__device__ __forceinline__ void shape_scores(uint32_t (&s)[128], const ScoreArgs &a, float scale_log2, float slope, int dist0) {
+// Raw scores of a query row against neighbouring keys brought to log2 units in place, by the formulas that hold everywhere: where the cap
+// is reached, where the bias is steep, where a row has keys on both sides.  dist0: the row's position minus that of the first key.
+template <bool kCap, bool kBias, int kCount>
+__device__ __forceinline__ void shape_scores(uint32_t (&s)[kCount], const ScoreArgs &a, float scale_log2, float slope, int dist0) {
     const float d0 = (float)dist0;
 #pragma unroll
-    for (int i = 0; i < 128; ++i) {
+    for (int i = 0; i < kCount; ++i) {
         float z = __uint_as_float(s[i]);
         z = kCap ? tanh_far(z * a.cap_in) * a.cap_out : z * scale_log2;
         if constexpr (kBias) z = fmaf(-slope, fabsf(d0 - (float)i), z);

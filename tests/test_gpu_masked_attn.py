@@ -220,7 +220,8 @@ def test_many_tiles_against_the_causal_kernel(basp):
     for score in (None, basp.basp_score(mask=mask), basp.basp_score()):
         o, lse = [torch.full_like(t, float("nan")) for t in q], [torch.empty((1, 4, 7600), device="cuda") for _ in range(2)]
         grads = [[torch.full_like(t, float("nan")) for t in x] for x in (q, k, v)]
-        ws = torch.empty(basp.basp_attn_bwd_workspace_bytes(pl), dtype=torch.uint8, device="cuda")
+        size = basp.basp_attn_bwd_workspace_bytes if score is None else basp.basp_attn_masked_bwd_workspace_bytes
+        ws = torch.empty(size(pl), dtype=torch.uint8, device="cuda")
         if score is None:
             basp.basp_attn_fwd(pl, q, k, v, o, lse)
             basp.basp_attn_bwd(pl, q, k, v, o, do, lse, *grads, ws)

@@ -89,11 +89,19 @@ def test_masked_layer_refusals(basp, plan):
     assert fwd(ws=0x20_0000_0008) == basp.BASP_ERR_ALIGN
     assert fwd(n=need - 1) == basp.BASP_ERR_WORKSPACE
     assert fwd(scale=-1.0) == basp.BASP_ERR_INVALID
-    n = basp.basp_layer_bwd_workspace_bytes(plan)
+    n = basp.basp_layer_masked_bwd_workspace_bytes(plan)
+    assert n > basp.basp_attn_masked_bwd_workspace_bytes(plan) and basp.lib.basp_layer_masked_bwd_workspace_bytes(None) == 0
     bwd = lambda ws=0x20_0000_0000, n=n: basp.lib.basp_layer_masked_bwd(plan.handle, score, *[P(table(0x10 + i)) for i in range(9)], ws, n, 0.0, None)
     assert bwd(ws=None) == basp.BASP_ERR_NULL
     assert bwd(n=n - 1) == basp.BASP_ERR_WORKSPACE
-    assert basp.basp_attn_masked_bwd_workspace_bytes(plan) <= basp.basp_attn_bwd_workspace_bytes(plan)      # the layer's has room for it
+
+
+def test_score_structure(basp):
+    """What the binding packs is the library's structure."""
+    m = type("M", (), {"space": lambda self, mask: (0x1234567890, 77)})()
+    packed = basp.basp_score(2.5, None, object()).pack(m, 0x9876543210)
+    s = basp._Score.from_buffer_copy(packed)
+    assert len(packed) == ctypes.sizeof(basp._Score) and (s.softcap, s.slopes, s.mask, s.mask_bytes) == (2.5, 0x9876543210, 0x1234567890, 77)
 
 
 @pytest.mark.parametrize("scaling", ["none", "linear", "yarn", "wavelength"])
