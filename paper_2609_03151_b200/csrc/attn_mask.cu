@@ -6,7 +6,7 @@
 //
 // Three steps, each over warps: a warp takes a query tile (its rows' ranges and their extremes), then a key tile (which query
 // tiles see it), then a work item (its place in the order, longest first, by counting the longer ones: the place does not depend
-// on timing).  Up to 32 tiles one block does all three, above that they are three launches that start early.  The tables are a
+// on timing).  Up to 64 tiles one block does all three, above that they are three launches that start early.  The tables are a
 // few kilobytes: what bounds the calls is latency (two sequences of 777 tokens: 14 tiles, one launch).
 #include <type_traits>
 
@@ -19,7 +19,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kSmallTiles = 32;     // one block of 32 warps
+constexpr int kSmallTiles = 64;     // one block of 32 warps, up to two tiles each
 constexpr int kBigWarps = 8;
 
 struct MaskParams {
@@ -36,27 +36,36 @@ struct MaskParams {
 __device__ __forceinline__ int clamp_to(long long v, int hi) { return (int)(v < 0 ? 0 : v > hi ? hi : v); }
 
 // Ranges of the rows of a query tile and their extremes.
-__device__ __forceinline__ void tile_step(const MaskParams &p, int idx, int lane) {
+__device__ __forceinline__ MaskTile tile_step(const MaskParams &p, int idx, int lane) {
     const int seq = idx / p.n_tiles, tile = idx - seq * p.n_tiles;
     int lo_min = p.S, lo_max = 0, hi_min = p.S, hi_max = 0;
+    // the loads of all four rows first (positions and prefix, or begin and end)
+    const int *one = p.positions ? p.positions : p.begin, *other = p.positions ? p.prefix : p.end;
+    int u[kMaskTile / 32], v[kMaskTile / 32];
+#pragma unroll
+    for (int k = 0; k < kMaskTile / 32; ++k) {
+        const int i = tile * kMaskTile + k * 32 + lane;
+        const size_t at = (size_t)seq * p.S + i;
+        u[k] = i < p.S ? one[at] : -1;
+        v[k] = i < p.S && other ? other[at] : 0;
+    }
 #pragma unroll
     for (int k = 0; k < kMaskTile / 32; ++k) {
         const int i = tile * kMaskTile + k * 32 + lane;
         int lo = 0, hi = 0;
         if (i < p.S) {
-            const size_t at = (size_t)seq * p.S + i;
             if (p.positions) {
-                const int pos = p.positions[at];
+                const int pos = u[k];
                 if (pos >= 0) {
                     long long first = (long long)i - pos, past = (long long)i + 1;
-                    if (p.prefix) past = max(past, first + p.prefix[at]);
+                    if (p.prefix) past = max(past, first + v[k]);
                     if (p.window > 0) first = max(first, (long long)i - p.window + 1);
                     lo = clamp_to(first, p.S);
                     hi = clamp_to(past, p.S);
                 }
             } else {
-                lo = clamp_to(p.begin[at], p.S);
-                hi = clamp_to(p.end[at], p.S);
+                lo = clamp_to(u[k], p.S);
+                hi = clamp_to(v[k], p.S);
             }
             if (hi <= lo) lo = hi = 0;
             if (hi > lo) { lo_min = min(lo_min, lo); hi_max = max(hi_max, hi); }
@@ -69,29 +78,30 @@ __device__ __forceinline__ void tile_step(const MaskParams &p, int idx, int lane
     lo_max = __reduce_max_sync(0xffffffffu, lo_max);
     hi_min = __reduce_min_sync(0xffffffffu, hi_min);
     hi_max = __reduce_max_sync(0xffffffffu, hi_max);
-    if (lane == 0) {
-        MaskTile t{0, 0, 0, 0};
-        if (hi_max > lo_min) {
-            t.begin = lo_min / kMaskTile;
-            t.end = (hi_max + kMaskTile - 1) / kMaskTile;
-            t.full = (lo_max + kMaskTile - 1) / kMaskTile;
-            t.full_end = hi_min / kMaskTile;
-        }
-        p.tiles[idx] = t;
+    MaskTile t{0, 0, 0, 0};
+    if (hi_max > lo_min) {
+        t.begin = lo_min / kMaskTile;
+        t.end = (hi_max + kMaskTile - 1) / kMaskTile;
+        t.full = (lo_max + kMaskTile - 1) / kMaskTile;
+        t.full_end = hi_min / kMaskTile;
     }
+    if (lane == 0) p.tiles[idx] = t;
+    return t;
 }
 
-// The query tiles that see a key tile.
-__device__ __forceinline__ void seen_step(const MaskParams &p, int idx, int lane) {
+// The query tiles that see a key tile.  `tiles`, here and below, and `seen`: p's own, or copies in shared memory.
+__device__ __forceinline__ int2 seen_step(const MaskParams &p, const MaskTile *tiles, int idx, int lane) {
     const int seq = idx / p.n_tiles, n = idx - seq * p.n_tiles;
     int first = p.n_tiles, last = 0;
     for (int m = lane; m < p.n_tiles; m += 32) {
-        const MaskTile t = p.tiles[seq * p.n_tiles + m];
+        const MaskTile t = tiles[seq * p.n_tiles + m];
         if (t.begin <= n && n < t.end) { first = min(first, m); last = m + 1; }
     }
     first = __reduce_min_sync(0xffffffffu, first);
     last = __reduce_max_sync(0xffffffffu, last);
-    if (lane == 0) p.seen[idx] = last > 0 ? make_int2(first, last) : make_int2(0, 0);
+    const int2 range = last > 0 ? make_int2(first, last) : make_int2(0, 0);
+    if (lane == 0) p.seen[idx] = range;
+    return range;
 }
 
 // The place of a work item of either pass among all of its pass.
@@ -105,46 +115,51 @@ __device__ __forceinline__ int place_of(int mine, int count, int lane, F &&cost_
     }
     return __reduce_add_sync(0xffffffffu, before);
 }
-__device__ __forceinline__ int fwd_cost(const MaskParams &p, int e) {
+__device__ __forceinline__ int fwd_cost(const MaskParams &p, const MaskTile *tiles, int e) {
     const int seq = e / p.n_blocks, tile = 2 * (e - seq * p.n_blocks);
-    const MaskTile a = p.tiles[seq * p.n_tiles + tile];
-    const MaskTile b = tile + 1 < p.n_tiles ? p.tiles[seq * p.n_tiles + tile + 1] : MaskTile{0, 0, 0, 0};
+    const MaskTile a = tiles[seq * p.n_tiles + tile];
+    const MaskTile b = tile + 1 < p.n_tiles ? tiles[seq * p.n_tiles + tile + 1] : MaskTile{0, 0, 0, 0};
     return a.end - a.begin + b.end - b.begin;
 }
-__device__ __forceinline__ int bwd_cost(const MaskParams &p, int e) {
-    const int2 s = p.seen[e];
-    return s.y - s.x;
-}
-__device__ __forceinline__ void order_step(const MaskParams &p, int idx, int lane) {
+__device__ __forceinline__ void order_step(const MaskParams &p, const MaskTile *tiles, const int2 *seen, int idx, int lane) {
     const int n_fwd = p.B * p.n_blocks, n_bwd = p.B * p.n_tiles;
     if (idx < n_fwd) {
-        const int place = place_of(idx, n_fwd, lane, [&](int e) { return fwd_cost(p, e); });
+        const int place = place_of(idx, n_fwd, lane, [&](int e) { return fwd_cost(p, tiles, e); });
         if (lane == 0) {
             MaskFwdEntry e{};
             e.seq = idx / p.n_blocks;
             e.block = idx - e.seq * p.n_blocks;
             const int tile = e.seq * p.n_tiles + 2 * e.block;
-            e.tile[0] = p.tiles[tile];
-            if (2 * e.block + 1 < p.n_tiles) e.tile[1] = p.tiles[tile + 1];
+            e.tile[0] = tiles[tile];
+            if (2 * e.block + 1 < p.n_tiles) e.tile[1] = tiles[tile + 1];
             p.fwd[place] = e;
         }
     } else {
-        const int i = idx - n_fwd, place = place_of(i, n_bwd, lane, [&](int e) { return bwd_cost(p, e); });
+        const int i = idx - n_fwd, place = place_of(i, n_bwd, lane, [&](int e) { return seen[e].y - seen[e].x; });
         if (lane == 0) {
-            const int2 s = p.seen[i];
+            const int2 s = seen[i];
             p.bwd[place] = MaskBwdEntry{i / p.n_tiles, i % p.n_tiles, s.x, s.y};
         }
     }
 }
 
-__global__ void __launch_bounds__(32 * kSmallTiles) mask_small_kernel(const __grid_constant__ MaskParams p) {
+__global__ void __launch_bounds__(1024) mask_small_kernel(const __grid_constant__ MaskParams p) {
+    __shared__ MaskTile tiles[kSmallTiles];
+    __shared__ int2 seen[kSmallTiles];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
     const int n = p.B * p.n_tiles, items = n + p.B * p.n_blocks;
-    for (int i = warp; i < n; i += warps) tile_step(p, i, lane);
+    allow_next_kernel();
+    for (int i = warp; i < n; i += warps) {
+        const MaskTile t = tile_step(p, i, lane);
+        if (lane == 0) tiles[i] = t;
+    }
     __syncthreads();
-    for (int i = warp; i < n; i += warps) seen_step(p, i, lane);
+    for (int i = warp; i < n; i += warps) {
+        const int2 s = seen_step(p, tiles, i, lane);
+        if (lane == 0) seen[i] = s;
+    }
     __syncthreads();
-    for (int i = warp; i < items; i += warps) order_step(p, i, lane);
+    for (int i = warp; i < items; i += warps) order_step(p, tiles, seen, i, lane);
 }
 
 template <int kStep>
@@ -154,8 +169,8 @@ __global__ void __launch_bounds__(32 * kBigWarps) mask_step_kernel(const __grid_
     allow_next_kernel();
     if (idx >= items) return;
     if (kStep == 0) tile_step(p, idx, lane);
-    if (kStep == 1) seen_step(p, idx, lane);
-    if (kStep == 2) order_step(p, idx, lane);
+    if (kStep == 1) seen_step(p, p.tiles, idx, lane);
+    if (kStep == 2) order_step(p, p.tiles, p.seen, idx, lane);
 }
 
 int mask_launch(const basp_plan *pl, MaskParams &p, void *mask, cudaStream_t st) {
