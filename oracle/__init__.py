@@ -632,7 +632,8 @@ def attn_shaped(q, k, v, begin, end, cap: float = 0.0, slopes=None, scale: float
         if given is not None:
             O = given[0][:, h]
             p = np.where(see & any_key[:, None], np.exp(z - np.where(any_key, given[1][h], 0.0)[:, None]), 0.0)
-        slope = scale * (1.0 - t * t)
+        with np.errstate(over="ignore"):
+            slope = scale / np.cosh(s / cap) ** 2 if cap else np.full_like(s, scale)        # 1 - tanh^2 without the difference
         ds = p * (do[:, h] @ V.T - (do[:, h] * O).sum(1)[:, None]) * slope
         out["dq"][:, h] = ds @ K
         out["mag_dq"][:, h] = np.abs(ds) @ np.abs(K)

@@ -196,17 +196,19 @@ __device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t to, co
                     off = fma2(off, minus2, add2(ramp[h], block));
                 } else off = mul2(off, minus2);
                 const uint64_t s2 = pack_f2(__uint_as_float(st[i]), __uint_as_float(st[i + 1]));
-                [[maybe_unused]] uint64_t capped = 0;
+                [[maybe_unused]] uint64_t slope2 = 0;          // the cap's derivative
                 uint64_t z;
                 if constexpr (!kCap) {
                     z = fma2(s2, both(scale_log2), off);
                 } else if constexpr (kFar) {
-                    capped = pack_f2(tanh_far(__uint_as_float(st[i]) * a.cap_in) * a.cap_out, tanh_far(__uint_as_float(st[i + 1]) * a.cap_in) * a.cap_out);
-                    z = add2(capped, off);
+                    float g0, g1;
+                    const float c0 = capped_far(__uint_as_float(st[i]), a, &g0), c1 = capped_far(__uint_as_float(st[i + 1]), a, &g1);
+                    z = add2(pack_f2(c0, c1), off);
+                    slope2 = pack_f2(g0, g1);
                 } else {
-                    const uint64_t q = cap_near_q(mul2(s2, s2), a);
-                    capped = mul2(s2, q);
+                    const uint64_t q = cap_near_q(mul2(s2, s2), a), capped = mul2(s2, q);
                     z = fma2(s2, q, off);
+                    slope2 = fma2(mul2(capped, capped), shrink, both(1.f));
                 }
                 float z0, z1;
                 unpack_f2(z, z0, z1);
@@ -223,7 +225,7 @@ __device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t to, co
                     if (!(row >= (int)((w >> 16) & 0xff) && row < (int)(w >> 24))) p1 = 0.f;
                 }
                 pk[(i >> 1) & 7] = pack_bf16x2(p0, p1);
-                if constexpr (kCap) unpack_f2(mul2(pack_f2(p0, p1), fma2(mul2(capped, capped), shrink, both(1.f))), p0, p1);
+                if constexpr (kCap) unpack_f2(mul2(pack_f2(p0, p1), slope2), p0, p1);
                 st[i] = __float_as_uint(p0);
                 st[i + 1] = __float_as_uint(p1);
             }

@@ -26,11 +26,21 @@ __device__ __forceinline__ float rcp_approx(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// tanh of any x.  The bound keeps exp(2x) finite; a NaN passes.
-__device__ __forceinline__ float tanh_far(float x) {
-    float w = x * 2.8853900817779268f;
-    w = w > 64.f ? 64.f : w;
-    return fmaf(-2.f, rcp_approx(exp2_approx(w) + 1.f), 1.f);
+// c tanh(s / c) in log2 units for any raw score, to some 2^-23 of the cap, and the cap's derivative 1 - tanh^2 = 4 e r^2 with e = exp(2x),
+// r = 1 / (e + 1): no difference of two near numbers where the cap is reached.  The bound keeps e finite; a NaN passes.
+__device__ __forceinline__ float capped_far(float s, const ScoreArgs &a, float *derivative) {
+    float w = s * a.cap_in * 2.8853900817779268f;
+    w = w > 120.f ? 120.f : w;
+    const float e = exp2_approx(w), r = rcp_approx(e + 1.f);
+    *derivative = 4.f * (e * r) * r;
+    return fmaf(-2.f * a.cap_out, r, a.cap_out);
+}
+// The same to 2^-22 of its own value: a score that is small against the cap by the polynomial
+__device__ __forceinline__ float capped_any(float s, const ScoreArgs &a) {
+    float derivative;
+    const float far = capped_far(s, a, &derivative);
+    const float y = s * s, near = s * fmaf(fmaf(fmaf(a.near[3], y, a.near[2]), y, a.near[1]), y, a.near[0]);
+    return fabsf(s) <= a.near_limit ? near : far;
 }
 
 // Raw scores of a query row against neighbouring keys brought to log2 units in place, by the formulas that hold everywhere: where the cap
@@ -41,7 +51,7 @@ __device__ __forceinline__ void shape_scores(uint32_t (&s)[kCount], const ScoreA
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
         float z = __uint_as_float(s[i]);
-        z = kCap ? tanh_far(z * a.cap_in) * a.cap_out : z * scale_log2;
+        z = kCap ? capped_any(z, a) : z * scale_log2;
         if constexpr (kBias) z = fmaf(-slope, fabsf(d0 - (float)i), z);
         s[i] = __float_as_uint(z);
     }

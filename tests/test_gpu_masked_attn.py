@@ -8,7 +8,11 @@ an absolute error of a few 2^-23: with m the largest sum of magnitudes scale |q|
   dV   as O, with its own magnitudes
   dQ   dS rounded to bf16 (2^-8 of each term), its P (2 dz), an absolute error of dO.v - dO.O of 2^-16 of the sums of magnitudes of
        D products in every row's share, the result rounded (2^-8), the sum of fp32 terms in any order 2^-18 of the magnitudes
-  dK   as dQ"""
+  dK   as dQ
+and 1e-30 besides, which nothing of these magnitudes is told from zero by (a saturated cap has a derivative of zero in fp64 and 2^-118 in
+fp32).  The cap's derivative 1 - tanh^2(s / c) is good to 2^-20 of itself at the score it is given (four roundings and two approximations of
+2^-22), within dQ's 2^-18; its logarithm changes by at most 2 / c for each unit of the score, so the score's own error ds (dz without
+the cap's part) moves it by up to exp(2 ds / c) - 1 of itself, which is what counts for a cap of 1e-4."""
 import numpy as np
 import pytest
 import torch
@@ -32,9 +36,9 @@ SHAPES = {
     "replicated kv": W(N=4, B=1, S=300, Hq=8, Hkv=2, D=96),
     "many ranks": W(N=16, B=4, S=260, Hq=8, Hkv=4, D=32),
 }
-KINDS = ["causal", "docs", "prefix", "window", "ranges", "all", "nothing"]
+KINDS = ["causal", "plan without a mask", "docs", "prefix", "window", "ranges", "all", "nothing"]
 SHAPING = {"plain": (0.0, False), "cap": (30.0, False), "tight cap": (1.5, False), "wide cap": (200.0, False), "bias": (0.0, True),
-           "cap bias": (20.0, True), "wide cap bias": (120.0, True)}
+           "cap bias": (20.0, True), "wide cap bias": (120.0, True), "tiny cap": (1e-4, False), "huge cap": (1e6, False)}
 
 
 def documents(rng, B, S, pad):
@@ -56,6 +60,8 @@ def mask_of(basp, pl, kind, rng):
     at = np.tile(np.arange(S), (B, 1))
     if kind == "causal":
         return None, 0 * at, at + 1
+    if kind == "plan without a mask":
+        return None, 0 * at, 0 * at + S
     mask = torch.full((basp.basp_mask_bytes(pl) + 32,), 255, dtype=torch.uint8, device="cuda")
     cu = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
     if kind in ("docs", "prefix", "window"):
@@ -95,7 +101,7 @@ def f64(t):
 def run(basp, w, kind, shaping, seed=0, backward=True, spread=1.0):
     rng = np.random.default_rng(seed + w.S)
     cap, bias = SHAPING[shaping]
-    pl = make_plan(basp, w, causal=kind not in ("all",))
+    pl = make_plan(basp, w, causal=kind not in ("all", "plan without a mask"))
     g = torch.Generator().manual_seed(seed)
     mk = lambda h: (spread * torch.randn((w.B, w.S, h, w.D), generator=g) * torch.exp(0.3 * torch.randn((h, 1), generator=g))).to(torch.bfloat16)
     q, k, v, do = mk(w.Hq), mk(w.Hkv), mk(w.Hkv), mk(w.Hq)
@@ -159,8 +165,9 @@ def check(w, pl, refs, o, lse, grads, info):
                 continue
             b = g * pl.Bl + bl
             G = H // w.Hkv
+            bend = np.expm1(2 * (w.D / 8 + 4) * 2.0 ** -23 * ref["top"] / cap) if cap else 0.0
             dots = 2.0 ** -16 * np.einsum("shd,shd->s", np.abs(f64(do[b])), np.abs(f64(v[b])).repeat(G, 1).max(0)[None] + np.abs(ref["o"])).max()
-            unit = lambda n: (2.0 ** -8 + 2 * p + 2.0 ** -18) * ref["mag_" + n] + dots * ref["row_" + n] + 2.0 ** -8 * np.abs(ref[n])
+            unit = lambda n: (2.0 ** -8 + 2 * p + 2.0 ** -18 + bend) * ref["mag_" + n] + dots * ref["row_" + n] + 2.0 ** -8 * np.abs(ref[n]) + 1e-30
             close(f64(grads[0][r][bl]), ref["dq"][:, hq], unit("dq")[:, hq], (r, bl, "dq"))
             # a rank with a shared KV head holds its own query heads' part: summed over the sharing ranks
             if w.Hkv < pl.K:
