@@ -18,7 +18,7 @@
 // Warps: 16 compute (a quarter of the score columns each), 4 dQ drain, TMA producer, MMA issuer.
 // Three kernels share this file's parameter block, work-item order and barriers: attn_bwd_d128.cuh (head dimensions
 // 80 .. 128), attn_bwd_d64.cuh (16 .. 64) and the two-pass form attn_bwd_2pass.cuh; each header says how it orders
-// the steps.  Helper kernels here: Delta = rowsum(dO * O); fp32 dQ accumulator -> bf16.
+// the steps.  The helper kernels around the products are in attn_bwd_common.cuh.
 #include <cuda.h>
 #include <math.h>
 

@@ -212,11 +212,12 @@ int basp_score_args(const basp_plan *p, const basp_score *score, float scale, Sc
         if (!(in >= 1e-9 && in <= 1e6 && score->softcap >= 1e-12f && score->softcap <= 1e12f)) return BASP_ERR_INVALID;
         out->cap_in = (float)in;
         out->cap_out = (float)(score->softcap * log2e);
-        const double c[4] = {0.99999988, -0.33331361, 0.13270971, -0.047553331};
+        const double c[5] = {0.999999846, -0.333315002, 0.132978737, -0.0515179165, 0.0146250855};
         double power = scale * log2e;                       // softcap log2(e) in^(2k + 1)
-        for (int k = 0; k < 4; ++k, power *= in * in) out->near[k] = (float)(c[k] * power);
-        // the powers have to be fp32 numbers: below 1e-6 the last one is not, and is not needed up to 0.05; above 1e3 they overflow
-        out->near_limit = in > 1e3 ? -1.f : (float)((in < 1e-6 ? 0.05 : 0.4) / in);
+        for (int k = 0; k < 5; ++k, power *= in * in) out->near[k] = (float)(c[k] * power);
+        // the coefficients have to be normal fp32 numbers: where the last one is not, it and the one before are not needed up to 0.05; for
+        // in above 1e3 they overflow
+        out->near_limit = in > 1e3 ? -1.f : (float)((out->near[4] < 1.2e-38f ? 0.05 : 0.65) / in);
     }
     if ((uintptr_t)score->slopes & 3) return BASP_ERR_ALIGN;
     out->slopes = score->slopes;

@@ -47,7 +47,7 @@ struct ScoreArgs {
     const MaskBwdEntry *bwd;
     const float *slopes;            // [Hq]
     float cap_in, cap_out;          // scale / softcap and softcap * log2(e); 0: no cap
-    float near[4], near_limit;      // coefficients of the capped score near zero (score.cuh), and up to which raw score
+    float near[5], near_limit;      // coefficients of the capped score near zero (score.cuh), and up to which raw score
     int B;
 };
 

@@ -123,7 +123,9 @@ __device__ __forceinline__ MbStats fetch_stats(const MaskedBwdParams<R> &p, cons
     }
     return s;
 }
-// To shared memory: LSE in log2 units, -Delta times the scale, the windows as lo | hi << 8, and whether the windows are to be looked at.
+// To shared memory: LSE in log2 units, -Delta times the scale, the windows, and whether the windows are to be looked at (bit 0 of edge).  A
+// window is lo | hi << 8 in keys of the tile, both 0 where there are none, with bit 7 where the query sees one key in all (bit 1 + g of edge:
+// one of queries 32 g .. + 31 does).
 template <int R>
 __device__ __forceinline__ void stage_stats(const MaskedBwdParams<R> &p, const MbItem &it, int m, int lane, const MbStats &s, float *lse,
                                             float *delta, uint16_t *win, int *edge) {
@@ -146,10 +148,18 @@ __device__ __forceinline__ void stage_stats(const MaskedBwdParams<R> &p, const M
         }
     }
     uint32_t w[4];
+    bool single = false;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)min(max(lo[e] - k0, 0), kT) | (uint32_t)min(max(hi[e] - k0, 0), kT) << 8;
+    for (int e = 0; e < 4; ++e) {
+        const int first = max(lo[e] - k0, 0), past = min(hi[e] - k0, kT);
+        const bool one = first < past && hi[e] - lo[e] == 1;
+        w[e] = first < past ? (uint32_t)(first | past << 8 | (one ? 0x80 : 0)) : 0u;
+        single = single || one;
+    }
     *reinterpret_cast<uint2 *>(win + 4 * lane) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-    if (lane == 0) *edge = look;
+    const uint32_t singles = __ballot_sync(0xffffffffu, single);
+    if (lane == 0)
+        *edge = look | (singles & 0xff ? 2 : 0) | (singles & 0xff00 ? 4 : 0) | (singles & 0xff0000 ? 8 : 0) | (singles & 0xff000000u ? 16 : 0);
 }
 
 // Thirty-two scores of a key row (queries side by side): the probabilities as bf16 to the tensor memory at `to`, sixteen at a time, and
@@ -221,10 +231,15 @@ __device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t to, co
                 float p0 = exp2_approx(z0), p1 = exp2_approx(z1);
                 if constexpr (kEdge) {
                     const uint32_t w = h ? w4.y : w4.x;
-                    if (!(row >= (int)(w & 0xff) && row < (int)((w >> 8) & 0xff))) p0 = 0.f;
-                    if (!(row >= (int)((w >> 16) & 0xff) && row < (int)(w >> 24))) p1 = 0.f;
+                    if (!(row >= (int)(w & 0x7f) && row < (int)((w >> 8) & 0xff))) p0 = 0.f;
+                    if (!(row >= (int)((w >> 16) & 0x7f) && row < (int)(w >> 24))) p1 = 0.f;
                 }
                 pk[(i >> 1) & 7] = pack_bf16x2(p0, p1);
+                if constexpr (kBias && kEdge) {       // drop_singles, without a loop of its own
+                    const uint32_t w = h ? w4.y : w4.x;
+                    if (w & 0x80) p0 = 0.f;
+                    if (w & 0x800000) p1 = 0.f;
+                }
                 if constexpr (kCap) unpack_f2(mul2(pack_f2(p0, p1), slope2), p0, p1);
                 st[i] = __float_as_uint(p0);
                 st[i + 1] = __float_as_uint(p1);
@@ -237,6 +252,18 @@ __device__ __forceinline__ void shaped_probs(uint32_t (&st)[32], uint32_t to, co
         else columns(std::false_type{});
     } else {
         columns(std::false_type{});
+    }
+}
+
+// A query that sees one key has P = 1 whatever the score: dS is 0, where the difference of dO.v and Delta would leave their roundings.  A
+// loop of its own, as hardly any tile has such a query (inside the scores' loop packed documents trained 3 % slower); but beside a bias, where
+// that loop is the longest, one loop more does not fit the instruction cache (16K tokens: 5.90 ms, against 5.66 inside).
+__device__ __forceinline__ void drop_singles(uint32_t (&st)[32], const uint16_t *win) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(win + i);
+        if (w & 0x80) st[i] = 0;
+        if (w & 0x800000) st[i + 1] = 0;
     }
 }
 
@@ -354,7 +381,8 @@ __global__ void __launch_bounds__(256) mb_finish_kernel(const __grid_constant__ 
 
 // Query heads of a key head that one work item takes.  All of them keep dK and dV in the tensor memory; but where the items are few, the
 // longest one (a key tile that all query tiles see) is much of the whole: they are divided until it is below 0.6 of an SM's share, and the
-// parts of dK and dV are added up behind (3001 tokens, 12/4 heads of 64, capped and biased: XX).
+// parts of dK and dV are added up behind (3001 tokens, 12/4 heads of 64, capped and biased: 185 us,
+// 160 with the work divided).
 int mb_part_heads(const basp_plan *p) {
     const int q_per_kv = p->Hq_l / p->Hkv_l;
     const double n = (p->S + kT - 1) / kT, pairs = p->causal ? n * (n + 1) / 2 : n * n;

@@ -85,10 +85,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_masked_bwd_d128_kernel(co
                     // derivative of the cap
                     {
                         const int dist = (m - item.n) * kT + 32 * g - row;      // position of the first column's query minus the key's
-                        if (s_edge[stage] || (kBias && m == item.n))
+                        const int edge = s_edge[stage];
+                        if (edge || (kBias && m == item.n))
                             shaped_probs<kCap, kBias, true>(st, st_col, lse_b, s_win + stage * kT + 32 * g, row, p.score, p.scale_log2, slope, dist, m - item.n);
                         else
                             shaped_probs<kCap, kBias, false>(st, st_col, lse_b, nullptr, row, p.score, p.scale_log2, slope, dist, m - item.n);
+                        if (!kBias && __builtin_expect(edge & 2 << g, 0)) drop_singles(st, s_win + stage * kT + 32 * g);
                     }
                     tmem_wait_st();
                     tc_fence_before();

@@ -265,7 +265,8 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.p_full[t]);
             }
-            sh.l[ep_cnt & 1][t][row] = l_run;
+            // one key: P is a rounded number that the sum below it has to be too, so that O is the key's value
+            sh.l[ep_cnt & 1][t][row] = hi - lo == 1 ? round_bf16(l_run) : l_run;
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.l_full[t][ep_cnt & 1]);
             ++ep_cnt;

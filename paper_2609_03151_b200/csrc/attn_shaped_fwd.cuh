@@ -14,8 +14,8 @@
 //   warps  0-15  softmax of query tile warp / 8, columns 64 (warp / 4 % 2) .. + 63 of its rows, and the epilogue of as many columns of O
 //   warp  16     TMA producer, 17 and 18 MMA issuers (S = Q K^T, O += P V), as in the plain kernel
 // TMEM: S | P_0 P_1 | O_0 | O_1 as there.  Registers: 104 a thread for the softmax, 56 for the rest, of the 96 that all are launched with.
-// 16K causal tokens, 32/8 heads of 128 (plain scores 1.55-1.7 ms): cap 50 1.97 ms, a bias 2.08, both 2.15; with two warpgroups 2.49, 2.32 and
-// 2.62.
+// 16K causal tokens, 32/8 heads of 128 (plain scores 1.55-1.7 ms): cap 50 2.05 ms, a bias 2.3, both 2.3, a cap that most tiles reach 3.3; with two
+// warpgroups cap 50 2.49 ms (then with a polynomial of four terms; four warpgroups 1.97).
 #pragma once
 
 constexpr int kSfThreads = 640;
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kSfThreads, 1) attn_shaped_fwd_kernel(const __
             if (lane == 0) mbar_arrive(&sh.l_full[t]);
             SF_WAIT(&sh.l_full[t], ep_cnt & 1, 16 + t, 0);
             const float l = sh.l[ep_cnt & 1][t][0][row] + sh.l[ep_cnt & 1][t][1][row];
-            const float inv_l = l == 0.f ? 0.f : 1.f / l;               // a row without a key: P was zero throughout
+            const float inv_l = l == 0.f ? 0.f : 1.f / (hi - lo == 1 ? round_bf16(l) : l);  // no key: P was zero throughout; one key: as there
             if (half == 0 && p.has_lse && in_seq)
                 p.lse[item.r][((size_t)item.bl * p.Hq_l + item.h) * p.S + s_pos] = l == 0.f ? -INFINITY : ref * 0.6931471805599453f + logf(l);
             SF_WAIT(&sh.o_final[t], ep_cnt & 1, 18 + t, 0);

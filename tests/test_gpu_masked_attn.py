@@ -290,3 +290,32 @@ def test_past_two_billion_elements(basp):
     assert (o[:, -n:].float() - o2.float()).abs().max().item() <= 2.0 ** -7 * v[:, -n:].float().abs().max().item()
     assert (lse[..., -n:] - lse2).abs().max().item() <= 1e-5
     assert torch.allclose(lse[0, :, 5], torch.log(torch.tensor(6.0)).cuda().expand(H), atol=1e-5)      # zero queries: a mean over the keys
+
+
+@pytest.mark.parametrize("shaping", ["plain", "cap", "wide cap", "bias", "cap bias"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_that_see_one_key(basp, D, shaping):
+    """P is 1 there whatever the score: O is the key's value and no gradient reaches Q and K, to the bit; dV is dO, rounded once."""
+    S, H = 300, 2
+    cap, bias = SHAPING[shaping]
+    pl = make_plan(basp, W(N=1, B=1, S=S, Hq=H, Hkv=H, D=D))
+    g = torch.Generator().manual_seed(D)
+    q, k, v, do = ([torch.randn((1, S, H, D), generator=g).to(torch.bfloat16).cuda()] for _ in range(4))
+    mask = torch.empty(basp.basp_mask_bytes(pl), dtype=torch.uint8, device="cuda")
+    slopes = torch.tensor([0.5, 0.01], device="cuda") if bias else None
+    o, dq, dk, dv = ([torch.full_like(t[0], float("nan"))] for t in (q, q, k, v))
+    lse = [torch.empty((1, H, S), device="cuda")]
+    ws = torch.empty(basp.basp_attn_masked_bwd_workspace_bytes(pl), dtype=torch.uint8, device="cuda")
+    one = torch.arange(S, dtype=torch.int32)
+    # documents of one token; a window of one; a first row of its own and whole documents behind it
+    for pos, window in ((0 * one, 0), (one, 1), (one % 150, 0)):
+        basp.basp_mask_packed(pl, pos.reshape(1, S).cuda(), mask, None, window)
+        sc = basp.basp_score(softcap=cap, slopes=slopes, mask=mask)
+        basp.basp_attn_masked_fwd(pl, sc, q, k, v, o, lse)
+        basp.basp_attn_masked_bwd(pl, sc, q, k, v, o, do, lse, dq, dk, dv, ws)
+        alone = torch.ones(S, dtype=torch.bool) if window or not pos.any() else pos == 0
+        assert torch.equal(o[0][0, alone], v[0][0, alone])
+        assert (dq[0][0, alone] == 0).all()
+        if alone.all():
+            assert (dk[0] == 0).all() and torch.equal(dv[0], do[0])
+    assert basp.basp_get_status() == [0, 0, 0, 0]
