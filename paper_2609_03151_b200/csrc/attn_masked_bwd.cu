@@ -1,6 +1,6 @@
 // Backward of the attention with masked and shaped scores (attn_masked_fwd.cu) over each virtual rank's head slice:
 //
-//   P_ij = exp(z_ij - LSE_i) on visible pairs,  Delta_i = dO_i.O_i,  dV_j = sum_i P_ij dO_i,
+//   P_ij = exp(z_ij - LSE_i) on visible pairs,  Delta_i = dO_i.O_i (= sum_j P_ij dO_i.v_j),  dV_j = sum_i P_ij dO_i,
 //   dZ_ij = P_ij (dO_i.v_j - Delta_i),  dS_ij = scale (1 - tanh^2(scale q_i.k_j / c)) dZ_ij,  dQ_i = sum_j dS_ij k_j,  dK_j = sum_i dS_ij q_i
 //
 // The kernels are those of attn_bwd.cu (five products per tile pair on tcgen05, dK and dV resident in TMEM, dQ added to an fp32
@@ -307,35 +307,100 @@ __device__ __forceinline__ void store_zeros(const MaskedBwdParams<R> &p, const M
 #include "attn_masked_bwd_d64.cuh"
 #include "attn_masked_bwd_d128.cuh"
 
-// In front of the products: Delta[bl][h][s] = sum_d O[bl][s][h][d] dO[bl][s][h][d] (16 lanes a row), and the dQ accumulator set to zero.
+// In front of the products: Delta[bl][h][s] of every row (16 lanes a row, eight features a lane), and the dQ accumulator set to zero.
+//
+// Delta is dO.O, but O comes rounded to bf16 and from rounded P: an error of some 2^-9 |dO||O| against dO.v - Delta, which is of the size
+// |dO||v|.  O is smaller by the root of the number of keys that count, so that it does not matter for long rows; with two to six keys
+// it put dQ and dK off by 1 % (2-norm).  Rows of up to kExactKeys keys therefore take Delta = sum_j P_ij dO_i.v_j from the scores, in fp32.
 // One launch for every rank: blockIdx.y = rank.
+constexpr int kExactKeys = 32;
+constexpr int kKeysAtOnce = 4;       // keys in flight: 128 bytes a lane
+
 template <int R>
-__global__ void __launch_bounds__(256) mb_prepare_kernel(const __grid_constant__ BwdHelperPtrs<R> hp, int S, int H, int D, long long rows, int zero) {
-    const int part = threadIdx.x % 16;
-    const long long row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
-    const bool mine = row < rows && part * 8 < D;
-    allow_next_kernel();
+struct PrepareParams {
+    const __nv_bfloat16 *q[R], *k[R], *v[R], *o[R], *dout[R];
+    const float *lse[R];
+    float *delta[R], *acc[R];
+    ScoreArgs score;
+    int K, Bl, S, H, Hkv, D, causal, n_tiles, zero;
+    float scale_log2;
+    long long rows;
+    FastDiv div_h, div_s, div_q_per_kv;
+};
+
+__device__ __forceinline__ float dot8(const uint4 &a, const uint4 &b) {
+    const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
     float acc = 0.f;
-    if (mine) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(hp.o[blockIdx.y] + row * D + part * 8);
-        const uint4 b = *reinterpret_cast<const uint4 *>(hp.dout[blockIdx.y] + row * D + part * 8);
-        const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            acc += __uint_as_float(av[i] << 16) * __uint_as_float(bv[i] << 16);
-            acc += __uint_as_float(av[i] & 0xffff0000u) * __uint_as_float(bv[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+        acc = fmaf(__uint_as_float(av[i] << 16), __uint_as_float(bv[i] << 16), acc);
+        acc = fmaf(__uint_as_float(av[i] & 0xffff0000u), __uint_as_float(bv[i] & 0xffff0000u), acc);
+    }
+    return acc;
+}
+
+template <int R>
+__global__ void __launch_bounds__(256) mb_prepare_kernel(const __grid_constant__ PrepareParams<R> p) {
+    const int part = threadIdx.x % 16, r = blockIdx.y;
+    const uint32_t group = 0xffffu << (threadIdx.x & 16);        // the lanes of this row
+    const long long row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
+    allow_next_kernel();
+    if (row >= p.rows) return;                                   // (all lanes of the row)
+    const bool mine = part * 8 < p.D;
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    const size_t at = (size_t)row * p.D + part * 8;
+    const uint4 up = mine ? *reinterpret_cast<const uint4 *>(p.dout[r] + at) : none;
+    const uint4 o = mine ? *reinterpret_cast<const uint4 *>(p.o[r] + at) : none;
+    if (p.zero && mine) {
+        float4 *to = reinterpret_cast<float4 *>(p.acc[r] + at);
+        to[0] = to[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    const long long sb = p.rows <= 0x7fffffffll ? (long long)fdiv((uint32_t)row, p.div_h) : row / p.H;
+    const int h = (int)(row - sb * p.H), bl = (int)fdiv((uint32_t)sb, p.div_s), s = (int)sb - bl * p.S;
+    int lo = 0, hi = p.causal ? s + 1 : p.S;
+    if (p.score.range) {
+        const int2 range = __ldg(p.score.range + ((size_t)(r / p.K * p.Bl + bl) * p.n_tiles * kT + s));
+        lo = range.x;
+        hi = range.y;
+    }
+    float *delta = p.delta[r] + ((size_t)bl * p.H + h) * p.S + s;
+    if (hi - lo > kExactKeys) {
+        float acc = dot8(o, up);
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) acc += __shfl_xor_sync(group, acc, off);
+        if (part == 0) *delta = acc;
+        return;
+    }
+    const uint4 q = mine ? *reinterpret_cast<const uint4 *>(p.q[r] + at) : none;
+    const float lse = seen_lse(p.lse[r][((size_t)bl * p.H + h) * p.S + s]);
+    const float slope = p.score.slopes ? __ldg(p.score.slopes + r % p.K * p.H + h) * 1.4426950408889634f : 0.f;
+    const size_t step = (size_t)p.Hkv * p.D, first = ((size_t)bl * p.S * p.Hkv + (int)fdiv((uint32_t)h, p.div_q_per_kv)) * p.D + part * 8;
+    const bool upper = part & 8;
+    float sum = 0.f;                     // of the keys so far, in every lane
+#pragma unroll 1
+    for (int j = lo; j < hi; j += kKeysAtOnce) {
+        uint4 kk[kKeysAtOnce], vv[kKeysAtOnce];
+#pragma unroll
+        for (int i = 0; i < kKeysAtOnce; ++i) {
+            const bool there = mine && j + i < hi;
+            kk[i] = there ? *reinterpret_cast<const uint4 *>(p.k[r] + first + (j + i) * step) : none;
+            vv[i] = there ? *reinterpret_cast<const uint4 *>(p.v[r] + first + (j + i) * step) : none;
         }
-        if (zero) {
-            float4 *to = reinterpret_cast<float4 *>(const_cast<float *>(hp.acc[blockIdx.y]) + row * D + part * 8);
-            to[0] = to[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kKeysAtOnce; ++i) {
+            // q.k to the lower eight lanes, dO.v to the upper eight
+            const float a = dot8(q, kk[i]), b = dot8(up, vv[i]);
+            float mine2 = upper ? b : a;
+            mine2 += __shfl_xor_sync(group, upper ? a : b, 8);
+#pragma unroll
+            for (int off = 4; off > 0; off >>= 1) mine2 += __shfl_xor_sync(group, mine2, off);
+            const float other = __shfl_xor_sync(group, mine2, 8), raw = upper ? other : mine2, dp = upper ? mine2 : other;
+            float z = p.score.cap_out > 0.f ? capped_any(raw, p.score) : raw * p.scale_log2;
+            z -= slope * fabsf((float)(s - (j + i)));
+            if (j + i < hi) sum = fmaf(exp2_approx(z - lse), dp, sum);
         }
     }
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) acc += __shfl_down_sync(0xffffffffu, acc, off, 16);
-    if (mine && part == 0) {
-        const long long sb = row / H, h = row - sb * H, bl = sb / S, s = sb - bl * S;
-        hp.delta[blockIdx.y][(bl * H + h) * S + s] = acc;
-    }
+    if (part == 0) *delta = sum;
 }
 
 // Behind the products: dQ's accumulator to bf16 (n_q vectors of eight a rank) and the parts of dK and dV added up in order (n_kv vectors of
@@ -410,7 +475,7 @@ int mb_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
     BASP_TRY(basp_score_args(pl, score, scale, &prm.score));
     const uint64_t rows = (uint64_t)pl->Bl * pl->S;
     const size_t acc_b = bwd_acc_bytes(pl), del_b = bwd_delta_bytes(pl);
-    BwdHelperPtrs<R> hp;
+    PrepareParams<R> pre;
     FinishParams<R> fin;
     for (int r = 0; r < pl->N; ++r) {
         BASP_TRY(tmap::encode_rows_heads_d(&prm.q[r], q[r], rows, pl->Hq_l, pl->D, kT));
@@ -425,10 +490,14 @@ int mb_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
         prm.delta[r] = delta;
         prm.dk[r] = (__nv_bfloat16 *)dk[r];
         prm.dv[r] = (__nv_bfloat16 *)dv[r];
-        hp.o[r] = (const __nv_bfloat16 *)o[r];
-        hp.dout[r] = (const __nv_bfloat16 *)dout[r];
-        hp.delta[r] = delta;
-        hp.acc[r] = acc;
+        pre.q[r] = (const __nv_bfloat16 *)q[r];
+        pre.k[r] = (const __nv_bfloat16 *)k[r];
+        pre.v[r] = (const __nv_bfloat16 *)v[r];
+        pre.o[r] = (const __nv_bfloat16 *)o[r];
+        pre.dout[r] = (const __nv_bfloat16 *)dout[r];
+        pre.lse[r] = lse[r];
+        pre.delta[r] = delta;
+        pre.acc[r] = acc;
         prm.dq[r] = (__nv_bfloat16 *)dq[r];
         fin.acc[r] = acc;
         fin.dq[r] = (__nv_bfloat16 *)dq[r];
@@ -466,7 +535,17 @@ int mb_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
     BASP_TRY(sm_count(&sms));
     const int grid = (int)(total < sms ? total : sms);
 
-    mb_prepare_kernel<R><<<dim3((unsigned)((q_rows + 15) / 16), (unsigned)pl->N), 256, 0, st>>>(hp, pl->S, pl->Hq_l, pl->D, q_rows, !prm.direct);
+    pre.score = prm.score;
+    pre.K = pl->K; pre.Bl = pl->Bl; pre.S = pl->S; pre.H = pl->Hq_l; pre.Hkv = pl->Hkv_l; pre.D = pl->D;
+    pre.causal = pl->causal;
+    pre.n_tiles = prm.n_tiles;
+    pre.zero = !prm.direct;
+    pre.scale_log2 = prm.scale_log2;
+    pre.rows = q_rows;
+    pre.div_h = make_fastdiv((uint32_t)pl->Hq_l);
+    pre.div_s = make_fastdiv((uint32_t)pl->S);
+    pre.div_q_per_kv = make_fastdiv((uint32_t)prm.q_per_kv);
+    mb_prepare_kernel<R><<<dim3((unsigned)((q_rows + 15) / 16), (unsigned)pl->N), 256, 0, st>>>(pre);
     BASP_CUDA_TRY(cudaGetLastError());
     BASP_TRY(dispatch_score(prm.score.cap_out > 0.f, prm.score.slopes != nullptr, [&](auto cap, auto bias) -> int {
         constexpr bool kCap = decltype(cap)::value, kBias = decltype(bias)::value;

@@ -8,7 +8,7 @@ an absolute error of a few 2^-23: with m the largest sum of magnitudes scale |q|
   dV   as O, with its own magnitudes
   dQ   dS rounded to bf16 (2^-8 of each term), its P (2 dz), an absolute error of dO.v - dO.O of 2^-16 of the sums of magnitudes of
        D products in every row's share, the result rounded (2^-8), the sum of fp32 terms in any order 2^-18 of the magnitudes
-  dK   as dQ
+  dK   as dQ; in rows of up to 32 keys Delta is summed from P that are 2 dz off themselves, which adds as much of the sum of magnitudes
 and 1e-30 besides, which nothing of these magnitudes is told from zero by (a saturated cap has a derivative of zero in fp64 and 2^-118 in
 fp32).  The cap's derivative 1 - tanh^2(s / c) is good to 2^-20 of itself at the score it is given (four roundings and two approximations of
 2^-22), within dQ's 2^-18; its logarithm changes by at most 2 / c for each unit of the score, so the score's own error ds (dz without
@@ -121,9 +121,11 @@ def run(basp, w, kind, shaping, seed=0, backward=True, spread=1.0):
     ref = [[None] * w.B for _ in range(2)]
     refs = [oracle.attn_shaped(f64(q[b]), f64(k[b]), f64(v[b]), begin[b], end[b], cap, None if slopes is None else slopes.double().numpy())
             for b in range(w.B)]
-    # the backward pass by itself: at the oracle's O and LSE
+    # the backward pass by itself: at the oracle's O and LSE (the O of rows of up to 32 keys is not used: Delta is the sum of P dO.v there,
+    # which is dO.O of the unrounded O)
     if backward:
         O = torch.from_numpy(np.stack([r["o"] for r in refs])).to(torch.bfloat16)
+        short = (end - begin <= 32)[..., None, None]
         L = torch.from_numpy(np.stack([r["lse"] for r in refs])).float()
         o_in = head_shards(O, pl, w.Hq, 1)
         l_in = [L[r // pl.K * pl.Bl:(r // pl.K + 1) * pl.Bl, r % pl.K * pl.Hq_l:(r % pl.K + 1) * pl.Hq_l].contiguous().cuda() for r in range(pl.N)]
@@ -133,7 +135,7 @@ def run(basp, w, kind, shaping, seed=0, backward=True, spread=1.0):
         basp.basp_get_status()
         refs = [{**r, **{n: t for n, t in oracle.attn_shaped(f64(q[b]), f64(k[b]), f64(v[b]), begin[b], end[b], cap,
                                                               None if slopes is None else slopes.double().numpy(), do=f64(do[b]),
-                                                              given=(f64(O[b]), L[b].double().numpy())).items() if n not in ("o", "lse", "mag_o")}}
+                                                              given=(np.where(short[b], r["o"], f64(O[b])), L[b].double().numpy())).items() if n not in ("o", "lse", "mag_o")}}
                 for b, r in enumerate(refs)]
     return pl, refs, o, lse, grads, (cap, 0.0 if slopes is None else float(slopes.max()), (q, k, v, do))
 
@@ -166,7 +168,7 @@ def check(w, pl, refs, o, lse, grads, info):
             b = g * pl.Bl + bl
             G = H // w.Hkv
             bend = np.expm1(2 * (w.D / 8 + 4) * 2.0 ** -23 * ref["top"] / cap) if cap else 0.0
-            dots = 2.0 ** -16 * np.einsum("shd,shd->s", np.abs(f64(do[b])), np.abs(f64(v[b])).repeat(G, 1).max(0)[None] + np.abs(ref["o"])).max()
+            dots = (2.0 ** -16 + p) * np.einsum("shd,shd->s", np.abs(f64(do[b])), np.abs(f64(v[b])).repeat(G, 1).max(0)[None] + np.abs(ref["o"])).max()
             unit = lambda n: (2.0 ** -8 + 2 * p + 2.0 ** -18 + bend) * ref["mag_" + n] + dots * ref["row_" + n] + 2.0 ** -8 * np.abs(ref[n]) + 1e-30
             close(f64(grads[0][r][bl]), ref["dq"][:, hq], unit("dq")[:, hq], (r, bl, "dq"))
             # a rank with a shared KV head holds its own query heads' part: summed over the sharing ranks
@@ -319,3 +321,30 @@ def test_queries_that_see_one_key(basp, D, shaping):
         if alone.all():
             assert (dk[0] == 0).all() and torch.equal(dv[0], do[0])
     assert basp.basp_get_status() == [0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("kind", ["two tokens", "window", "documents"])
+@pytest.mark.parametrize("D", [16, 64, 128])
+def test_gradients_of_rows_with_few_keys(basp, D, kind):
+    """Forward and backward in a row, where dO.v - Delta is small against the roundings of O: the result's 2-norm is off by the roundings of
+    dS and of the result, 2^-9 rms each at most, and by those of P (2^-9 of each term of Delta) in no row."""
+    S, H = (2 if kind == "two tokens" else 300), 8
+    pl = make_plan(basp, W(N=1, B=1, S=S, Hq=H, Hkv=H, D=D))
+    g = torch.Generator().manual_seed(D)
+    q, k, v, do = ([torch.randn((1, S, H, D), generator=g).to(torch.bfloat16).cuda()] for _ in range(4))
+    pos = np.arange(S, dtype=np.int32)[None] % (5 if kind == "documents" else S)
+    window = 3 if kind == "window" else 0
+    mask = torch.empty(basp.basp_mask_bytes(pl), dtype=torch.uint8, device="cuda")
+    basp.basp_mask_packed(pl, torch.from_numpy(pos).cuda(), mask, None, window)
+    begin, end = oracle.packed_ranges(pos, None, window)
+    for cap, slopes in ((0.0, None), (20.0, torch.linspace(0.01, 0.5, H))):
+        sc = basp.basp_score(softcap=cap, slopes=None if slopes is None else slopes.cuda(), mask=mask)
+        o, dq, dk, dv = ([torch.full_like(t[0], float("nan"))] for t in (q, q, k, v))
+        lse = [torch.empty((1, H, S), device="cuda")]
+        ws = torch.empty(basp.basp_attn_masked_bwd_workspace_bytes(pl), dtype=torch.uint8, device="cuda")
+        basp.basp_attn_masked_fwd(pl, sc, q, k, v, o, lse)
+        basp.basp_attn_masked_bwd(pl, sc, q, k, v, o, do, lse, dq, dk, dv, ws)
+        ref = oracle.attn_shaped(*(f64(t[0][0]) for t in (q, k, v)), begin[0], end[0], cap, None if slopes is None else slopes.double().numpy(),
+                                 do=f64(do[0][0]))
+        for got, n in ((dq, "dq"), (dk, "dk")):
+            assert np.linalg.norm(f64(got[0][0]) - ref[n]) <= 2.0 ** -8 * np.linalg.norm(ref[n]), (cap, n)
