@@ -452,7 +452,8 @@ size_t basp_lm_loss_grad_workspace_bytes(const basp_plan *plan, int hidden, int 
  * be finite numbers in hidden places and padding too.
  * The backward pass takes the forward's O and LSE:
  *   P = exp(z - LSE),  dV_j = sum_i P_ij dO_i,  dZ_ij = P_ij (dO_i.v_j - dO_i.O_i),  dS = scale (1 - tanh^2) dZ,  dQ = dS K,  dK = dS^T Q
- * (no gradient for the slopes); keys that nothing sees get zeros.  dQ is summed by floating-point atomics.  workspace:
+ * (no gradient for the slopes; queries of up to eight keys take sum_j P_ij dO_i.v_j in the place of dO_i.O_i, which is the same without O's
+ * rounding); keys that nothing sees get zeros.  dQ is summed by floating-point atomics.  workspace:
  * basp_attn_masked_bwd_workspace_bytes(plan). */
 typedef struct basp_score {
     float softcap;

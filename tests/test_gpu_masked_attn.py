@@ -8,7 +8,7 @@ an absolute error of a few 2^-23: with m the largest sum of magnitudes scale |q|
   dV   as O, with its own magnitudes
   dQ   dS rounded to bf16 (2^-8 of each term), its P (2 dz), an absolute error of dO.v - dO.O of 2^-16 of the sums of magnitudes of
        D products in every row's share, the result rounded (2^-8), the sum of fp32 terms in any order 2^-18 of the magnitudes
-  dK   as dQ; in rows of up to 32 keys Delta is summed from P that are 2 dz off themselves, which adds as much of the sum of magnitudes
+  dK   as dQ; in rows of up to eight keys Delta is summed from P that are 2 dz off themselves, which adds as much of the sum of magnitudes
 and 1e-30 besides, which nothing of these magnitudes is told from zero by (a saturated cap has a derivative of zero in fp64 and 2^-118 in
 fp32).  The cap's derivative 1 - tanh^2(s / c) is good to 2^-20 of itself at the score it is given (four roundings and two approximations of
 2^-22), within dQ's 2^-18; its logarithm changes by at most 2 / c for each unit of the score, so the score's own error ds (dz without
@@ -121,11 +121,11 @@ def run(basp, w, kind, shaping, seed=0, backward=True, spread=1.0):
     ref = [[None] * w.B for _ in range(2)]
     refs = [oracle.attn_shaped(f64(q[b]), f64(k[b]), f64(v[b]), begin[b], end[b], cap, None if slopes is None else slopes.double().numpy())
             for b in range(w.B)]
-    # the backward pass by itself: at the oracle's O and LSE (the O of rows of up to 32 keys is not used: Delta is the sum of P dO.v there,
+    # the backward pass by itself: at the oracle's O and LSE (the O of rows of up to eight keys is not used: Delta is the sum of P dO.v there,
     # which is dO.O of the unrounded O)
     if backward:
         O = torch.from_numpy(np.stack([r["o"] for r in refs])).to(torch.bfloat16)
-        short = (end - begin <= 32)[..., None, None]
+        short = (end - begin <= 8)[..., None, None]
         L = torch.from_numpy(np.stack([r["lse"] for r in refs])).float()
         o_in = head_shards(O, pl, w.Hq, 1)
         l_in = [L[r // pl.K * pl.Bl:(r // pl.K + 1) * pl.Bl, r % pl.K * pl.Hq_l:(r % pl.K + 1) * pl.Hq_l].contiguous().cuda() for r in range(pl.N)]
