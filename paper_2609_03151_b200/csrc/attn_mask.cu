@@ -7,7 +7,8 @@
 // Three steps, each over warps: a warp takes a query tile (its rows' ranges and their extremes), then a key tile (which query
 // tiles see it), then a work item (its place in the order, longest first, by counting the longer ones: the place does not depend
 // on timing).  Up to 64 tiles one block does all three, above that they are three launches that start early.  The tables are a
-// few kilobytes: what bounds the calls is latency (two sequences of 777 tokens: 14 tiles, one launch).
+// few kilobytes: what bounds the calls is latency (two sequences of 777 tokens: 14 tiles in
+// one launch, 4.3 us; in three launches 8.6).
 #include <type_traits>
 
 #include "attn_mask.cuh"

@@ -6,6 +6,8 @@
 // The kernels are those of attn_bwd.cu (five products per tile pair on tcgen05, dK and dV resident in TMEM, dQ added to an fp32
 // accumulator), walking the tile pairs of the mask object: a work item is a key tile and the query tiles that see some of it,
 // longest first.  A row without a key has LSE = -inf and takes no part; a key tile that nothing sees gets zeros.
+// 16K causal tokens, 32/8 heads of 128: plain 5.4-5.6 ms (1000 TFLOP/s, as the causal kernel), bias 5.7-5.9, cap 50 6.9-7.0, both 7.0; bound by the
+// reductions of dQ and, with a cap, by the shaping's issue and instruction fetch.
 #include <cuda.h>
 #include <math.h>
 
