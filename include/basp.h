@@ -530,7 +530,7 @@ int basp_rope(const basp_plan *plan, const basp_rope_turns *rope, const void *co
  * reaches h from elsewhere; NULL: none) and dn (NULL without w_pre), and writes dx = the gradient of h in all, which is x's, dy, and
  * the sums over all tokens dw_post, dgate, dw_pre (fp32 [hidden], written, not added to; NULL for what there is not).  y_seq NULL: no dy.
  * y may be NULL with a dy wanted where neither w_post nor gate is there (dy = res_scale dx).  dx_seq[r] may be dh_out[r] or dn[r] itself,
- * dy_seq[r] may be y_seq[r].  The same inputs give the same bits.
+ * dy_seq[r] may be y_seq[r].  Without any of the three weights the workspace is not touched (NULL will do).  The same inputs give the same bits.
  * fp32 arithmetic.  Requires hidden a multiple of 8 up to 16384, eps > 0 and res_scale finite. */
 int basp_block_norm(const basp_plan *plan, int hidden, const void *const *x_seq, const void *const *y_seq, const void *w_post,
                     const void *gate, const void *w_pre, float res_scale, float eps, void *const *h_seq, void *const *n_seq,

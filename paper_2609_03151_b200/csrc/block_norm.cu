@@ -38,7 +38,7 @@ struct NormParams {
     const __nv_bfloat16 *in[4][R];         // forward: x, y; backward: h, y, dh_out, dn
     __nv_bfloat16 *out[2][R];              // forward: h, n; backward: dx, dy
     const __nv_bfloat16 *w[3];             // w_post, gate, w_pre (nullptr: not there)
-    float *partial;                        // backward: [blocks][3][hidden]
+    float *partial;                        // backward: [blocks][3][hidden]; nullptr without weights
     int has[4];                            // which of the inputs are read
     int n_in;                              // how many
     float scale, eps, inv;                 // inv: 1 / hidden
@@ -370,6 +370,7 @@ __global__ void __launch_bounds__(kWarp ? 32 * kWarpRows : 512, kWarp || (!kBwd 
         while (globaltimer_ns() - t0 < 200000ull) { }
     }
     if constexpr (kBwd) {
+        if (!p.partial) return;                    // no weights, no sums
         float *to = p.partial + (size_t)blockIdx.x * 3 * p.hidden;
         if constexpr (kWarp) {                     // the groups' sums added one after another where the weights were
             float *sum = reinterpret_cast<float *>(smem);        // [3][hidden]: 3 rows of 4 bytes where 3 of 2 and a ring were
@@ -545,17 +546,20 @@ int run_bwd(const basp_plan *p, int hidden, const void *const *h_seq, const void
     if (w_pre) BASP_TRY(add_shards(p, &spans, hidden, dn, false, 0, prm.in[3]));
     BASP_TRY(add_shards(p, &spans, hidden, dx_seq, true, 0, const_cast<const __nv_bfloat16 **>(prm.out[0])));
     if (dy_seq) BASP_TRY(add_shards(p, &spans, hidden, dy_seq, true, 1, const_cast<const __nv_bfloat16 **>(prm.out[1])));
-    if (w_post || gate || w_pre) BASP_TRY(spans.add_out(workspace, bwd_workspace_bytes(hidden)));
-    if ((w_post || gate || w_pre) && workspace_bytes < bwd_workspace_bytes(hidden)) return BASP_ERR_WORKSPACE;
+    const bool weights = w_post || gate || w_pre;
+    if (weights) {
+        BASP_TRY(spans.add_out(workspace, bwd_workspace_bytes(hidden)));
+        if (workspace_bytes < bwd_workspace_bytes(hidden)) return BASP_ERR_WORKSPACE;
+    }
     BASP_TRY(spans.overlaps());
     prm.has[0] = prm.has[3] = w_pre != nullptr;
     prm.has[1] = w_post || gate;
     prm.has[2] = dh_out != nullptr;
-    prm.partial = (float *)workspace;
+    prm.partial = weights ? (float *)workspace : nullptr;       // (without weights nothing is known of the workspace)
     prm.scale = res_scale; prm.eps = eps;
     int blocks;
     BASP_TRY((launch<true, R>(p, prm, hidden, st, &blocks)));
-    if (w_post || gate || w_pre) {
+    if (weights) {
         BASP_CUDA_TRY(launch_early(norm_dw_kernel, dim3(hidden / 8, 3), 256, st, (const float *)prm.partial, hidden, blocks,
                                    w_post ? dw_post : (float *)nullptr, gate ? dgate : (float *)nullptr, w_pre ? dw_pre : (float *)nullptr));
         basp_count_launch(1);

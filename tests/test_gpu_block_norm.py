@@ -202,3 +202,21 @@ def test_in_place_and_zero_rows(basp, hidden):
         basp.basp_block_norm_bwd(pl, hidden, X, Y, a, b, (a, b)[over], Y, *s1, space, **kw)
         assert all(torch.equal(p, q) or (torch.isnan(p) == torch.isnan(q)).all() for p, q in zip(dx + dy + s0, (a, b)[over] + Y + s1))
     assert all(torch.isfinite(t.float()).all() for t in dx + dy + s0)
+
+
+@pytest.mark.parametrize("hidden", [64, 520, 4096])
+def test_no_weights_no_workspace(basp, hidden):
+    """Without weights there are no sums: the workspace may be missing, small, or full of someone else's data, which stays."""
+    w = SHAPES["uneven"]
+    pl, mk, _ = setup(basp, w, hidden)
+    dh = mk()
+    guard = torch.full((64 + 148 * 16 * 3 * hidden * 4,), 7, dtype=torch.uint8, device="cuda")       # more than any number of blocks could write
+    want = [(0.5 * f64(t), f64(t)) for t in dh]
+    basp.basp_clear_status()
+    for space in (None, guard[16:32], guard[17:18]):
+        dx, dy = blank(cuda(dh)), blank(cuda(dh))
+        basp.basp_block_norm_bwd(pl, hidden, None, None, cuda(dh), None, dx, dy, None, None, None, space, res_scale=0.5, eps=EPS)
+        basp.basp_get_status()
+        for r in range(pl.N):
+            assert np.array_equal(f64(dx[r]), want[r][1]) and np.array_equal(f64(dy[r]), want[r][0])       # a power of two: exact
+        assert (guard == 7).all()
