@@ -80,8 +80,8 @@ __device__ __forceinline__ bool mf_get_item(const MaskedFwdParams<R> &p, int rou
     it.hkv = (int)fdiv((uint32_t)it.h, p.div_q_per_kv);
     if (p.score.range) {
         const MaskFwdEntry *at = p.score.fwd + e;
-        const int4 a = __ldg(reinterpret_cast<const int4 *>(at)), b = __ldg(reinterpret_cast<const int4 *>(at) + 1),
-                   c = __ldg(reinterpret_cast<const int4 *>(at) + 2);
+        const int4 *from = reinterpret_cast<const int4 *>(at);
+        const int4 a = ld_written(from), b = ld_written(from + 1), c = ld_written(from + 2);
         it.seq = min(max(a.x, 0), p.score.B - 1);
         it.block = min(max(a.y, 0), p.n_blocks - 1);
         it.t[0] = MaskTile{b.x, b.y, b.z, b.w};
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kMfThreads, 1) attn_masked_fwd_kernel(const __
             // keys [lo, hi) of this thread's row
             int lo = 0, hi = 0;
             if (p.score.range) {
-                const int2 range = __ldg(p.score.range + ((size_t)item.seq * p.n_tiles + qt) * kTile + row);
+                const int2 range = ld_written(p.score.range + ((size_t)item.seq * p.n_tiles + qt) * kTile + row);
                 lo = range.x;
                 hi = range.y;
             } else if (s_pos < p.S) {

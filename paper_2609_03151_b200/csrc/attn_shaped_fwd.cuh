@@ -105,13 +105,13 @@ __global__ void __launch_bounds__(kSfThreads, 1) attn_shaped_fwd_kernel(const __
             // keys [lo, hi) of this thread's row
             int lo = 0, hi = 0;
             if (p.score.range) {
-                const int2 range = __ldg(p.score.range + ((size_t)item.seq * p.n_tiles + qt) * kTile + row);
+                const int2 range = ld_written(p.score.range + ((size_t)item.seq * p.n_tiles + qt) * kTile + row);
                 lo = range.x;
                 hi = range.y;
             } else if (in_seq) {
                 hi = p.causal ? s_pos + 1 : p.S;
             }
-            [[maybe_unused]] const float slope = kBias ? __ldg(p.score.slopes + (item.r % p.K) * p.Hq_l + item.h) * 1.4426950408889634f : 0.f;
+            [[maybe_unused]] const float slope = kBias ? ld_written(p.score.slopes + (item.r % p.K) * p.Hq_l + item.h) * 1.4426950408889634f : 0.f;
             [[maybe_unused]] const bool steep = kForm == 2 || fabsf(slope) * (float)(kHalf - 1) > 96.f;
             float ref = kForm == 0 ? 0.f : -INFINITY;
             if constexpr (kForm == 0 && kBias) {

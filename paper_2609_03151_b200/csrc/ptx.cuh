@@ -204,6 +204,23 @@ __device__ __forceinline__ void mma_ss_pair(uint32_t d_tmem, uint64_t a_desc, ui
 // started so waits here until the previous one has finished and its writes can be read.
 __device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Loads of what a kernel may have written that this one was started under.  Behind wait_previous_kernel() that takes the ordinary load: __ldg
+// (ld.global.nc) wants memory that nothing writes from this kernel's start on, and may be moved ahead of the wait.
+__device__ __forceinline__ int4 ld_written(const int4 *p) {
+    int4 v;
+    asm volatile("ld.global.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int2 ld_written(const int2 *p) {
+    int2 v;
+    asm volatile("ld.global.v2.s32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float ld_written(const float *p) {
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
 
 // Instruction descriptor of kind::f16 with bf16 A and B, fp32 D.
 //   bits 4-5 D format (1 = f32) | 7-9 A format (1 = bf16) | 10-12 B format (1 = bf16)

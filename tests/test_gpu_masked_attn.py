@@ -348,3 +348,36 @@ def test_gradients_of_rows_with_few_keys(basp, D, kind):
                                  do=f64(do[0][0]))
         for got, n in ((dq, "dq"), (dk, "dk")):
             assert np.linalg.norm(f64(got[0][0]) - ref[n]) <= 2.0 ** -8 * np.linalg.norm(ref[n]), (cap, n)
+
+
+@pytest.mark.parametrize("S", [300, 8400])
+def test_a_mask_rewritten_between_calls(basp, S):
+    """One mask buffer filled for one batch after another, each read by the calls right behind it (which start under the mask's own launches: one
+    block up to 64 tiles, three launches above): the results with a wait after every call."""
+    pl = make_plan(basp, W(N=1, B=1, S=S, Hq=2, Hkv=1, D=64))
+    g = torch.Generator(device="cuda").manual_seed(S)
+    q, k, v = ([torch.randn((1, S, h, 64), generator=g, device="cuda").to(torch.bfloat16)] for h in (2, 1, 1))
+    at = torch.arange(S, dtype=torch.int32, device="cuda")[None]
+    batches = [(at % n).contiguous() for n in (S, 1, 130, 64, 257, 7)]
+    mask = torch.zeros(basp.basp_mask_bytes(pl), dtype=torch.uint8, device="cuda")
+    scores = [basp.basp_score(mask=mask), basp.basp_score(softcap=20.0, mask=mask)]
+    fresh = lambda: [[([torch.empty_like(q[0])], [torch.empty((1, 2, S), device="cuda")]) for _ in scores] for _ in batches]
+
+    def calls(pos, out, pause):
+        basp.basp_mask_packed(pl, pos, mask)
+        pause()
+        for score, (o, lse) in zip(scores, out):
+            basp.basp_attn_masked_fwd(pl, score, q, k, v, o, lse)
+            pause()
+
+    basp.basp_clear_status()
+    want, got = fresh(), [fresh() for _ in range(8)]
+    for pos, out in zip(batches, want):
+        calls(pos, out, torch.cuda.synchronize)
+    for turn in got:
+        for pos, out in zip(batches, turn):
+            calls(pos, out, lambda: None)
+    basp.basp_get_status()
+    for turn in got:
+        for a, b in zip(want, turn):
+            assert all(torch.equal(x[0], y[0]) for m, n in zip(a, b) for x, y in zip(m, n))

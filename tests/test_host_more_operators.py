@@ -2,12 +2,14 @@
 host: no GPU needed (every refusal comes before the first launch; the addresses are made up)."""
 import ctypes
 import math
+import os
 
 import numpy as np
 import pytest
 import torch
 
 import oracle
+from paper_2609_03151_b200 import build
 
 N = 4
 P = lambda xs: None if xs is None else (ctypes.c_void_p * len(xs))(*xs)
@@ -180,6 +182,16 @@ def test_block_norm_refusals(basp, plan):
     assert bwd(n=need - 1) == basp.BASP_ERR_WORKSPACE
     assert bwd(dwp=A(0x19) + 2) == bwd(ws=A(0x1c) + 4) == basp.BASP_ERR_ALIGN
     assert bwd(dx=table(0x10)) == bwd(dx=table(0x11)) == bwd(dy=table(0x15)) == bwd(dy=table(0x17)) == bwd(dwp=A(0x1a)) == basp.BASP_ERR_ALIAS
+
+
+def test_loads_of_what_an_overlapping_kernel_writes():
+    """The forward kernels start under the launch before them, which may be the one that writes the mask object: no load of theirs is one
+    that wants memory which nothing writes while the kernel runs."""
+    for name in ("attn_masked_fwd.cu", "attn_shaped_fwd.cuh"):
+        with open(os.path.join(build.CSRC, name)) as f:
+            code = f.read()
+        assert "__ldg" not in code and "ld.global.nc" not in code, name
+        assert name != "attn_masked_fwd.cu" or "launch_early_smem(attn_masked_fwd_kernel" in code
 
 
 def test_marshalling_refusals(basp, plan):
