@@ -220,3 +220,28 @@ def test_no_weights_no_workspace(basp, hidden):
         for r in range(pl.N):
             assert np.array_equal(f64(dx[r]), want[r][1]) and np.array_equal(f64(dy[r]), want[r][0])       # a power of two: exact
         assert (guard == 7).all()
+
+
+@pytest.mark.parametrize("hidden", [64, 328, 4096, 16384])
+@pytest.mark.parametrize("shape", ["uneven", "many rows"])
+def test_backward_in_place_to_the_bit(basp, shape, hidden):
+    """dx over dh_out or over dn, dy over y: every gradient has the bits that separate outputs get."""
+    w = SHAPES[shape]
+    pl, mk, (wp, g, wn) = setup(basp, w, hidden)
+    x, y, dh, dn = (cuda(mk()) for _ in range(4))
+    copy = lambda ts: [t.clone() for t in ts]
+    kw = dict(w_post=wp.cuda(), gate=g.cuda(), w_pre=wn.cuda(), res_scale=0.7, eps=EPS)
+    space = torch.empty(basp.basp_block_norm_bwd_workspace_bytes(pl, hidden), dtype=torch.uint8, device="cuda")
+    dx, dy, sums = blank(x), blank(x), [torch.empty(hidden, device="cuda") for _ in range(3)]
+    basp.basp_clear_status()
+    basp.basp_block_norm_bwd(pl, hidden, x, y, dh, dn, dx, dy, *sums, space, **kw)
+    want = dx + dy + sums
+    assert all(torch.isfinite(t.float()).all() and (t != 0).any() for t in want)
+    for over in (0, 1):
+        a, b, Y = copy(dh), copy(dn), copy(y)
+        s1 = [torch.full((hidden,), float("nan"), device="cuda") for _ in range(3)]
+        basp.basp_block_norm_bwd(pl, hidden, x, Y, a, b, (a, b)[over], Y, *s1, space, **kw)
+        for p, q in zip(want, (a, b)[over] + Y + s1):
+            assert torch.equal(p, q)
+        assert all(torch.equal(p, q) for p, q in zip((b, a)[over], (dn, dh)[over]))       # the other input stays
+    basp.basp_get_status()
