@@ -66,7 +66,14 @@ class _BaspAttention(torch.autograd.Function):
             else:
                 binding.basp_layer_fwd(plan, list(q_seq), list(k_seq), list(v_seq), o_seq, ws, lse_shards=lse,
                                        softmax_scale=softmax_scale)
-        ctx.score = score
+        if score is not None:
+            # the backward reads them again: as saved tensors, so that one which was written in between is refused (raw addresses and
+            # tensors of an inference mode have no record of that)
+            tensors = (score.slopes, score.mask)
+            kept = [isinstance(t, torch.Tensor) and not t.is_inference() for t in tensors]
+            ctx.score = (score.softcap, *(None if keep else t for t, keep in zip(tensors, kept)))
+            ctx.save_for_backward(*(t if keep else None for t, keep in zip(tensors, kept)))
+        ctx.has_score = score is not None
         ctx.plan, ctx.softmax_scale, ctx.ws, ctx.lse, ctx.fused, ctx.checkpoint8 = plan, softmax_scale, ws, lse, fused, checkpoint8
         ctx.shapes = [t.shape for t in shards]
         return tuple(o_seq)
@@ -92,11 +99,13 @@ class _BaspAttention(torch.autograd.Function):
                                        grads[2 * n:], ws2, softmax_scale=ctx.softmax_scale)
             return (None, None, None, None, None, None, *grads)
         qh, kh, vh, oh = (binding.as_shards(a) for a in binding.basp_layer_workspace_shards(plan, ctx.ws))
-        size = binding.basp_layer_bwd_workspace_bytes if ctx.score is None else binding.basp_layer_masked_bwd_workspace_bytes
+        size = binding.basp_layer_masked_bwd_workspace_bytes if ctx.has_score else binding.basp_layer_bwd_workspace_bytes
         ws2 = torch.empty(size(plan), dtype=torch.uint8, device=dev)
-        if ctx.score is not None:
+        if ctx.has_score:
+            softcap, *given = ctx.score
+            score = binding.basp_score(softcap, *(t if saved is None else saved for saved, t in zip(ctx.saved_tensors, given)))
             with torch.cuda.device(dev):
-                binding.basp_layer_masked_bwd(plan, ctx.score, qh, kh, vh, oh, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:],
+                binding.basp_layer_masked_bwd(plan, score, qh, kh, vh, oh, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:],
                                               ws2, softmax_scale=ctx.softmax_scale)
         else:
             binding.basp_layer_bwd(plan, qh, kh, vh, oh, ctx.lse, do_seq, grads[:n], grads[n:2 * n], grads[2 * n:], ws2,
@@ -109,8 +118,9 @@ def basp_attention(plan, q_seq, k_seq, v_seq, softmax_scale: float = 0.0, fused:
     all-to-alls and the attention of Section IV-C, differentiable.  Returns the list of n_ranks output shards in the
     layout of q_seq.  checkpoint8 (with fused): keep Q, K, V and O in 8 bits for the backward; O besides what others keep of it.
     score (without fused): a binding.basp_score, for capped scores, a bias by distance and masks of documents, prefixes, windows or
-    any key ranges; its tensors are read again by the backward and get no gradients.  Second derivatives are refused."""
-    if score is not None and score.slopes is not None and score.slopes.requires_grad:
+    any key ranges; its tensors are read again by the backward, which is refused where they were written in between (a mask refilled for the
+    next batch among it: a mask for each batch whose backward is to come), and get no gradients.  Second derivatives are refused."""
+    if score is not None and getattr(score.slopes, "requires_grad", False):
         raise ValueError("the slopes of a score are not differentiable")
     return list(_BaspAttention.apply(plan, float(softmax_scale), bool(fused), bool(checkpoint8), score, torch.is_grad_enabled(), *q_seq,
                                      *k_seq, *v_seq))

@@ -643,12 +643,19 @@ def _tokens(plan):
     return plan.cfg.micro_batch * plan.S
 
 
+def _refilled(mask):
+    """Tells torch that a mask object was written: a backward pass that has it saved is then refused, instead of taking another mask."""
+    if not mask.is_inference():
+        torch.autograd.graph.increment_version(mask)
+
+
 def basp_mask_ranges(plan, key_begin, key_end, mask, stream=None):
     """The mask object of key ranges: query i of sequence b sees the keys [key_begin[b, i], key_end[b, i]) (int32 [B, S]);
     mask: uint8 tensor of basp_mask_bytes(plan)."""
     m, n = _Marshal(), _tokens(plan)
     a = m.addresses(("key_begin", _I32, key_begin, n), ("key_end", _I32, key_end, n))
     _check(lib.basp_mask_ranges(plan.handle, *a, *m.space(mask), m.stream(stream)), "basp_mask_ranges")
+    _refilled(mask)
 
 
 def basp_mask_packed(plan, positions, mask, prefix=None, window=0, stream=None):
@@ -658,6 +665,7 @@ def basp_mask_packed(plan, positions, mask, prefix=None, window=0, stream=None):
     m, n = _Marshal(), _tokens(plan)
     a = m.addresses(("positions", _I32, positions, n), ("prefix", _I32, prefix, n))
     _check(lib.basp_mask_packed(plan.handle, *a, int(window), *m.space(mask), m.stream(stream)), "basp_mask_packed")
+    _refilled(mask)
 
 
 _pack_score = struct.Struct("f4xPPN").pack          # the fields of _Score

@@ -222,3 +222,49 @@ def test_block_norm_forms_through_autograd(basp, form):
     (ref * u.double()).sum().backward()
     for a, b in pairs:          # the sum h and the result rounded once each: 2^-8 of the norm and what a norm makes of it
         assert ((a.grad.double() - b.grad).norm() / b.grad.norm()).item() <= 2.0 ** -6
+
+
+def test_a_score_changed_between_the_passes(basp, setting):
+    """The backward reads the mask and the slopes again: one that was refilled in between is refused, as torch refuses any saved tensor that was
+    written; another mask or cap put into the score object changes nothing."""
+    from paper_2609_03151_b200.autograd import basp_attention
+    plan, pos, slopes, mask, rope, up = setting
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q, k, v = ([normal(g, 105, h, 64).requires_grad_() for _ in range(4)] for h in (4, 2, 2))
+    u = [normal(g, 105, 4, 64) for _ in range(4)]
+    begin = torch.zeros((2, 210), dtype=torch.int32, device="cuda")
+
+    def forward():
+        for t in q + k + v:
+            t.grad = None
+        score = basp.basp_score(8.0, slopes, mask)
+        return score, sum((o.float() * t.float()).sum() for o, t in zip(basp_attention(plan, q, k, v, score=score), u))
+
+    basp.basp_clear_status()
+    forward()[1].backward()
+    want = [t.grad.clone() for t in q + k + v]
+    for write in (lambda: basp.basp_mask_packed(plan, pos, mask), lambda: basp.basp_mask_ranges(plan, begin, begin + 1, mask), lambda: mask.zero_(),
+                  lambda: slopes.mul_(2.0)):
+        basp.basp_mask_packed(plan, pos, mask)
+        loss = forward()[1]
+        write()
+        with pytest.raises(RuntimeError, match="inplace"):
+            loss.backward()
+    slopes.div_(2.0)
+    basp.basp_mask_packed(plan, pos, mask)
+    score, loss = forward()
+    score.mask, score.slopes, score.softcap = None, None, 0.0
+    loss.backward()
+    basp.basp_get_status()
+    for t, ref in zip(q + k + v, want):
+        assert ((t.grad.float() - ref.float()).norm() / ref.float().norm()).item() <= 2.0 ** -8        # dQ's sums in another order
+    with torch.no_grad():                                  # no backward comes: the buffer is free for the next batch
+        basp_attention(plan, q, k, v, score=basp.basp_score(8.0, slopes, mask))
+        basp.basp_mask_packed(plan, pos, mask)
+    with torch.inference_mode():                           # a mask without a record of its writes serves as well
+        mask = torch.empty_like(mask)
+        basp.basp_mask_packed(plan, pos, mask)
+    forward()[1].backward()
+    basp.basp_get_status()
+    for t, ref in zip(q + k + v, want):
+        assert ((t.grad.float() - ref.float()).norm() / ref.float().norm()).item() <= 2.0 ** -8
