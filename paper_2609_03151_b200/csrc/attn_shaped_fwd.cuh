@@ -148,7 +148,14 @@ __global__ void __launch_bounds__(kSfThreads, 1) attn_shaped_fwd_kernel(const __
                     for (int i = 0; i < kHalf; i += 4)
 #pragma unroll
                         for (int k = 0; k < 2; ++k) top[k] = max3_abs(top[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
-                    far = fold || __any_sync(0xffffffffu, fmaxf(top[0], top[1]) > p.score.near_limit);
+                    const float largest = fmaxf(top[0], top[1]);
+                    far = fold || __any_sync(0xffffffffu, largest > p.score.near_limit);
+                    // -infinity stands for a hidden key from here on: a product beyond fp32 is the cap's lower end instead
+                    if (__builtin_expect(far && __any_sync(0xffffffffu, largest == INFINITY), 0)) {
+#pragma unroll
+                        for (int i = 0; i < kHalf; ++i)
+                            if (s[i] == 0xff800000u) s[i] = 0xff7fffffu;
+                    }
                 }
                 [[maybe_unused]] const bool placed = kForm != 0 && (steep || fold);
                 if constexpr (kForm != 0)

@@ -381,3 +381,45 @@ def test_a_mask_rewritten_between_calls(basp, S):
     for turn in got:
         for a, b in zip(want, turn):
             assert all(torch.equal(x[0], y[0]) for m, n in zip(a, b) for x, y in zip(m, n))
+
+
+@pytest.mark.parametrize("shaping", ["cap", "cap bias", "wide cap"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_capped_scores_beyond_fp32(basp, D, shaping):
+    """Products of 1e60 are infinite as raw scores; capped they are the cap, with its sign, and keys at -cap keep the weight that the formula
+    gives them: all of it where a row sees no others.  Tolerances as above, with the sums of magnitudes of the other features (where the
+    first one is not zero it decides the score alone); dV takes the forward's LSE, so its P has that error too."""
+    S, H = 300, 2
+    cap, bias = SHAPING[shaping]
+    pl = make_plan(basp, W(N=1, B=1, S=S, Hq=H, Hkv=H, D=D))
+    g = torch.Generator().manual_seed(D)
+    q, k, v, do = (torch.randn((1, S, H, D), generator=g) for _ in range(4))
+    q[..., 0], k[..., 0] = 0.0, 0.0
+    ordinary = float((q.abs().amax(1) * k.abs().amax(1)).sum(-1).max()) / D ** 0.5       # no sum of magnitudes without the first feature is larger
+    q[0, ::2, :, 0] = 1e30
+    kind = torch.arange(S) % 7
+    kind[:5] = 0
+    kind[128:256] = 0                                     # tile borders among keys at -cap, and a whole tile of them
+    k[0, kind == 0, :, 0], k[0, kind == 1, :, 0] = -1e30, 1e30
+    q, k, v, do = ([t.to(torch.bfloat16).cuda()] for t in (q, k, v, do))
+    slopes = torch.tensor([0.01, 0.1]) if bias else None
+    o, lse = [torch.full_like(q[0], float("nan"))], [torch.full((1, H, S), float("nan"), device="cuda")]
+    grads = [[torch.full_like(t[0], float("nan"))] for t in (q, k, v)]
+    mask = torch.empty(basp.basp_mask_bytes(pl), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(basp.basp_attn_masked_bwd_workspace_bytes(pl), dtype=torch.uint8, device="cuda")
+    # causal rows; windows of four keys, which in the whole tile are all at -cap; documents of 60
+    for pos, window in ((torch.arange(S), 0), (torch.arange(S), 4), (torch.arange(S) % 60, 0)):
+        basp.basp_mask_packed(pl, pos.int()[None].cuda(), mask, None, window)
+        begin, end = oracle.packed_ranges(pos[None].numpy(), None, window)
+        sc = basp.basp_score(cap, None if slopes is None else slopes.cuda(), mask)
+        basp.basp_clear_status()
+        basp.basp_attn_masked_fwd(pl, sc, q, k, v, o, lse)
+        basp.basp_attn_masked_bwd(pl, sc, q, k, v, o, do, lse, *grads, ws)
+        basp.basp_get_status()
+        ref = oracle.attn_shaped(*(f64(t[0][0]) for t in (q, k, v)), begin[0], end[0], cap, None if slopes is None else slopes.double().numpy(),
+                                 do=f64(do[0][0]))
+        dz = (D / 8 + 4) * 2.0 ** -23 * ordinary + 2.0 ** -21 * cap + (2.0 ** -22 * 0.1 * S if bias else 0.0)
+        close(lse[0][0].double().cpu().numpy(), ref["lse"], dz + 2.0 ** -20 * (1 + np.abs(ref["lse"])), "lse")
+        close(f64(o[0][0]), ref["o"], (2.0 ** -8 + 4 * dz) * ref["mag_o"] + 2.0 ** -8 * np.abs(ref["o"]), "o")
+        close(f64(grads[2][0][0]), ref["dv"], (2.0 ** -8 + 8 * dz + 2.0 ** -19 * cap) * ref["mag_dv"] + 2.0 ** -8 * np.abs(ref["dv"]), "dv")
+        assert all(torch.isfinite(t[0].float()).all() for t in grads)
