@@ -474,7 +474,8 @@ int basp_attn_masked_bwd(const basp_plan *plan, const basp_score *score, const v
 size_t basp_attn_masked_bwd_workspace_bytes(const basp_plan *plan);
 /* The whole layer with such scores, on sequence-sharded shards: basp_layer_fwd and basp_layer_bwd with the attention above in
  * their middle.  The forward's workspace is that of basp_layer_fwd (afterwards basp_layer_workspace_shards has what the backward
- * takes), the backward's has a size of its own. */
+ * takes), the backward's has a size of its own.  What the attention in the middle refuses is refused before the first launch; the score's
+ * tensors may lie neither in the workspace nor in anything else that the call writes (BASP_ERR_ALIAS). */
 int basp_layer_masked_fwd(const basp_plan *plan, const basp_score *score, const void *const *q_seq, const void *const *k_seq,
                           const void *const *v_seq, void *const *o_seq, float *const *lse_shards, void *workspace,
                           size_t workspace_bytes, float softmax_scale, void *stream);

@@ -3,6 +3,7 @@
 // the ranges and says which 128 x 128 tiles there are anything to do in.
 #pragma once
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -58,5 +59,15 @@ int dispatch_score(bool cap, bool bias, F &&f) {
     return bias ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
 
+inline float resolved_scale(const basp_plan *p, float softmax_scale) { return softmax_scale == 0.f ? 1.f / sqrtf((float)p->D) : softmax_scale; }
+
 // Checks a basp_score and fills in what the kernels take of it (attn_mask.cu).
 int basp_score_args(const basp_plan *p, const basp_score *score, float scale, ScoreArgs *out);
+
+// What basp_attn_masked_fwd and _bwd refuse, found without a launch (the layer asks before its first exchange).
+int basp_attn_masked_fwd_check(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                               const void *const *v_head, void *const *o_head, float *const *lse_shards, float softmax_scale);
+int basp_attn_masked_bwd_check(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                               const void *const *v_head, const void *const *o_head, const void *const *do_head,
+                               const float *const *lse_shards, void *const *dq_head, void *const *dk_head, void *const *dv_head,
+                               void *workspace, size_t workspace_bytes, float softmax_scale);

@@ -579,10 +579,10 @@ int mb_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
 
 extern "C" size_t basp_attn_masked_bwd_workspace_bytes(const basp_plan *p) { return p ? mb_workspace_bytes(p) : 0; }
 
-extern "C" int basp_attn_masked_bwd(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
-                                    const void *const *v_head, const void *const *o_head, const void *const *do_head,
-                                    const float *const *lse_shards, void *const *dq_head, void *const *dk_head, void *const *dv_head,
-                                    void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
+int basp_attn_masked_bwd_check(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                               const void *const *v_head, const void *const *o_head, const void *const *do_head,
+                               const float *const *lse_shards, void *const *dq_head, void *const *dk_head, void *const *dv_head,
+                               void *workspace, size_t workspace_bytes, float softmax_scale) {
     if (!pl || !score || !q_head || !k_head || !v_head || !o_head || !do_head || !lse_shards || !dq_head || !dk_head || !dv_head)
         return BASP_ERR_NULL;
     if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
@@ -603,7 +603,17 @@ extern "C" int basp_attn_masked_bwd(const basp_plan *pl, const basp_score *score
     BASP_TRY(spans.add_out(workspace, mb_workspace_bytes(pl)));
     if (workspace_bytes < mb_workspace_bytes(pl)) return BASP_ERR_WORKSPACE;
     BASP_TRY(spans.overlaps());
-    const float scale = softmax_scale == 0.f ? 1.f / sqrtf((float)pl->D) : softmax_scale;
+    ScoreArgs args;
+    return basp_score_args(pl, score, resolved_scale(pl, softmax_scale), &args);
+}
+
+extern "C" int basp_attn_masked_bwd(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                                    const void *const *v_head, const void *const *o_head, const void *const *do_head,
+                                    const float *const *lse_shards, void *const *dq_head, void *const *dk_head, void *const *dv_head,
+                                    void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
+    BASP_TRY(basp_attn_masked_bwd_check(pl, score, q_head, k_head, v_head, o_head, do_head, lse_shards, dq_head, dk_head, dv_head, workspace,
+                                        workspace_bytes, softmax_scale));
+    const float scale = resolved_scale(pl, softmax_scale);
     return pl->N <= 8 ? mb_run<8>(pl, score, q_head, k_head, v_head, o_head, do_head, lse_shards, dq_head, dk_head, dv_head,
                                   (char *)workspace, scale, (cudaStream_t)stream)
                       : mb_run<BASP_MAX_RANKS>(pl, score, q_head, k_head, v_head, o_head, do_head, lse_shards, dq_head, dk_head, dv_head,

@@ -541,9 +541,8 @@ int mf_run(const basp_plan *pl, const basp_score *score, const void *const *q, c
 
 }  // namespace
 
-extern "C" int basp_attn_masked_fwd(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
-                                    const void *const *v_head, void *const *o_head, float *const *lse_shards, float softmax_scale,
-                                    void *stream) {
+int basp_attn_masked_fwd_check(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                               const void *const *v_head, void *const *o_head, float *const *lse_shards, float softmax_scale) {
     if (!pl || !score || !q_head || !k_head || !v_head || !o_head) return BASP_ERR_NULL;
     if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
     if (pl->D < 16 || pl->D > 128 || pl->D % 16 != 0) return BASP_ERR_UNSUPPORTED;
@@ -559,7 +558,15 @@ extern "C" int basp_attn_masked_fwd(const basp_plan *pl, const basp_score *score
     if (score->slopes) BASP_TRY(spans.add_in(score->slopes, (size_t)pl->Hq * 4, 4));
     if (score->mask) BASP_TRY(spans.add_in(score->mask, basp_mask_bytes(pl)));
     BASP_TRY(spans.overlaps());
-    const float scale = softmax_scale == 0.f ? 1.f / sqrtf((float)pl->D) : softmax_scale;
+    ScoreArgs args;
+    return basp_score_args(pl, score, resolved_scale(pl, softmax_scale), &args);
+}
+
+extern "C" int basp_attn_masked_fwd(const basp_plan *pl, const basp_score *score, const void *const *q_head, const void *const *k_head,
+                                    const void *const *v_head, void *const *o_head, float *const *lse_shards, float softmax_scale,
+                                    void *stream) {
+    BASP_TRY(basp_attn_masked_fwd_check(pl, score, q_head, k_head, v_head, o_head, lse_shards, softmax_scale));
+    const float scale = resolved_scale(pl, softmax_scale);
     return pl->N <= 8 ? mf_run<8>(pl, score, q_head, k_head, v_head, o_head, lse_shards, scale, (cudaStream_t)stream)
                       : mf_run<BASP_MAX_RANKS>(pl, score, q_head, k_head, v_head, o_head, lse_shards, scale, (cudaStream_t)stream);
 }

@@ -1,6 +1,8 @@
 // Whole-layer entry points: the three-launch path (all-to-all, attention, reverse all-to-all)
 // through a caller-provided workspace, and the host-buffer wrapper around the fused kernel.
+#include "attn_mask.cuh"
 #include "common.cuh"
+#include "spans.h"
 
 #include <mutex>
 #include <vector>
@@ -31,10 +33,10 @@ extern "C" size_t basp_host_arena_bytes(const basp_plan *p) {
 }
 
 namespace {
-// The three-launch layer with `attend(qh, kh, vh, oh)` as its attention.
-template <typename Attend>
+// The three-launch layer with `attend(qh, kh, vh, oh)` as its attention; `check` of the same is asked before the first launch.
+template <typename Check, typename Attend>
 int layer_fwd_with(const basp_plan *p, const void *const *q_seq, const void *const *k_seq, const void *const *v_seq, void *const *o_seq,
-                   void *workspace, size_t workspace_bytes, float softmax_scale, void *stream, Attend &&attend) {
+                   void *workspace, size_t workspace_bytes, float softmax_scale, void *stream, Check &&check, Attend &&attend) {
     if (!p || !workspace) return BASP_ERR_NULL;
     if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
     if (!aligned16(workspace)) return BASP_ERR_ALIGN;
@@ -48,11 +50,29 @@ int layer_fwd_with(const basp_plan *p, const void *const *q_seq, const void *con
         vh[r] = w + (size_t)p->N * (qb + kb) + (size_t)r * kb;
         oh[r] = w + (size_t)p->N * (qb + 2 * kb) + (size_t)r * qb;
     }
-    int rc = basp_reshard_qkv_s2h(p, q_seq, k_seq, v_seq, qh, kh, vh, stream);
+    int rc = check(qh, kh, vh, oh);
+    if (rc != BASP_OK) return rc;
+    rc = basp_reshard_qkv_s2h(p, q_seq, k_seq, v_seq, qh, kh, vh, stream);
     if (rc != BASP_OK) return rc;
     rc = attend(qh, kh, vh, oh);
     if (rc != BASP_OK) return rc;
     return basp_reshard_h2s(p, p->Hq, oh, o_seq, stream);
+}
+
+// What the attention in the middle does not see: the sequence shards that a masked layer writes are there, and neither they nor the
+// workspace hold the tensors of the score, which every layer and both passes read.
+bool in_score(const basp_plan *p, const basp_score *score, const void *at, size_t bytes) {
+    const SpanSet::Span s{(uintptr_t)at, bytes, -1};
+    return (score->slopes && SpanSet::meet(s, {(uintptr_t)score->slopes, (size_t)p->Hq * 4, -1})) ||
+           (score->mask && SpanSet::meet(s, {(uintptr_t)score->mask, basp_mask_bytes(p), -1}));
+}
+int masked_shards(const basp_plan *p, const basp_score *score, void *const *shards, int heads) {
+    if (!shards) return BASP_ERR_NULL;
+    for (int r = 0; r < p->N; ++r) {
+        BASP_TRY(SpanSet::check(shards[r], 16));
+        if (in_score(p, score, shards[r], (size_t)p->Bl * basp_rank_tokens(p, r % p->K) * heads * p->D * 2)) return BASP_ERR_ALIAS;
+    }
+    return BASP_OK;
 }
 }  // namespace
 
@@ -60,6 +80,7 @@ extern "C" int basp_layer_fwd(const basp_plan *p, const void *const *q_seq, cons
                               const void *const *v_seq, void *const *o_seq, float *const *lse_shards,
                               void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
     return layer_fwd_with(p, q_seq, k_seq, v_seq, o_seq, workspace, workspace_bytes, softmax_scale, stream,
+                          [](void *const *, void *const *, void *const *, void *const *) { return BASP_OK; },
                           [&](void *const *qh, void *const *kh, void *const *vh, void *const *oh) {
                               return basp_attn_dispatch(p, qh, kh, vh, oh, lse_shards, softmax_scale, false, stream);
                           });
@@ -69,6 +90,11 @@ extern "C" int basp_layer_masked_fwd(const basp_plan *p, const basp_score *score
                                      const void *const *v_seq, void *const *o_seq, float *const *lse_shards, void *workspace,
                                      size_t workspace_bytes, float softmax_scale, void *stream) {
     return layer_fwd_with(p, q_seq, k_seq, v_seq, o_seq, workspace, workspace_bytes, softmax_scale, stream,
+                          [&](void *const *qh, void *const *kh, void *const *vh, void *const *oh) {
+                              BASP_TRY(basp_attn_masked_fwd_check(p, score, qh, kh, vh, oh, lse_shards, softmax_scale));
+                              if (in_score(p, score, workspace, basp_workspace_bytes(p))) return BASP_ERR_ALIAS;
+                              return masked_shards(p, score, o_seq, p->Hq);
+                          },
                           [&](void *const *qh, void *const *kh, void *const *vh, void *const *oh) {
                               return basp_attn_masked_fwd(p, score, qh, kh, vh, oh, lse_shards, softmax_scale, stream);
                           });
@@ -95,10 +121,10 @@ extern "C" size_t basp_layer_bwd_workspace_bytes(const basp_plan *p) {
 }
 
 namespace {
-// The layer's backward pass with `attend(doh, dqh, dkh, dvh, workspace, bytes)` as that of its attention.
-template <typename Attend>
+// The layer's backward pass with `attend(doh, dqh, dkh, dvh, workspace, bytes)` as that of its attention, and `check` of the same.
+template <typename Check, typename Attend>
 int layer_bwd_with(const basp_plan *p, const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq,
-                   void *workspace, size_t workspace_bytes, size_t need, float softmax_scale, void *stream, Attend &&attend) {
+                   void *workspace, size_t workspace_bytes, size_t need, float softmax_scale, void *stream, Check &&check, Attend &&attend) {
     if (!p || !workspace) return BASP_ERR_NULL;
     if (!scale_ok(softmax_scale)) return BASP_ERR_INVALID;
     if (!aligned16(workspace)) return BASP_ERR_ALIGN;
@@ -113,7 +139,9 @@ int layer_bwd_with(const basp_plan *p, const void *const *do_seq, void *const *d
         dvh[r] = w + (size_t)p->N * (2 * qb + kb) + (size_t)r * kb;
     }
     char *bwd_ws = w + (size_t)p->N * (2 * qb + 2 * kb);
-    int rc = basp_reshard_s2h(p, p->Hq, do_seq, doh, stream);
+    int rc = check(doh, dqh, dkh, dvh, bwd_ws, workspace_bytes - (size_t)(bwd_ws - w));
+    if (rc != BASP_OK) return rc;
+    rc = basp_reshard_s2h(p, p->Hq, do_seq, doh, stream);
     if (rc != BASP_OK) return rc;
     rc = attend(doh, dqh, dkh, dvh, bwd_ws, workspace_bytes - (size_t)(bwd_ws - w));
     if (rc != BASP_OK) return rc;
@@ -127,6 +155,7 @@ extern "C" int basp_layer_bwd(const basp_plan *p, const void *const *q_head, con
                               void *const *dv_seq, void *workspace, size_t workspace_bytes, float softmax_scale,
                               void *stream) {
     return layer_bwd_with(p, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes, basp_layer_bwd_workspace_bytes(p), softmax_scale, stream,
+                          [](void *const *, void *const *, void *const *, void *const *, void *, size_t) { return BASP_OK; },
                           [&](void *const *doh, void *const *dqh, void *const *dkh, void *const *dvh, void *ws, size_t bytes) {
                               return basp_attn_bwd(p, q_head, k_head, v_head, o_head, doh, lse_shards, dqh, dkh, dvh, ws, bytes,
                                                    softmax_scale, stream);
@@ -143,6 +172,14 @@ extern "C" int basp_layer_masked_bwd(const basp_plan *p, const basp_score *score
                                      const void *const *do_seq, void *const *dq_seq, void *const *dk_seq, void *const *dv_seq,
                                      void *workspace, size_t workspace_bytes, float softmax_scale, void *stream) {
     return layer_bwd_with(p, do_seq, dq_seq, dk_seq, dv_seq, workspace, workspace_bytes, basp_layer_masked_bwd_workspace_bytes(p), softmax_scale, stream,
+                          [&](void *const *doh, void *const *dqh, void *const *dkh, void *const *dvh, void *ws, size_t bytes) {
+                              BASP_TRY(basp_attn_masked_bwd_check(p, score, q_head, k_head, v_head, o_head, doh, lse_shards, dqh, dkh, dvh, ws, bytes,
+                                                                  softmax_scale));
+                              if (in_score(p, score, workspace, basp_layer_masked_bwd_workspace_bytes(p))) return BASP_ERR_ALIAS;
+                              BASP_TRY(masked_shards(p, score, dq_seq, p->Hq));
+                              BASP_TRY(masked_shards(p, score, dk_seq, p->Hkv));
+                              return masked_shards(p, score, dv_seq, p->Hkv);
+                          },
                           [&](void *const *doh, void *const *dqh, void *const *dkh, void *const *dvh, void *ws, size_t bytes) {
                               return basp_attn_masked_bwd(p, score, q_head, k_head, v_head, o_head, doh, lse_shards, dqh, dkh, dvh, ws,
                                                           bytes, softmax_scale, stream);

@@ -98,6 +98,56 @@ def test_masked_layer_refusals(basp, plan):
     assert bwd(n=n - 1) == basp.BASP_ERR_WORKSPACE
 
 
+def test_masked_layer_refuses_before_its_first_launch(basp, plan):
+    """What the attention in the middle of the layer refuses, and what the exchange behind it would, is refused before the exchange in front of it
+    (whose launch fails here, without a GPU, with another code); the score's tensors lie in nothing that the layer writes."""
+    need, size = basp.basp_workspace_bytes(plan), basp.basp_mask_bytes(plan)
+    ws, mask, slopes = 0x20_0000_0000, 0x21_0000_0000, 0x22_0000_0000
+
+    def score(cap=0.0, slopes=None, mask=None, mask_bytes=size):
+        return ctypes.byref(basp._Score(cap, slopes, mask, mask_bytes))
+
+    def fwd(sc=score(), lse=table(0x14), **kw):
+        a = dict(q=table(0x10), k=table(0x11), v=table(0x12), o=table(0x13))
+        a.update(kw)
+        return basp.lib.basp_layer_masked_fwd(plan.handle, sc, P(a["q"]), P(a["k"]), P(a["v"]), P(a["o"]), P(lse), ws, need, 0.0, None)
+
+    bytes_bwd = basp.basp_layer_masked_bwd_workspace_bytes(plan)
+
+    def bwd(sc=score(), **kw):
+        a = {n: table(0x40 + i) for i, n in enumerate(("q", "k", "v", "o", "lse", "do", "dq", "dk", "dv"))}
+        a.update(kw)
+        return basp.lib.basp_layer_masked_bwd(plan.handle, sc, *[P(t) for t in a.values()], ws, bytes_bwd, 0.0, None)
+
+    for call in (fwd, bwd):
+        if not torch.cuda.is_available():
+            assert call() == call(score(30.0, slopes, mask)) == basp.BASP_ERR_CUDA               # nothing to refuse: the launch
+        assert call(None) == basp.BASP_ERR_NULL
+        assert call(score(-1.0)) == call(score(math.nan)) == call(score(1e-13)) == basp.BASP_ERR_INVALID
+        assert call(score(slopes=slopes + 2)) == call(score(mask=mask + 8)) == basp.BASP_ERR_ALIGN
+        assert call(score(mask=mask, mask_bytes=size - 1)) == basp.BASP_ERR_WORKSPACE
+        # in the workspace's first shard (an input of the attention) and in its last bytes
+        n = need if call is fwd else bytes_bwd
+        for at in (ws, ws + n - 16):
+            assert call(score(mask=at)) == call(score(slopes=at)) == basp.BASP_ERR_ALIAS
+        missing, odd = {"lse": table(0x14)[:3] + [None]}, {"lse": table(0x14)[:3] + [table(0x14)[3] + 2]}
+        assert call(**missing) == basp.BASP_ERR_NULL and call(**odd) == basp.BASP_ERR_ALIGN
+    outs = {fwd: {"o": 0x13}, bwd: {"dq": 0x46, "dk": 0x47, "dv": 0x48}}
+    for call, named in outs.items():
+        for name, base in named.items():
+            t = table(base)
+            assert call(**{name: None}) == call(**{name: t[:3] + [None]}) == basp.BASP_ERR_NULL
+            assert call(**{name: t[:3] + [t[3] + 8]}) == basp.BASP_ERR_ALIGN
+            assert call(score(mask=t[1] + 64)) == call(score(slopes=t[2])) == basp.BASP_ERR_ALIAS
+    assert fwd(score(mask=table(0x14)[0])) == basp.BASP_ERR_ALIAS                                 # LSE is written too
+    for name in ("q", "k", "v", "o"):
+        assert bwd(**{name: table(0x10)[:3] + [None]}) == basp.BASP_ERR_NULL
+    for D in (40, 144):
+        other = basp.basp_plan_create(N, 2, 1024, 8, 4, D)
+        assert basp.lib.basp_layer_masked_fwd(other.handle, score(), P(table(0x10)), P(table(0x11)), P(table(0x12)), P(table(0x13)), None, ws,
+                                              basp.basp_workspace_bytes(other), 0.0, None) == basp.BASP_ERR_UNSUPPORTED
+
+
 def test_score_structure(basp):
     """What the binding packs is the library's structure."""
     m = type("M", (), {"space": lambda self, mask: (0x1234567890, 77)})()
