@@ -175,7 +175,8 @@ class _BlockNorm(torch.autograd.Function):
             binding.basp_block_norm(plan, hidden, x, y, h, after, w_post=w_post, gate=gate, w_pre=w_pre, res_scale=res_scale, eps=eps)
         ctx.plan, ctx.res_scale, ctx.eps, ctx.hidden, ctx.has_y = plan, res_scale, eps, hidden, has_y
         ctx.has = [t is not None for t in (w_post, gate, w_pre)]
-        ctx.shapes = [t.shape for t in x]
+        ctx.shapes, ctx.y_shapes = [t.shape for t in x], [t.shape for t in y or ()]
+        ctx.weight_shapes = [None if t is None else t.shape for t in (w_post, gate, w_pre)]
         ctx.save_for_backward(*[t for t in (w_post, gate, w_pre) if t is not None], *((h if has_y else x) if w_pre is not None else ()),
                               *(y if w_post is not None or gate is not None else ()))
         return tuple((h or []) + (after or []))
@@ -195,13 +196,14 @@ class _BlockNorm(torch.autograd.Function):
         # the stream's own gradient may be missing (the last sum's) where that through the norm is there
         dh = None if dn is not None and all(g is None for g in dh) else fill(dh)
         dx = [torch.empty(s, dtype=torch.bfloat16, device=dev) for s in ctx.shapes]
-        dy = [torch.empty_like(t) for t in dx] if ctx.has_y else None
+        dy = [torch.empty(s, dtype=torch.bfloat16, device=dev) for s in ctx.y_shapes] if ctx.has_y else None
         sums = [torch.empty(ctx.hidden, dtype=torch.float32, device=dev) if there else None for there in ctx.has]
         ws = torch.empty(binding.basp_block_norm_bwd_workspace_bytes(plan, ctx.hidden), dtype=torch.uint8, device=dev)
         with torch.cuda.device(dev):
             binding.basp_block_norm_bwd(plan, ctx.hidden, h, y, dh, dn, dx, dy, *sums, ws, w_post=w_post, gate=gate, w_pre=w_pre,
                                         res_scale=ctx.res_scale, eps=ctx.eps)
-        return (None, None, None, *[None if s is None else s.to(torch.bfloat16) for s in sums], *dx, *(dy or []))
+        return (None, None, None, *[None if s is None else s.to(torch.bfloat16).reshape(shape) for s, shape in zip(sums, ctx.weight_shapes)],
+                *dx, *(dy or []))
 
 
 def basp_block_norm(plan, x_seq, y_seq=None, w_post=None, gate=None, w_pre=None, res_scale: float = 1.0, eps: float = 1e-6):

@@ -268,3 +268,21 @@ def test_a_score_changed_between_the_passes(basp, setting):
     basp.basp_get_status()
     for t, ref in zip(q + k + v, want):
         assert ((t.grad.float() - ref.float()).norm() / ref.float().norm()).item() <= 2.0 ** -8
+
+
+def test_block_norm_takes_the_attention_output_as_it_is(basp):
+    """y in the attention's [tokens, heads, features], a weight of [1, hidden]: gradients in the inputs' own shapes, the bits of flat ones."""
+    from paper_2609_03151_b200.autograd import basp_block_norm
+    plan = basp.basp_plan_create(2, 1, 210, 4, 2, 64)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x, up = ([normal(g, 105, HIDDEN) for _ in range(2)] for _ in range(2))
+    y = [normal(g, 105, 4, 64) for _ in range(2)]
+    w = [normal(g, HIDDEN) for _ in range(3)]
+    grads = []
+    for shape, row in (((105, 4, 64), (1, HIDDEN)), ((105, HIDDEN), (HIDDEN,))):
+        leaves = [t.clone().requires_grad_() for t in x + [t.reshape(shape) for t in y] + [t.reshape(row) for t in w]]
+        h, n = basp_block_norm(plan, leaves[:2], leaves[2:4], *leaves[4:])
+        torch.autograd.backward(h + n, up + up)
+        assert all(t.grad.shape == t.shape for t in leaves)
+        grads.append([t.grad.flatten() for t in leaves])
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
