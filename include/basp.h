@@ -448,8 +448,9 @@ size_t basp_lm_loss_grad_workspace_bytes(const basp_plan *plan, int hidden, int 
  *                        begin_i = max(i - pos_i, i - window + 1),   end_i = max(i + 1, i - pos_i + prefix_i)
  *                      (where the two meet the window has the last word).  BASP_ERR_INVALID for a plan that is not causal.
  * Operands, layouts and limits as basp_attn_fwd and basp_attn_bwd; outputs may not overlap inputs (BASP_ERR_ALIAS).  bf16 operands, fp32
- * scores, softmax and sums, P and dS rounded to bf16 as operands.  What a mask hides is multiplied by zero: Q, K, V, O and dO have to
- * be finite numbers in hidden places and padding too.
+ * scores, softmax and sums, P and dS rounded to bf16 as operands of the tensor cores.  In the 2-norm O is off by 0.0019 to 0.0024, where the
+ * exact result rounded to bf16 is by 0.0017, dQ and dK by 0.0025 to 0.0029, up to 0.0041 where few keys of many have a query's weight
+ * (steep slopes).  What a mask hides is multiplied by zero: Q, K, V, O and dO have to be finite numbers in hidden places and padding too.
  * The backward pass takes the forward's O and LSE:
  *   P = exp(z - LSE),  dV_j = sum_i P_ij dO_i,  dZ_ij = P_ij (dO_i.v_j - dO_i.O_i),  dS = scale (1 - tanh^2) dZ,  dQ = dS K,  dK = dS^T Q
  * (no gradient for the slopes; queries of up to eight keys take sum_j P_ij dO_i.v_j in the place of dO_i.O_i, which is the same without O's
@@ -496,7 +497,8 @@ size_t basp_layer_masked_bwd_workspace_bytes(const basp_plan *plan);
  *                         beta_slow times are divided by stretch, a ramp over j between them;  factor = 0.1 ln(stretch) + 1
  *   BASP_ROPE_WAVELENGTH  (Llama 3) the same by the turns themselves, above high and below low, a ramp over them in between
  * and keeps them in turns per token as 64-bit fixed-point numbers: position x frequency wraps round where a whole turn does, so the
- * angle is exact to 2^-32 turns at any int32 position (negative ones too).  No tables in device memory.
+ * whole turns go without a rounding at any int32 position (negative ones too): the fraction that stays is good to 2^-32 turns, and to
+ * 2^-26 turns (10^-7 radian) as the fp32 number that the sine and cosine are taken of.  No tables in device memory.
  * positions: device int32 [B][S] in sequence order, or NULL for the place in the sequence.  inverse: 0 rotates; 1 is the transpose
  * (turned back, times factor): the gradient of the forward call.  q_out[r] may be q_seq[r] itself, k_out[r] k_seq[r]; no other
  * overlap.  Requires D a multiple of 16 up to 128, rotary_dim a multiple of 16 up to D.  fp32 arithmetic, one rounding to bf16. */

@@ -1,5 +1,6 @@
 // Backward with masked and shaped scores, head dimensions 80 .. 128: the pipeline of attn_bwd_d128.cuh (order of the products, TMEM
-// and stages as there).  What is different: a key tile's query tiles come from the mask object and may be none; the producer
+// and stages as there; the barriers and the order of issue are written out in both files: a change of one is a change of the other).
+// What is different: a key tile's query tiles come from the mask object and may be none; the producer
 // stages for every query the window of the tile's keys that it sees, and whether any of it matters; the probabilities carry
 // the cap and the bias, and dS the cap's derivative.
 #pragma once

@@ -14,7 +14,7 @@
 //   warps  0-15  softmax of query tile warp / 8, columns 64 (warp / 4 % 2) .. + 63 of its rows, and the epilogue of as many columns of O
 //   warp  16     TMA producer, 17 and 18 MMA issuers (S = Q K^T, O += P V), as in the plain kernel
 // TMEM: S | P_0 P_1 | O_0 | O_1 as there.  Registers: 104 a thread for the softmax, 56 for the rest, of the 96 that all are launched with.
-// 16K causal tokens, 32/8 heads of 128 (plain scores 1.55-1.7 ms): cap 50 2.05 ms, a bias 2.3, both 2.3, a cap that most tiles reach 3.3; with two
+// 16K causal tokens, 32/8 heads of 128 (plain scores 1.55-1.7 ms): cap 50 2.05-2.1 ms, a bias 2.3-2.5, both 2.3, a cap that most tiles reach 3.3; with two
 // warpgroups cap 50 2.49 ms (then with a polynomial of four terms; four warpgroups 1.97).
 #pragma once
 

@@ -4,7 +4,8 @@
 //   (x_u, x_v) -> factor (x_u cos a - x_v sin a,  x_v cos a + x_u sin a),  a = position theta_j
 //
 // The frequencies are 64-bit fixed-point turns per token: position x frequency in 64-bit integers drops whole turns by itself, and
-// the angle comes out to 2^-32 of a turn at any position, where fp32 (2^-24 of the angle) is 0.01 radian off at 128K.  So a lane makes
+// the fraction that is left is good to 2^-32 of a turn at any position (2^-26, some 10^-7 radian, once it is the fp32 argument of the sine
+// and cosine), where fp32 throughout (2^-24 of the angle) is 0.01 radian off at 128K.  So a lane makes
 // its eight angles from the position alone (an integer product and a sine and a cosine each) and no table is read.
 //
 // HBM-bound: 2 bytes read and 2 written per element.  A lane holds two vectors of 16 bytes, D / 16 lanes a head: in the half layout the two
