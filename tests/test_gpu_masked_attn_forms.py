@@ -260,3 +260,35 @@ def test_backward_on_two_streams(basp):
     for (_, _, S), a, b in zip(jobs, alone, out):
         assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
         assert torch.equal(a[0], b[0]) if S <= 128 else ((a[0].float() - b[0].float()).norm() / a[0].float().norm()).item() <= 2.0 ** -8
+
+
+@pytest.mark.parametrize("cap,biased", [(0.0, False), (20.0, False), (0.0, True), (120.0, True)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scale_of_the_caller(basp, D, cap, biased):
+    """Four times the default scale is the default on four times Q, to the bit (a power of two passes through every rounding); O without a place
+    for the LSE has the same bits."""
+    S, H = 300, 2
+    pl = basp.basp_plan_create(1, 1, S, H, H, D)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    q, k, v, do = (torch.randn((1, S, H, D), generator=g, device="cuda").to(torch.bfloat16) for _ in range(4))
+    pos = (torch.arange(S, device="cuda") % 140).int()
+    pos[-30:] = torch.arange(30, device="cuda") % 3                     # rows of up to eight keys too
+    mask = torch.empty(basp.basp_mask_bytes(pl), dtype=torch.uint8, device="cuda")
+    basp.basp_mask_packed(pl, pos[None].contiguous(), mask)
+    score = basp.basp_score(cap, torch.tensor([0.5, 0.01], device="cuda") if biased else None, mask)
+    ws = torch.empty(basp.basp_attn_masked_bwd_workspace_bytes(pl), dtype=torch.uint8, device="cuda")
+    basp.basp_clear_status()
+    got = []
+    for Q, scale in ((q, float(np.float32(1.0) / np.sqrt(np.float32(D))) * 4.0), (q * 4, 0.0)):
+        o, alone, lse = torch.full_like(q, float("nan")), torch.full_like(q, float("nan")), torch.empty((1, H, S), device="cuda")
+        grads = [[torch.full_like(t, float("nan"))] for t in (q, k, v)]
+        basp.basp_attn_masked_fwd(pl, score, [Q], [k], [v], [o], [lse], softmax_scale=scale)
+        basp.basp_attn_masked_fwd(pl, score, [Q], [k], [v], [alone], None, softmax_scale=scale)
+        basp.basp_attn_masked_bwd(pl, score, [Q], [k], [v], [o], [do], [lse], *grads, ws, softmax_scale=scale)
+        assert torch.equal(o, alone)
+        got.append((o, lse, *(t[0] for t in grads)))
+    basp.basp_get_status()
+    (o, lse, dq, dk, dv), (o4, lse4, dq4, dk4, dv4) = got
+    # dS has the scale as a factor: four times as large in the first call, and multiplied by a quarter of the second one's Q for dK
+    assert torch.equal(o, o4) and torch.equal(lse, lse4) and torch.equal(dv, dv4) and torch.equal(dk, dk4)
+    assert ((dq.float() - 4 * dq4.float()).norm() / dq.float().norm()).item() <= 2.0 ** -8              # the order of dQ's sums
