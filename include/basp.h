@@ -449,9 +449,9 @@ size_t basp_lm_loss_grad_workspace_bytes(const basp_plan *plan, int hidden, int 
  *                      (where the two meet the window has the last word).  BASP_ERR_INVALID for a plan that is not causal.
  * Operands, layouts and limits as basp_attn_fwd and basp_attn_bwd; outputs may not overlap inputs (BASP_ERR_ALIAS).  bf16 operands, fp32
  * scores, softmax and sums, P and dS rounded to bf16 as operands of the tensor cores.  In the 2-norm O is off by 0.0019 to 0.0024, where the
- * exact result rounded to bf16 is by 0.0017, dQ and dK by 0.0025 to 0.0029, up to 0.005 where some ten or twenty keys have a query's weight
- * (short windows, steep slopes).  A bias is an fp32 number, so a score has 2^-24 of |slope| |i - j| as an error.  What a mask hides is
- * multiplied by zero: Q, K, V, O and dO have to be finite numbers in hidden places and padding too.
+ * exact result rounded to bf16 is by 0.0017, dQ and dK by 0.0025 to 0.0029, up to 0.005 in a shard where few keys of more than eight have a
+ * query's weight (short windows, steep slopes, large scores).  A bias is an fp32 number, so a score has 2^-24 of |slope| |i - j| as an
+ * error.  What a mask hides is multiplied by zero: Q, K, V, O and dO have to be finite numbers in hidden places and padding too.
  * The backward pass takes the forward's O and LSE:
  *   P = exp(z - LSE),  dV_j = sum_i P_ij dO_i,  dZ_ij = P_ij (dO_i.v_j - dO_i.O_i),  dS = scale (1 - tanh^2) dZ,  dQ = dS K,  dK = dS^T Q
  * (no gradient for the slopes; queries of up to eight keys take sum_j P_ij dO_i.v_j in the place of dO_i.O_i, which is the same without O's

@@ -7,8 +7,8 @@
 // accumulator), walking the tile pairs of the mask object: a work item is a key tile and the query tiles that see some of it,
 // longest first.  A row without a key has LSE = -inf and takes no part; a key tile that nothing sees gets zeros.
 // P and dS become bf16 as operands of the products (the tensor cores take no wider ones at their full rate), everything else is fp32 up to the
-// results: dQ and dK are off by 0.0025 to 0.0029 (2-norm; 0.0017 for the exact result rounded), by up to 0.005 where some ten or twenty keys
-// have a query's weight (short windows, steep slopes) and the roundings of O count (mb_prepare_kernel).
+// results: dQ and dK are off by 0.0025 to 0.0029 (2-norm; 0.0017 for the exact result rounded), by up to 0.005 in a shard where few keys of
+// more than eight have a query's weight (short windows, steep slopes, large scores) and the roundings of P and O in Delta count (mb_prepare_kernel).
 // 16K causal tokens, 32/8 heads of 128: plain 5.4-5.6 ms (1000 TFLOP/s, as the causal kernel), through a mask object 5.96-6.1 (the tile's entry and
 // the rows' ranges, loaded and staged at every step), bias 5.7-5.9, cap 50 6.9-7.0, both 6.9-7.0.  The tensor pipe is busy for half of the time
 // on packed documents; the rest is instruction fetch, the chain of a step's products and the reductions of dQ.
